@@ -302,6 +302,113 @@ int adahop_vote_pattern(const int32_t *patterns, int n);
  * returns ADAHOP_E_INVALID_ARG (as a negative value) on bad arguments. */
 int adahop_select_strategy(adahop_pattern_t pattern_a, adahop_pattern_t pattern_b, int level, int *full_bf16);
 
+/* ---------------------------------------------------------------------------------------------
+ * Training operators around the products: the norms before and after a block, the gated activation
+ * of an MLP, and 8-bit checkpoints of activations, which the first two write on their way and whose
+ * readers are the backward passes and the weight gradient (Eq. 3 with X kept in 8 bits).
+ *
+ * adahop_tensor_t: a row-major [rows, cols] array, bf16 (f32 = 0) or float (f32 = 1); row r begins
+ * at element r * ld, ld >= cols (unused for a vector of cols elements).  Aligned to its elements;
+ * 16-byte aligned rows are not needed.  data = NULL: absent.
+ *
+ * adahop_ckpt8_t: OCP MXFP8 along the columns.  codes: E4M3, row r at codes + r * ld_codes (16-byte
+ * aligned, ld_codes >= cols and a multiple of 16; bytes past cols are neither read nor written).
+ * scales: E8M0 biased by 127, one per 32 consecutive columns (the last ones of an odd width fewer),
+ * row r at scales + r * ld_scales, ld_scales >= ceil(cols / 32).  Scale = 127 + floor(log2(amax)) - 8,
+ * not below 0; 0 for a block of zeros; amax is that of the finite elements.  Elements: round to
+ * nearest even, saturating at 448; infinities and NaN become NaN.  codes = NULL: absent.
+ *
+ * Sizes: 0 <= rows <= 2^21 (0: nothing is done, sums over rows are 0), 1 <= cols <= 2^21,
+ * rows * cols < 2^35; cols <= 16384 for the block norm.
+ * All sums are in fp32 in an order that depends on the sizes alone; bf16 outputs are rounded once.
+ * No output may overlap an input, except where stated.
+ * ------------------------------------------------------------------------------------------- */
+typedef struct {
+    void *data;
+    int64_t ld;
+    int f32;
+} adahop_tensor_t;
+
+typedef struct {
+    uint8_t *codes, *scales;
+    int64_t ld_codes, ld_scales;
+} adahop_ckpt8_t;
+
+int adahop_ckpt8_pack(int64_t rows, int64_t cols, const adahop_tensor_t *x, const adahop_ckpt8_t *out, void *stream);
+/* out = what the checkpoint stands for, times col_scale [cols] if that is not NULL.  With out in bf16 and no
+ * col_scale nothing is rounded (down to 2^-133): an operand for adahop_gemm. */
+int adahop_ckpt8_unpack(int64_t rows, int64_t cols, const adahop_ckpt8_t *x, const adahop_tensor_t *col_scale,
+                        const adahop_tensor_t *out, void *stream);
+
+/* Gated activation a = silu(g) * u, silu(g) = g / (1 + exp(-g)).
+ *   forward   reads g, u (one type), writes a and, where present, ckpt_g and ckpt_u.
+ *   backward  reads d_a and either ckpt_g and ckpt_u (both present) or g and u; writes
+ *             d_g = d_a u silu'(g), d_u = d_a silu(g) and, where present, a (again) and ckpt_a, so that a
+ *             need not be kept for the down projection's weight gradient.  d_g and d_u may be d_a, g or u
+ *             themselves (same address, ld and type).
+ * g and u may be the halves of one [rows, 2 cols] array, d_g and d_u likewise. */
+typedef struct {
+    int64_t rows, cols;
+    adahop_tensor_t g, u, a;
+    adahop_ckpt8_t ckpt_g, ckpt_u;
+    adahop_tensor_t d_a, d_g, d_u; /* backward only */
+    adahop_ckpt8_t ckpt_a;         /* backward only */
+} adahop_swiglu_t;
+
+int adahop_swiglu(const adahop_swiglu_t *p, void *stream);
+int adahop_swiglu_backward(const adahop_swiglu_t *p, void *stream);
+
+/* The norm after a block, its gate, the residual sum with its scales, and the norm before the next block:
+ *   yhat = y / sqrt(mean(y^2) + eps)            (post_norm = 0: yhat = y)
+ *   s    = residual_scale x + branch_scale gate * w_post * yhat
+ *   shat = s / sqrt(mean(s^2) + eps),  h = w_pre * shat
+ * with the means over a row.
+ *   forward   x absent: s is the branch alone; y absent (post_norm = 0, no gate): s = residual_scale x, as before the
+ *             first block.  s absent: not stored; h absent: no second norm.  w_post, w_pre, gate absent: 1.
+ *             gate: row r of the operand takes gate row r / gate_rows of `gates` (gates * gate_rows >= rows): one
+ *             for all (gates = 1), one per sequence, or one per token (gate_rows = 1).
+ *             rstd_post, rstd_pre (float [rows], or NULL): 1 / sqrt(...) of the two norms; ckpt_y, ckpt_s: yhat
+ *             and shat (without their weights) in 8 bits.  These, or y and s themselves, are what the backward needs.
+ *             x and s are of one type; x may be s.
+ *   backward  reads d_s, d_h (either may be absent), rstd_pre and ckpt_s or s if d_h is present, rstd_post if
+ *             post_norm, ckpt_y or y if post_norm or d_w_post or d_gate is wanted (8-bit checkpoints of both or of
+ *             neither), the weights, the gate and the scales; writes those present of d_x, d_y, d_w_post, d_w_pre
+ *             (float [cols]; d_w_pre needs d_h) and d_gate ([gates, cols]).  d_s, d_x (and s, where read) are of one
+ *             type, d_h, d_y (and y, where read) of one.  d_x may be d_s, d_y may be d_h.
+ *             workspace: device scratch of adahop_block_norm_backward_workspace_bytes(rows, cols, gate_rows) bytes,
+ *             gate_rows = 0 without a gate; 256-byte aligned, contents undefined on return.
+ * w_post and w_pre are vectors of cols elements. */
+typedef struct {
+    int64_t rows, cols;
+    int post_norm;
+    float eps, residual_scale, branch_scale; /* eps > 0 (forward) */
+    adahop_tensor_t x, y, w_post, w_pre;
+    adahop_tensor_t gate;
+    int64_t gates, gate_rows;
+    adahop_tensor_t s, h;
+    float *rstd_post, *rstd_pre;
+    adahop_ckpt8_t ckpt_y, ckpt_s;
+    adahop_tensor_t d_s, d_h, d_x, d_y, d_gate; /* backward only */
+    float *d_w_post, *d_w_pre;                  /* backward only */
+} adahop_block_norm_t;
+
+int adahop_block_norm(const adahop_block_norm_t *p, void *stream);
+size_t adahop_block_norm_backward_workspace_bytes(int64_t rows, int64_t cols, int64_t gate_rows);
+int adahop_block_norm_backward(const adahop_block_norm_t *p, void *workspace, size_t workspace_bytes, void *stream);
+
+/* Weight gradient from an 8-bit checkpoint of the layer's input:
+ *   C[n, d] = col_scale[d] * sum_t G[t, n] x[t, d]  (+ add[n, d])
+ * G: bf16 [tokens, d_out], 16-byte aligned, ld a multiple of 8.  x: a checkpoint of [tokens, d_in].  C: [d_out, d_in].
+ * col_scale [d_in] (or NULL): the weight of the norm whose shat the checkpoint holds, so that the same checkpoint serves
+ * adahop_block_norm_backward and every product that h feeds.  add (or NULL): what earlier micro-batches
+ * left; it may be C.  The products are of bf16 values (an E4M3 element times its power of two is one) with
+ * fp32 accumulation.  tokens = 0: C = add, or 0.  workspace: adahop_ckpt8_wgrad_workspace_bytes() bytes, 256-byte
+ * aligned, contents undefined on return. */
+size_t adahop_ckpt8_wgrad_workspace_bytes(int64_t tokens, int64_t d_out, int64_t d_in);
+int adahop_ckpt8_wgrad(int64_t tokens, int64_t d_out, int64_t d_in, const adahop_tensor_t *G, const adahop_ckpt8_t *x,
+                       const adahop_tensor_t *col_scale, const adahop_tensor_t *add, const adahop_tensor_t *C,
+                       void *workspace, size_t workspace_bytes, void *stream);
+
 /* hipError_t (as int) of the most recent failed HIP call on this thread, 0 if none. */
 int adahop_last_hip_error(void);
 const char *adahop_status_string(int status);

@@ -1,0 +1,121 @@
+// The norms after one block and before the next, with what stands between them (forward):
+//
+//     yhat = y / sqrt(mean(y^2) + eps),   s = alpha x + beta gate * w_post * yhat
+//     shat = s / sqrt(mean(s^2) + eps),   h = w_pre * shat
+//
+// in one pass: a workgroup holds a row in registers, eight consecutive elements per lane and piece, and sums its squares
+// twice.  Bound by the memory: x and y are read once, s, h and the 8-bit checkpoints of yhat and shat are written once.  The sums are in fp32; h and
+// the checkpoints are formed from s before its rounding to bf16, so that each output is rounded once.
+#include "ckpt8.h"
+#include "row_sums.h"
+
+namespace adahop {
+
+namespace {
+
+// C: pieces of 8 columns per lane; SF32, YF32: the type of x and s, and of y.
+template <int C, bool SF32, bool YF32> __global__ __launch_bounds__(ROW_THREADS) void k_block_norm(adahop_block_norm_t q)
+{
+    __shared__ row_sums_t<1> lds;
+    const int threads = blockDim.x, waves = threads >> 6;
+    int turn = 0, n[C];
+    float wpost[C][8], wpre[C][8], gate[C][8];
+#pragma unroll
+    for (int j = 0; j < C; ++j) {
+        const int c = (threadIdx.x + j * threads) * 8;
+        n[j] = (int)q.cols - c;
+#pragma unroll
+        for (int i = 0; i < 8; ++i) wpost[j][i] = wpre[j][i] = gate[j][i] = 1.0f;
+        if (n[j] > 0) {
+            if (q.w_post.data) load8_any(q.w_post, c, n[j], wpost[j]);
+            if (q.w_pre.data) load8_any(q.w_pre, c, n[j], wpre[j]);
+        }
+    }
+    const float over_cols = 1.0f / (float)q.cols;
+    int64_t gate_row = -1;
+    for (int64_t row = blockIdx.x; row < q.rows; row += gridDim.x) {
+        float z[C][8], v[C][8], sum[1];
+        if (q.gate.data && row / q.gate_rows != gate_row) {
+            gate_row = row / q.gate_rows;
+#pragma unroll
+            for (int j = 0; j < C; ++j)
+                if (n[j] > 0) load8_any(q.gate, gate_row * q.gate.ld + (threadIdx.x + j * threads) * 8, n[j], gate[j]);
+        }
+#pragma unroll
+        for (int j = 0; j < C; ++j) {
+            const int c = (threadIdx.x + j * threads) * 8;
+            widen8(q.x.data && n[j] > 0 ? load8<SF32>(q.x.data, row * q.x.ld + c, n[j]) : zero8<SF32>(), z[j]);
+            widen8(q.y.data && n[j] > 0 ? load8<YF32>(q.y.data, row * q.y.ld + c, n[j]) : zero8<YF32>(), v[j]);
+        }
+        if (q.post_norm) {
+            sum[0] = 0.0f;
+#pragma unroll
+            for (int j = 0; j < C; ++j)
+#pragma unroll
+                for (int i = 0; i < 8; ++i) sum[0] = __builtin_fmaf(v[j][i], v[j][i], sum[0]);
+            row_sums(lds, turn, waves, sum);
+            const float r = 1.0f / sqrtf(sum[0] * over_cols + q.eps);
+            if (q.rstd_post && threadIdx.x == 0) q.rstd_post[row] = r;
+#pragma unroll
+            for (int j = 0; j < C; ++j)
+#pragma unroll
+                for (int i = 0; i < 8; ++i) v[j][i] *= r;
+        }
+        if (q.ckpt_y.codes) {
+#pragma unroll
+            for (int j = 0; j < C; ++j) {
+                const packed8 k = pack8(v[j]);
+                if (n[j] > 0) store_packed8(q.ckpt_y, row, (threadIdx.x + j * threads) * 8, n[j], k);
+            }
+        }
+        sum[0] = 0.0f;
+#pragma unroll
+        for (int j = 0; j < C; ++j) {
+#pragma unroll
+            for (int i = 0; i < 8; ++i) {
+                z[j][i] = (q.x.data ? q.residual_scale * z[j][i] : 0.0f) + q.branch_scale * (v[j][i] * wpost[j][i] * gate[j][i]);
+                sum[0] = __builtin_fmaf(z[j][i], z[j][i], sum[0]);
+            }
+            if (q.s.data && n[j] > 0) store8<SF32>(q.s.data, row * q.s.ld + (threadIdx.x + j * threads) * 8, n[j], z[j]);
+        }
+        if (!q.h.data) continue;
+        row_sums(lds, turn, waves, sum);
+        const float r = 1.0f / sqrtf(sum[0] * over_cols + q.eps);
+        if (q.rstd_pre && threadIdx.x == 0) q.rstd_pre[row] = r;
+#pragma unroll
+        for (int j = 0; j < C; ++j) {
+            const int c = (threadIdx.x + j * threads) * 8;
+#pragma unroll
+            for (int i = 0; i < 8; ++i) z[j][i] *= r;
+            if (q.ckpt_s.codes) {
+                const packed8 k = pack8(z[j]);
+                if (n[j] > 0) store_packed8(q.ckpt_s, row, c, n[j], k);
+            }
+#pragma unroll
+            for (int i = 0; i < 8; ++i) z[j][i] *= wpre[j][i];
+            if (n[j] > 0) store8_any(q.h, row * q.h.ld + c, n[j], z[j]);
+        }
+    }
+}
+
+template <int C> int launch(const adahop_block_norm_t &q, int threads, unsigned groups, hipStream_t st)
+{
+    if (q.s.data ? q.s.f32 : q.x.f32)
+        q.y.f32 ? k_block_norm<C, true, true><<<groups, threads, 0, st>>>(q) : k_block_norm<C, true, false><<<groups, threads, 0, st>>>(q);
+    else
+        q.y.f32 ? k_block_norm<C, false, true><<<groups, threads, 0, st>>>(q) : k_block_norm<C, false, false><<<groups, threads, 0, st>>>(q);
+    return check_launch();
+}
+
+} // namespace
+
+int launch_block_norm(const adahop_block_norm_t &q, hipStream_t st)
+{
+    const int64_t pieces = ceil_div(q.cols, 8);
+    const int threads = (int)(pieces > ROW_THREADS ? ROW_THREADS : ceil_div(pieces, 64) * 64);
+    const int64_t most = 256 * (int64_t)(2048 / threads); // 256 compute units of 2048 threads at most
+    const unsigned groups = (unsigned)(q.rows < most ? q.rows : most);
+    return pieces > ROW_THREADS ? launch<2>(q, threads, groups, st) : launch<1>(q, threads, groups, st);
+}
+
+} // namespace adahop

@@ -175,6 +175,20 @@ size_t pattern_workspace_bytes(const adahop_operand_t &x);
 int launch_detect_pattern(const adahop_operand_t &x, double tau, double eps, int32_t *pattern_out, double *stats_out,
                           void *workspace, hipStream_t st);
 
+// Training operators around the products.
+int launch_ckpt8_pack(int64_t rows, int64_t cols, const adahop_tensor_t &x, const adahop_ckpt8_t &out, hipStream_t st);
+int launch_ckpt8_unpack(int64_t rows, int64_t cols, const adahop_ckpt8_t &x, const adahop_tensor_t &col_scale, const adahop_tensor_t &out, hipStream_t st);
+int launch_swiglu(const adahop_swiglu_t &q, hipStream_t st);
+int launch_swiglu_backward(const adahop_swiglu_t &q, hipStream_t st);
+int launch_block_norm(const adahop_block_norm_t &q, hipStream_t st);
+size_t block_norm_backward_workspace_bytes(int64_t rows, int64_t cols, int64_t gate_rows);
+// s32: d_s, d_x and s are fp32; y32: d_h, d_y and y are; kept: the saved tensors are the 8-bit checkpoints.
+int launch_block_norm_backward(const adahop_block_norm_t &q, bool s32, bool y32, bool kept, void *workspace, hipStream_t st);
+int launch_block_norm_no_rows(const adahop_block_norm_t &q, hipStream_t st); // sums over nothing
+size_t wgrad8_workspace_bytes(int64_t tokens, int64_t d_out, int64_t d_in);
+int launch_wgrad8(int64_t tokens, int64_t d_out, int64_t d_in, const adahop_tensor_t &G, const adahop_ckpt8_t &x, const adahop_tensor_t &col_scale,
+                  const adahop_tensor_t &add, const adahop_tensor_t &C, void *workspace, hipStream_t st);
+
 // One-time set-up per device (function attributes, device properties): the only state the library keeps.
 // need(dev) is true until mark(dev) has been called for that device; devices numbered 64 and above are set
 // up on every call.
