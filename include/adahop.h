@@ -312,7 +312,7 @@ int adahop_select_strategy(adahop_pattern_t pattern_a, adahop_pattern_t pattern_
  * 16-byte aligned rows are not needed.  data = NULL: absent.
  *
  * adahop_ckpt8_t: OCP MXFP8 along the columns.  codes: E4M3, row r at codes + r * ld_codes (16-byte
- * aligned, ld_codes >= cols and a multiple of 16; bytes past cols are neither read nor written).
+ * aligned, ld_codes >= cols and a multiple of 16; bytes past cols are not written, and what they hold does not matter).
  * scales: E8M0 biased by 127, one per 32 consecutive columns (the last ones of an odd width fewer),
  * row r at scales + r * ld_scales, ld_scales >= ceil(cols / 32).  Scale = 127 + floor(log2(amax)) - 8,
  * not below 0; 0 for a block of zeros; amax is that of the finite elements.  Elements: round to
@@ -399,6 +399,7 @@ int adahop_block_norm_backward(const adahop_block_norm_t *p, void *workspace, si
 /* Weight gradient from an 8-bit checkpoint of the layer's input:
  *   C[n, d] = col_scale[d] * sum_t G[t, n] x[t, d]  (+ add[n, d])
  * G: bf16 [tokens, d_out], 16-byte aligned, ld a multiple of 8.  x: a checkpoint of [tokens, d_in].  C: [d_out, d_in].
+ * ld, ld_codes and ld_scales of the inputs below 2^25.
  * col_scale [d_in] (or NULL): the weight of the norm whose shat the checkpoint holds, so that the same checkpoint serves
  * adahop_block_norm_backward and every product that h feeds.  add (or NULL): what earlier micro-batches
  * left; it may be C.  The products are of bf16 values (an E4M3 element times its power of two is one) with

@@ -37,6 +37,7 @@ int configure_oe_rowcol();
 int configure_oht();
 int configure_foid();
 int configure_iht_quantize();
+int configure_wgrad8();
 
 // Launchers (one per kernel family); each validates nothing and returns a status.
 // Stage-major copy of the scales for the tiled GEMM kernels [ceil(K/256)][rows][8].

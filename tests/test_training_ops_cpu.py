@@ -177,6 +177,7 @@ def test_wgrad_refuses():
     assert wgrad(T=-1) == wgrad(N=0) == wgrad(D=0) == wgrad(T=(1 << 21) + 1) == wgrad(N=1 << 20, D=1 << 16) == BAD
     assert wgrad(G=None) == wgrad(x=None) == wgrad(C_=None) == BAD
     assert wgrad(G=t(f32=1)) == wgrad(G=t(ld=68)) == wgrad(G=t(ld=56)) == wgrad(G=t(data=FAKE + 8)) == wgrad(G=t(data=None)) == BAD
+    assert wgrad(G=t(ld=1 << 25)) == wgrad(x=k(ld=1 << 25)) == wgrad(x=k(ls=1 << 25)) == BAD
     assert wgrad(x=k(ld=48)) == wgrad(x=k(ls=1)) == wgrad(x=k(codes=FAKE + 4)) == wgrad(x=k(codes=None)) == wgrad(x=k(codes=None, scales=None)) == BAD
     assert wgrad(C_=t(data=None)) == wgrad(C_=t(ld=63)) == wgrad(w=t(data=FAKE + 1)) == wgrad(add=t(ld=8)) == wgrad(add=t(f32=5)) == BAD
     L = ah.lib()
