@@ -25,7 +25,7 @@ namespace {
 typedef short v4s __attribute__((ext_vector_type(4)));
 typedef uint32_t rsrc_t __attribute__((ext_vector_type(4)));
 
-constexpr int STAGE = 64, STEPS = STAGE / 16; // tokens per stage; matrix-core steps in it
+constexpr int STAGE = 32, STEPS = STAGE / 16; // tokens per stage; matrix-core steps in it
 
 struct wgrad_t {
     adahop_tensor_t G, col_scale, add, C;
@@ -40,7 +40,7 @@ struct wgrad_t {
 __device__ __forceinline__ rsrc_t resource(const uint8_t *base, int64_t bytes)
 {
     base = uniform_ptr(base);
-    const int64_t most = bytes < 0 ? 0 : bytes > 0xfffffffc ? 0xfffffffc : bytes;
+    const int64_t most = bytes > 0x80000000 ? 0x80000000 : bytes; // a stage's offsets are below 2^31
     rsrc_t r;
     r.x = (uint32_t)(uint64_t)base;
     r.y = (uint32_t)((uint64_t)base >> 32);
@@ -60,9 +60,14 @@ __device__ __forceinline__ void dma16_bounded(rsrc_t r, uint32_t voff, uint32_t 
                  : "memory", "m0");
 }
 
-__device__ __forceinline__ __amdgpu_buffer_rsrc_t typed(rsrc_t r)
+// Lane i's byte at voff lands at lds_addr + 4 i as a word.
+__device__ __forceinline__ void dma1_bounded(rsrc_t r, uint32_t voff, uint32_t lds_addr)
 {
-    return __builtin_amdgcn_make_buffer_rsrc(reinterpret_cast<void *>((uint64_t)r.y << 32 | r.x), 0, (int)r.z, (int)r.w);
+    lds_addr = __builtin_amdgcn_readfirstlane(lds_addr);
+    asm volatile("s_mov_b32 m0, %2\n\ts_nop 0\n\tbuffer_load_ubyte %0, %1, 0 offen lds"
+                 :
+                 : "v"(voff), "s"(r), "s"(lds_addr)
+                 : "memory", "m0");
 }
 
 __device__ __forceinline__ u32x2 transposed(uint32_t lds_addr)
@@ -75,23 +80,73 @@ __device__ __forceinline__ float element(const adahop_tensor_t &t, int64_t at)
     return t.f32 ? static_cast<const float *>(t.data)[at] : bf16_one(static_cast<const uint16_t *>(t.data)[at]);
 }
 
-// Tiles of 64 MT x 64 NT of C by four waves of 32 MT x 32 NT.  Two buffers of a stage each: while a stage is multiplied, the next one's G is
-// copied and its X8 is loaded (step 0), converted and written (step 2); one barrier per stage, before step 3, in which the first operands of the
-// next stage are read.  The operands of a step are read during the step before it.
-template <int MT, int NT> struct tile_t {
+// C[r, c .. c + have) = v times scale, plus what is added.
+__device__ __forceinline__ void put4(const adahop_tensor_t &to, const adahop_tensor_t &add, int64_t r, int64_t c, int have, const float (&scale)[4], float4 v)
+{
+    float o[4] = {v.x * scale[0], v.y * scale[1], v.z * scale[2], v.w * scale[3]};
+    if (add.data) {
+        const int64_t at = r * add.ld + c;
+        if (have == 4 && add.f32) {
+            const u32x4 a = *reinterpret_cast<const u32x4_e4 *>(static_cast<const uint32_t *>(add.data) + at);
+#pragma unroll
+            for (int i = 0; i < 4; ++i) o[i] += __uint_as_float(a[i]);
+        } else {
+#pragma unroll
+            for (int i = 0; i < 4; ++i)
+                if (i < have) o[i] += element(add, at + i);
+        }
+    }
+    const int64_t at = r * to.ld + c;
+    if (to.f32) {
+        uint32_t *const p = static_cast<uint32_t *>(to.data) + at;
+        if (have == 4) {
+            const u32x4 w = {__float_as_uint(o[0]), __float_as_uint(o[1]), __float_as_uint(o[2]), __float_as_uint(o[3])};
+            *reinterpret_cast<u32x4_e4 *>(p) = w;
+        } else {
+#pragma unroll
+            for (int i = 0; i < 3; ++i)
+                if (i < have) p[i] = __float_as_uint(o[i]);
+        }
+    } else {
+        uint16_t *const p = static_cast<uint16_t *>(to.data) + at;
+        const u32x2 w = {bf16_pair(o[0], o[1]), bf16_pair(o[2], o[3])};
+        if (have == 4) {
+            typedef uint32_t u32x2_e2 __attribute__((ext_vector_type(2), aligned(2), may_alias));
+            *reinterpret_cast<u32x2_e2 *>(p) = w;
+        } else {
+#pragma unroll
+            for (int i = 0; i < 3; ++i)
+                if (i < have) p[i] = (uint16_t)(w[i >> 1] >> 16 * (i & 1));
+        }
+    }
+}
+
+// Tiles of 64 MT x 64 NT of C by four waves of 32 MT x 32 NT.
+//
+// A stage of G (bf16), of X8's codes and of its scales is copied to a ring of RING slots in LDS, RING - 1 stages ahead of its use.  During a
+// stage, each wave converts the part of the next one's codes that it has copied itself (step 0: it waits for its own copies alone),
+// into one of two buffers of bf16 rows.  One barrier per stage, before its last step, in which the first operands of the next stage are
+// read; the operands of a step are always read during the step before it, and the copies are issued behind the barrier: the slot that they go
+// to is one that every wave has read.
+template <int MT, int NT, int RING> struct tile_t {
     static constexpr int TM = 64 * MT, TN = 64 * NT, RA = 2 * TM, RB = 2 * TN;      // columns; bytes of a row in LDS
-    static constexpr uint32_t A = STAGE * RA, B = STAGE * RB, LDS = 2 * (A + B);    // bytes of a buffer; of all four
-    static constexpr int COPIES = STAGE * RA / 1024 / 4;                            // of G per wave and stage
-    static constexpr int PIECES = STAGE * TN / 16 / 256;                            // of 16 codes per lane and stage
-    static constexpr int ROWS_PER_COPY = 1024 / RA, ROWS_PER_PIECE = 256 / (TN / 16);
+    static constexpr uint32_t A = STAGE * RA, Q = STAGE * TN, S = 4 * 256, B = STAGE * RB; // bytes of a stage: G, codes, scales, bf16 of X8
+    static constexpr uint32_t Q0 = RING * A, S0 = Q0 + RING * Q, B0 = S0 + RING * S, LDS = B0 + 2 * B;
+    static constexpr int WAVE_ROWS = STAGE / 4;                                     // tokens whose codes and scales a wave copies and converts
+    static constexpr int COPIES = A / 1024 / 4, ROWS_PER_COPY = 1024 / RA;          // of G: per wave and stage
+    static constexpr int CODE_COPIES = Q / 1024 / 4, ROWS_PER_CODE_COPY = 1024 / TN;
+    static constexpr int ISSUED = COPIES + CODE_COPIES + 1;                         // copies per wave and stage
+    static constexpr int UNITS = WAVE_ROWS * TN / 8 / 64, ROWS_PER_UNIT = 512 / TN; // of 8 codes per lane
 };
 
-template <int MT, int NT> __global__ __launch_bounds__(256) void k_wgrad8(wgrad_t q)
+template <int N> __device__ __forceinline__ void wait_for_copies() { asm volatile("s_waitcnt vmcnt(%0)" ::"n"(N) : "memory"); } // all but the last N
+
+template <int MT, int NT, int RING> __global__ __launch_bounds__(256) void k_wgrad8(wgrad_t q)
 {
-    typedef tile_t<MT, NT> K;
+    typedef tile_t<MT, NT, RING> K;
     extern __shared__ __attribute__((aligned(1024))) uint8_t smem[];
     const int tid = threadIdx.x, lane = tid & 63, w = __builtin_amdgcn_readfirstlane(tid >> 6), wn = w >> 1, wd = w & 1;
-    const uint32_t lds = lds_address(smem);
+    const uint32_t lds = __builtin_amdgcn_readfirstlane(lds_address(smem));
 
     // Workgroups go round the eight XCDs; each takes a run of tiles, which it walks in columns of four tiles: what runs on it at a time
     // shares four tiles of G's columns and eight of X's (half as many bytes each).
@@ -101,63 +156,76 @@ template <int MT, int NT> __global__ __launch_bounds__(256) void k_wgrad8(wgrad_
     const int64_t n0 = (int64_t)(4 * group + in % high) * K::TM, d0 = (int64_t)(in / high) * K::TN;
     const int64_t begin = (int64_t)blockIdx.y * q.slice, end = begin + q.slice < q.T ? begin + q.slice : q.T;
 
-    // Where this wave's and this lane's parts of a stage lie.
+    // What this wave and this lane copy of a stage.
     const uint32_t ld = (uint32_t)(q.G.ld * 2), ldc = (uint32_t)q.x.ld_codes, lds_s = (uint32_t)q.x.ld_scales;
     const int row = w * K::COPIES * K::ROWS_PER_COPY + lane / (K::RA / 16), chunk = lane % (K::RA / 16);
     uint32_t voff[2];
 #pragma unroll
     for (int i = 0; i < 2; ++i) // copies of even and odd number
         voff[i] = (uint32_t)row * ld + (((chunk >> 2) ^ ((row + i * K::ROWS_PER_COPY) & 3)) * 64 + (chunk & 3) * 16);
-    const int prow = tid / (K::TN / 16), pc = tid % (K::TN / 16);
+    const uint32_t qoff = (uint32_t)(w * K::WAVE_ROWS + lane / (K::TN / 16)) * ldc + lane % (K::TN / 16) * 16;
+    constexpr int BLOCKS = K::TN / 32; // scales of a row; lanes without one read past the end
+    const uint32_t soff = lane < K::WAVE_ROWS * BLOCKS ? (uint32_t)(w * K::WAVE_ROWS + lane / BLOCKS) * lds_s + lane % BLOCKS : 0xfffffff0u;
     const uint8_t *gp = reinterpret_cast<const uint8_t *>(q.G.data) + begin * q.G.ld * 2 + n0 * 2;
     const uint8_t *xp = q.x.codes + begin * q.x.ld_codes + d0, *sp = q.x.scales + begin * q.x.ld_scales + (d0 >> 5);
-    int64_t left = end - begin; // tokens from the stage at hand on
+    int64_t ahead = end - begin, left = ahead; // tokens from the stage that is copied next on, and from the one at hand on
     // bytes of a row of the tile that exist, in whole words
     const int64_t ge = ((q.N - n0) * 2 + 3) & ~3LL, xe = (q.D - d0 + 3) & ~3LL, se = (q.D - d0 + 31) >> 5;
 
-    uint32_t copy_to = lds + w * K::COPIES * 1024;
-    uint32_t put = lds + 2 * K::A + prow * K::RB + (((pc >> 1) ^ (prow & 3)) * 64 + (pc & 1) * 32);
+    // What it converts and reads.
+    const int urow = w * K::WAVE_ROWS + lane / (K::TN / 8), unit = lane % (K::TN / 8);
+    const uint32_t raw = lds + K::Q0 + w * K::WAVE_ROWS * K::TN + lane * 8, raw_scale = lds + K::S0 + w * 256 + (lane / (K::TN / 8) * BLOCKS + unit / 4) * 4;
+    uint32_t put[2]; // units of even and odd number
+#pragma unroll
+    for (int i = 0; i < 2; ++i) put[i] = lds + K::B0 + urow * K::RB + (((unit >> 2) ^ ((urow + i * K::ROWS_PER_UNIT) & 3)) * 64 + (unit & 3) * 16);
     const int s16 = lane & 15, h = lane >> 5;
-    uint32_t va[MT], vb[NT];
+    uint32_t ra[MT], rb[NT], va[MT], vb[NT];
 #pragma unroll
-    for (int m = 0; m < MT; ++m) va[m] = lds + (8 * h + (s16 >> 2)) * K::RA + (((wn * MT + m) ^ (s16 >> 2)) * 64) + 32 * ((lane >> 4) & 1) + 8 * (s16 & 3);
+    for (int m = 0; m < MT; ++m) va[m] = ra[m] = lds + (8 * h + (s16 >> 2)) * K::RA + (((wn * MT + m) ^ (s16 >> 2)) * 64) + 32 * ((lane >> 4) & 1) + 8 * (s16 & 3);
 #pragma unroll
-    for (int n = 0; n < NT; ++n) vb[n] = lds + 2 * K::A + (8 * h + (s16 >> 2)) * K::RB + (((wd * NT + n) ^ (s16 >> 2)) * 64) + 32 * ((lane >> 4) & 1) + 8 * (s16 & 3);
+    for (int n = 0; n < NT; ++n)
+        vb[n] = rb[n] = lds + K::B0 + (8 * h + (s16 >> 2)) * K::RB + (((wd * NT + n) ^ (s16 >> 2)) * 64) + 32 * ((lane >> 4) & 1) + 8 * (s16 & 3);
 
-    u32x4 codes[K::PIECES];
-    uint32_t scales[K::PIECES];
+    uint32_t slot_to = 0, slot_raw = 0, slot_at = 0, buffer = 0; // ring slots: copied to next, converted next, read next; bf16 buffer of slot_raw
+    const auto after = [](uint32_t slot) { return slot + 1 == RING ? 0 : slot + 1; };
     rsrc_t rg, rx, rs;
-    const auto aim = [&] { // at the stage that begins at gp, xp, sp
-        rg = resource(gp, left > 0 ? (left - 1) * (int64_t)ld + ge : 0);
-        rx = resource(xp, left > 0 ? (left - 1) * (int64_t)ldc + xe : 0);
-        rs = resource(sp, left > 0 ? (left - 1) * (int64_t)lds_s + se : 0);
+    const auto aim = [&] { // at the stage that is copied next
+        rg = resource(gp, ahead > 0 ? (ahead - 1) * (int64_t)ld + ge : 0);
+        rx = resource(xp, ahead > 0 ? (ahead - 1) * (int64_t)ldc + xe : 0);
+        rs = resource(sp, ahead > 0 ? (ahead - 1) * (int64_t)lds_s + se : 0);
     };
-    const auto copy = [&](int i) { dma16_bounded(rg, voff[i & 1] + i * K::ROWS_PER_COPY * ld, copy_to + i * 1024); };
+    const auto copy = [&](int i) {
+        if (i < K::COPIES) {
+            dma16_bounded(rg, voff[i & 1] + i * K::ROWS_PER_COPY * ld, lds + slot_to * K::A + (w * K::COPIES + i) * 1024);
+        } else if (i < K::COPIES + K::CODE_COPIES) {
+            const int j = i - K::COPIES;
+            dma16_bounded(rx, qoff + j * K::ROWS_PER_CODE_COPY * ldc, lds + K::Q0 + slot_to * K::Q + (w * K::CODE_COPIES + j) * 1024);
+        } else {
+            dma1_bounded(rs, soff, lds + K::S0 + slot_to * K::S + w * 256);
+        }
+    };
+    const auto copied = [&] {
+        gp += (int64_t)STAGE * ld;
+        xp += (int64_t)STAGE * ldc;
+        sp += (int64_t)STAGE * lds_s;
+        ahead -= STAGE;
+        slot_to = after(slot_to);
+    };
+    u32x2 codes[K::UNITS];
+    uint32_t scales[K::UNITS];
     const auto fetch = [&](int j) {
-        const uint32_t r = prow + j * K::ROWS_PER_PIECE;
-        codes[j] = __builtin_amdgcn_raw_buffer_load_b128(typed(rx), r * ldc + pc * 16, 0, 0);
-        scales[j] = __builtin_amdgcn_raw_buffer_load_b8(typed(rs), r * lds_s + (pc >> 1), 0, 0);
+        codes[j] = *(__attribute__((address_space(3))) u32x2 *)(raw + slot_raw * K::Q + j * 512);
+        scales[j] = *(__attribute__((address_space(3))) uint32_t *)(raw_scale + slot_raw * K::S + j * K::ROWS_PER_UNIT * BLOCKS * 4);
     };
-    const auto convert = [&](int j, int half) { // eight codes: 16 bytes of LDS
+    const auto convert = [&](int j) {
         const float scale = __uint_as_float(scales[j] << 23);
         u32x4 v;
 #pragma unroll
         for (int i = 0; i < 2; ++i) {
-            const uint32_t four = codes[j][2 * half + i];
-            v[2 * i] = __builtin_bit_cast(uint32_t, __builtin_amdgcn_cvt_scalef32_pk_bf16_fp8(four, scale, false));
-            v[2 * i + 1] = __builtin_bit_cast(uint32_t, __builtin_amdgcn_cvt_scalef32_pk_bf16_fp8(four, scale, true));
+            v[2 * i] = __builtin_bit_cast(uint32_t, __builtin_amdgcn_cvt_scalef32_pk_bf16_fp8(codes[j][i], scale, false));
+            v[2 * i + 1] = __builtin_bit_cast(uint32_t, __builtin_amdgcn_cvt_scalef32_pk_bf16_fp8(codes[j][i], scale, true));
         }
-        *(__attribute__((address_space(3))) u32x4 *)(put + j * K::ROWS_PER_PIECE * K::RB + half * 16) = v;
-    };
-    const auto next = [&] {
-        gp += (int64_t)STAGE * ld;
-        xp += (int64_t)STAGE * ldc;
-        sp += (int64_t)STAGE * lds_s;
-        left -= STAGE;
-    };
-    const auto other_buffer = [&] { // of what is written; what is read follows a step later
-        copy_to = lds + ((copy_to - lds) ^ K::A);
-        put = lds + 2 * K::A + ((put - lds - 2 * K::A) ^ K::B);
+        *(__attribute__((address_space(3))) u32x4 *)(put[j & 1] + buffer * K::B + j * K::ROWS_PER_UNIT * K::RB) = v;
     };
 
     v16f acc[MT][NT];
@@ -176,108 +244,131 @@ template <int MT, int NT> __global__ __launch_bounds__(256) void k_wgrad8(wgrad_
         else
             fa[set][tile - NT][part] = transposed(va[tile - NT] + (16 * step + 4 * part) * K::RA);
     };
+    const auto turn = [&] { // reads go to the next stage
+#pragma unroll
+        for (int m = 0; m < MT; ++m) va[m] = ra[m] + slot_at * K::A;
+#pragma unroll
+        for (int n = 0; n < NT; ++n) vb[n] = rb[n] + buffer * K::B;
+    };
     constexpr int READS = 2 * (MT + NT), SLOTS = MT * NT;
+    static_assert(STEPS == 2 && K::UNITS <= SLOTS, "a stage's work fits its two steps");
 
     if (left > 0) {
-        aim();
+#pragma unroll 1
+        for (int i = 0; i < RING - 1; ++i) {
+            aim();
 #pragma unroll
-        for (int i = 0; i < K::COPIES; ++i) copy(i);
-#pragma unroll
-        for (int j = 0; j < K::PIECES; ++j) fetch(j);
-#pragma unroll
-        for (int j = 0; j < K::PIECES; ++j) {
-            convert(j, 0);
-            convert(j, 1);
+            for (int c = 0; c < K::ISSUED; ++c) copy(c);
+            copied();
         }
-        other_buffer();
-        asm volatile("s_waitcnt vmcnt(0) lgkmcnt(0)\n\ts_barrier" ::: "memory");
+        wait_for_copies<(RING - 2) * K::ISSUED>();
+#pragma unroll
+        for (int j = 0; j < K::UNITS; ++j) fetch(j);
+#pragma unroll
+        for (int j = 0; j < K::UNITS; ++j) convert(j);
+        asm volatile("s_waitcnt lgkmcnt(0)\n\ts_barrier" ::: "memory");
 #pragma unroll
         for (int i = 0; i < READS; ++i) read(0, 0, i);
     }
     while (left > 0) {
-        next();
+        slot_raw = after(slot_raw);
+        buffer ^= 1;
         aim();
 #pragma unroll
         for (int step = 0; step < STEPS; ++step) {
-            if (step == STEPS - 1) {
-                asm volatile("s_waitcnt vmcnt(0) lgkmcnt(0)\n\ts_barrier" ::: "memory");
-                other_buffer();
-#pragma unroll
-                for (int m = 0; m < MT; ++m) va[m] = lds + ((va[m] - lds) ^ K::A);
-#pragma unroll
-                for (int n = 0; n < NT; ++n) vb[n] = lds + 2 * K::A + ((vb[n] - lds - 2 * K::A) ^ K::B);
+            if (step == 0) {
+                wait_for_copies<(RING - 3) * K::ISSUED>(); // of the next stage, this wave's
+            } else {
+                asm volatile("s_waitcnt lgkmcnt(0)\n\ts_barrier" ::: "memory"); // everyone's, and its converted rows
+                slot_at = after(slot_at);
+                turn();
             }
             ADAHOP_PIN();
 #pragma unroll
             for (int slot = 0; slot < SLOTS; ++slot) {
-                const int m = slot / NT, n = slot % NT, set = step & 1;
+                const int m = slot / NT, n = slot % NT;
                 const auto whole = [](const u32x2 (&f)[2]) { return make_uint4(f[0].x, f[0].y, f[1].x, f[1].y); };
-                acc[m][n] = mfma_bf16(whole(fa[set][m]), whole(fb[set][n]), acc[m][n]);
+                acc[m][n] = mfma_bf16(whole(fa[step][m]), whole(fb[step][n]), acc[m][n]);
 #pragma unroll
-                for (int i = slot * READS / SLOTS; i < (slot + 1) * READS / SLOTS; ++i) read(set ^ 1, (step + 1) % STEPS, i);
+                for (int i = slot * READS / SLOTS; i < (slot + 1) * READS / SLOTS; ++i) read(step ^ 1, step ^ 1, i);
                 if (step == 0) {
+                    if (slot < K::UNITS) fetch(slot);
+                    constexpr int FIRST = SLOTS / 2 < K::UNITS ? SLOTS - K::UNITS : SLOTS / 2;
+                    if (slot >= FIRST && slot < FIRST + K::UNITS) convert(slot - FIRST);
+                } else {
 #pragma unroll
-                    for (int i = slot * K::COPIES / SLOTS; i < (slot + 1) * K::COPIES / SLOTS; ++i) copy(i);
-#pragma unroll
-                    for (int j = slot * K::PIECES / SLOTS; j < (slot + 1) * K::PIECES / SLOTS; ++j) fetch(j);
-                }
-                if (step == 2) {
-#pragma unroll
-                    for (int i = slot * 2 * K::PIECES / SLOTS; i < (slot + 1) * 2 * K::PIECES / SLOTS; ++i) convert(i >> 1, i & 1);
+                    for (int i = slot * K::ISSUED / SLOTS; i < (slot + 1) * K::ISSUED / SLOTS; ++i) copy(i);
                 }
                 ADAHOP_PIN();
             }
         }
+        copied();
+        left -= STAGE;
     }
+    wait_for_copies<0>(); // those past the end
 
-    // lane: column lane % 32 of each tile of 32 x 32, rows 8 (i / 4) + 4 h + i % 4
-    const int64_t nb = n0 + wn * MT * 32 + 4 * h, db = d0 + wd * NT * 32 + (lane & 31);
-    if (q.part) {
-        float *const p = q.part + (int64_t)blockIdx.y * q.N * q.D;
+    // C, 32 rows of a wave at a time by way of its own patch of LDS, so that a lane has four consecutive columns of a row: 16-byte stores of
+    // whole rows, and little code.  In the accumulators a lane has column lane % 32 of a tile, rows 8 (i / 4) + 4 h + i % 4.
+    wait_for_copies<0>();
+    asm volatile("s_barrier" ::: "memory"); // no wave reads or copies any more
+    constexpr int PITCH = 32 * NT + 4, LANES = 8 * NT;
+    float *const patch = reinterpret_cast<float *>(smem) + w * 32 * PITCH;
+    const int c4 = lane % LANES * 4, r0 = lane / LANES;
+    const int64_t c = d0 + wd * NT * 32 + c4;
+    const int have = (int)(q.D - c < 4 ? q.D - c : 4);
+    float scale[4] = {1.0f, 1.0f, 1.0f, 1.0f};
+    if (q.col_scale.data) {
 #pragma unroll
-        for (int m = 0; m < MT; ++m)
-#pragma unroll
-            for (int n = 0; n < NT; ++n)
-#pragma unroll
-                for (int i = 0; i < 16; ++i) {
-                    const int64_t r = nb + 32 * m + 8 * (i >> 2) + (i & 3), c = db + 32 * n;
-                    if (r < q.N && c < q.D) p[r * q.D + c] = acc[m][n][i];
-                }
-        return;
+        for (int i = 0; i < 4; ++i)
+            if (i < have) scale[i] = element(q.col_scale, c + i);
     }
-    float scale[NT];
+    adahop_tensor_t to = q.C;
+    if (q.part) to = {q.part + (int64_t)blockIdx.y * q.N * q.D, q.D, 1};
 #pragma unroll
-    for (int n = 0; n < NT; ++n) scale[n] = q.col_scale.data && db + 32 * n < q.D ? element(q.col_scale, db + 32 * n) : 1.0f;
-#pragma unroll
-    for (int m = 0; m < MT; ++m)
+    for (int m = 0; m < MT; ++m) {
+        lds_between_lanes();
 #pragma unroll
         for (int n = 0; n < NT; ++n)
 #pragma unroll
-            for (int i = 0; i < 16; ++i) {
-                const int64_t r = nb + 32 * m + 8 * (i >> 2) + (i & 3), c = db + 32 * n;
-                if (r >= q.N || c >= q.D) continue;
-                float v = acc[m][n][i] * scale[n];
-                if (q.add.data) v += element(q.add, r * q.add.ld + c);
-                if (q.C.f32)
-                    static_cast<float *>(q.C.data)[r * q.C.ld + c] = v;
-                else
-                    static_cast<uint16_t *>(q.C.data)[r * q.C.ld + c] = (uint16_t)bf16_pair(v, 0.0f);
-            }
+            for (int i = 0; i < 16; ++i) patch[(8 * (i >> 2) + 4 * h + (i & 3)) * PITCH + 32 * n + (lane & 31)] = acc[m][n][i];
+        lds_between_lanes();
+        const int64_t first = n0 + (wn * MT + m) * 32 + r0;
+        if (have <= 0) continue;
+#pragma unroll 4
+        for (int i = 0; i < 32; i += 64 / LANES) {
+            const int64_t r = first + i;
+            if (r < q.N) put4(to, q.add, r, c, have, scale, *reinterpret_cast<const float4 *>(patch + (r0 + i) * PITCH + c4));
+        }
+    }
 }
 
-// The sums of the slices, in their order, and what the kernel above does with a single one's.
+// The sums of the slices, in their order, and what the kernel above does with a single one's.  A lane has four columns.
 __global__ __launch_bounds__(256) void k_wgrad8_join(wgrad_t q, int slices)
 {
-    const int64_t c = (int64_t)blockIdx.x * 256 + threadIdx.x, r = blockIdx.y + (int64_t)blockIdx.z * 65535;
+    const int64_t c = ((int64_t)blockIdx.x * 64 + (threadIdx.x & 63)) * 4, r = (int64_t)blockIdx.y * 4 + (threadIdx.x >> 6);
     if (c >= q.D || r >= q.N) return;
-    float v = 0.0f;
-    for (int s = 0; s < slices; ++s) v += q.part[((int64_t)s * q.N + r) * q.D + c];
-    if (q.col_scale.data) v *= element(q.col_scale, c);
-    if (q.add.data) v += element(q.add, r * q.add.ld + c);
-    if (q.C.f32)
-        static_cast<float *>(q.C.data)[r * q.C.ld + c] = v;
-    else
-        static_cast<uint16_t *>(q.C.data)[r * q.C.ld + c] = (uint16_t)bf16_pair(v, 0.0f);
+    const int have = (int)(q.D - c < 4 ? q.D - c : 4);
+    float v[4] = {}, scale[4] = {1.0f, 1.0f, 1.0f, 1.0f};
+    const uint32_t *p = reinterpret_cast<const uint32_t *>(q.part) + r * q.D + c;
+    if (have == 4) {
+#pragma unroll 4
+        for (int s = 0; s < slices; ++s, p += q.N * q.D) {
+            const u32x4 a = *reinterpret_cast<const u32x4_e4 *>(p);
+#pragma unroll
+            for (int i = 0; i < 4; ++i) v[i] += __uint_as_float(a[i]);
+        }
+    } else {
+        for (int s = 0; s < slices; ++s, p += q.N * q.D)
+#pragma unroll
+            for (int i = 0; i < 3; ++i)
+                if (i < have) v[i] += __uint_as_float(p[i]);
+    }
+    if (q.col_scale.data) {
+#pragma unroll
+        for (int i = 0; i < 4; ++i)
+            if (i < have) scale[i] = element(q.col_scale, c + i);
+    }
+    put4(q.C, q.add, r, c, have, scale, make_float4(v[0], v[1], v[2], v[3]));
 }
 
 struct plan_t {
@@ -309,9 +400,9 @@ int configure_wgrad8()
     int dev = 0;
     int rc = check_hip(hipGetDevice(&dev));
     if (rc != ADAHOP_OK || !g_once.need(dev)) return rc;
-    rc = check_hip(hipFuncSetAttribute(reinterpret_cast<const void *>(&k_wgrad8<4, 4>), hipFuncAttributeMaxDynamicSharedMemorySize, tile_t<4, 4>::LDS));
+    rc = check_hip(hipFuncSetAttribute(reinterpret_cast<const void *>(&k_wgrad8<4, 4, 5>), hipFuncAttributeMaxDynamicSharedMemorySize, tile_t<4, 4, 5>::LDS));
     if (rc == ADAHOP_OK)
-        rc = check_hip(hipFuncSetAttribute(reinterpret_cast<const void *>(&k_wgrad8<2, 2>), hipFuncAttributeMaxDynamicSharedMemorySize, tile_t<2, 2>::LDS));
+        rc = check_hip(hipFuncSetAttribute(reinterpret_cast<const void *>(&k_wgrad8<2, 2, 4>), hipFuncAttributeMaxDynamicSharedMemorySize, tile_t<2, 2, 4>::LDS));
     if (rc == ADAHOP_OK) g_once.mark(dev);
     return rc;
 }
@@ -329,16 +420,18 @@ int launch_wgrad8(int64_t T, int64_t N, int64_t D, const adahop_tensor_t &G, con
     if (rc != ADAHOP_OK) return rc;
     const plan_t p = plan_of(T, N, D);
     wgrad_t q = {G, col_scale, add, C, x, T, N, D, p.slices > 1 ? static_cast<float *>(workspace) : nullptr, p.slice, 0, 0};
+    if (q.part) q.col_scale = q.add = {}; // the slices' sums come first
     if (p.large) {
         q.nt = (uint32_t)ceil_div(N, 256), q.dt = (uint32_t)ceil_div(D, 256);
-        k_wgrad8<4, 4><<<dim3(q.nt * q.dt, p.slices), 256, tile_t<4, 4>::LDS, st>>>(q);
+        k_wgrad8<4, 4, 5><<<dim3(q.nt * q.dt, p.slices), 256, tile_t<4, 4, 5>::LDS, st>>>(q);
     } else {
         q.nt = (uint32_t)ceil_div(N, 128), q.dt = (uint32_t)ceil_div(D, 128);
-        k_wgrad8<2, 2><<<dim3(q.nt * q.dt, p.slices), 256, tile_t<2, 2>::LDS, st>>>(q);
+        k_wgrad8<2, 2, 4><<<dim3(q.nt * q.dt, p.slices), 256, tile_t<2, 2, 4>::LDS, st>>>(q);
     }
     rc = check_launch();
     if (rc != ADAHOP_OK || !q.part) return rc;
-    k_wgrad8_join<<<dim3((unsigned)ceil_div(D, 256), (unsigned)(N < 65535 ? N : 65535), (unsigned)ceil_div(N, 65535)), 256, 0, st>>>(q, p.slices);
+    q.col_scale = col_scale, q.add = add;
+    k_wgrad8_join<<<dim3((unsigned)ceil_div(D, 256), (unsigned)ceil_div(N, 4)), 256, 0, st>>>(q, p.slices);
     return check_launch();
 }
 
