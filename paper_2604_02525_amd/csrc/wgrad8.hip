@@ -60,11 +60,11 @@ __device__ __forceinline__ void dma16_bounded(rsrc_t r, uint32_t voff, uint32_t 
                  : "memory", "m0");
 }
 
-// Lane i's byte at voff lands at lds_addr + 4 i as a word.
-__device__ __forceinline__ void dma1_bounded(rsrc_t r, uint32_t voff, uint32_t lds_addr)
+// Lane i's word at voff lands at lds_addr + 4 i.
+__device__ __forceinline__ void dma4_bounded(rsrc_t r, uint32_t voff, uint32_t lds_addr)
 {
     lds_addr = __builtin_amdgcn_readfirstlane(lds_addr);
-    asm volatile("s_mov_b32 m0, %2\n\ts_nop 0\n\tbuffer_load_ubyte %0, %1, 0 offen lds"
+    asm volatile("s_mov_b32 m0, %2\n\ts_nop 0\n\tbuffer_load_dword %0, %1, 0 offen lds"
                  :
                  : "v"(voff), "s"(r), "s"(lds_addr)
                  : "memory", "m0");
@@ -121,31 +121,32 @@ __device__ __forceinline__ void put4(const adahop_tensor_t &to, const adahop_ten
     }
 }
 
-// Tiles of 64 MT x 64 NT of C by four waves of 32 MT x 32 NT.
+// Tiles of C by WN x WD waves of 32 MT x 32 NT.  Two waves per SIMD, in one workgroup or in two: a wave issues an instruction every four
+// cycles at most, and what it has to issue beside its matrix instructions does not fit between them.
 //
 // A stage of G (bf16), of X8's codes and of its scales is copied to a ring of RING slots in LDS, RING - 1 stages ahead of its use.  During a
 // stage, each wave converts the part of the next one's codes that it has copied itself (step 0: it waits for its own copies alone),
 // into one of two buffers of bf16 rows.  One barrier per stage, before its last step, in which the first operands of the next stage are
-// read; the operands of a step are always read during the step before it, and the copies are issued behind the barrier: the slot that they go
-// to is one that every wave has read.
-template <int MT, int NT, int RING> struct tile_t {
-    static constexpr int TM = 64 * MT, TN = 64 * NT, RA = 2 * TM, RB = 2 * TN;      // columns; bytes of a row in LDS
-    static constexpr uint32_t A = STAGE * RA, Q = STAGE * TN, S = 4 * 256, B = STAGE * RB; // bytes of a stage: G, codes, scales, bf16 of X8
+// read; the operands of a step are always read during the step before it.  The slot that is copied to is that of the stage before, which every
+// wave has read at that stage's barrier.
+template <int MT, int NT, int WN, int WD, int RING> struct tile_t {
+    static constexpr int WAVES = WN * WD, TM = 32 * WN * MT, TN = 32 * WD * NT, RA = 2 * TM, RB = 2 * TN;      // columns; bytes of a row in LDS
+    static constexpr uint32_t A = STAGE * RA, Q = STAGE * TN, S = STAGE * 16, B = STAGE * RB; // bytes of a stage: G, codes, scales, bf16 of X8
     static constexpr uint32_t Q0 = RING * A, S0 = Q0 + RING * Q, B0 = S0 + RING * S, LDS = B0 + 2 * B;
-    static constexpr int WAVE_ROWS = STAGE / 4;                                     // tokens whose codes and scales a wave copies and converts
-    static constexpr int COPIES = A / 1024 / 4, ROWS_PER_COPY = 1024 / RA;          // of G: per wave and stage
-    static constexpr int CODE_COPIES = Q / 1024 / 4, ROWS_PER_CODE_COPY = 1024 / TN;
+    static constexpr int WAVE_ROWS = STAGE / WAVES;                                 // tokens whose codes and scales a wave copies and converts
+    static constexpr int COPIES = A / 1024 / WAVES, ROWS_PER_COPY = 1024 / RA;          // of G: per wave and stage
+    static constexpr int CODE_COPIES = Q / 1024 / WAVES, ROWS_PER_CODE_COPY = 1024 / TN;
     static constexpr int ISSUED = COPIES + CODE_COPIES + 1;                         // copies per wave and stage
     static constexpr int UNITS = WAVE_ROWS * TN / 8 / 64, ROWS_PER_UNIT = 512 / TN; // of 8 codes per lane
 };
 
 template <int N> __device__ __forceinline__ void wait_for_copies() { asm volatile("s_waitcnt vmcnt(%0)" ::"n"(N) : "memory"); } // all but the last N
 
-template <int MT, int NT, int RING> __global__ __launch_bounds__(256) void k_wgrad8(wgrad_t q)
+template <int MT, int NT, int WN, int WD, int RING> __global__ __launch_bounds__(64 * WN * WD, 2) void k_wgrad8(wgrad_t q)
 {
-    typedef tile_t<MT, NT, RING> K;
+    typedef tile_t<MT, NT, WN, WD, RING> K;
     extern __shared__ __attribute__((aligned(1024))) uint8_t smem[];
-    const int tid = threadIdx.x, lane = tid & 63, w = __builtin_amdgcn_readfirstlane(tid >> 6), wn = w >> 1, wd = w & 1;
+    const int tid = threadIdx.x, lane = tid & 63, w = __builtin_amdgcn_readfirstlane(tid >> 6), wn = w / WD, wd = w % WD;
     const uint32_t lds = __builtin_amdgcn_readfirstlane(lds_address(smem));
 
     // Workgroups go round the eight XCDs; each takes a run of tiles, which it walks in columns of four tiles: what runs on it at a time
@@ -164,17 +165,27 @@ template <int MT, int NT, int RING> __global__ __launch_bounds__(256) void k_wgr
     for (int i = 0; i < 2; ++i) // copies of even and odd number
         voff[i] = (uint32_t)row * ld + (((chunk >> 2) ^ ((row + i * K::ROWS_PER_COPY) & 3)) * 64 + (chunk & 3) * 16);
     const uint32_t qoff = (uint32_t)(w * K::WAVE_ROWS + lane / (K::TN / 16)) * ldc + lane % (K::TN / 16) * 16;
-    constexpr int BLOCKS = K::TN / 32; // scales of a row; lanes without one read past the end
-    const uint32_t soff = lane < K::WAVE_ROWS * BLOCKS ? (uint32_t)(w * K::WAVE_ROWS + lane / BLOCKS) * lds_s + lane % BLOCKS : 0xfffffff0u;
+    // Scales: at most eight bytes of a row, at any address: four whole words from the one on that holds the first (copying the bytes one by
+    // one takes the kernel a millisecond longer at 16384 x 28672 x 8192).
+    const uint8_t *sp = q.x.scales + begin * q.x.ld_scales + (d0 >> 5);
+    const uint32_t odd = (uint32_t)(uintptr_t)sp & 3; // the same in every stage
+    sp -= odd;
+    const uint32_t soff = ((odd + (w * K::WAVE_ROWS + lane / 4) * lds_s) & ~3u) + lane % 4 * 4;
     const uint8_t *gp = reinterpret_cast<const uint8_t *>(q.G.data) + begin * q.G.ld * 2 + n0 * 2;
-    const uint8_t *xp = q.x.codes + begin * q.x.ld_codes + d0, *sp = q.x.scales + begin * q.x.ld_scales + (d0 >> 5);
+    const uint8_t *xp = q.x.codes + begin * q.x.ld_codes + d0;
     int64_t ahead = end - begin, left = ahead; // tokens from the stage that is copied next on, and from the one at hand on
     // bytes of a row of the tile that exist, in whole words
-    const int64_t ge = ((q.N - n0) * 2 + 3) & ~3LL, xe = (q.D - d0 + 3) & ~3LL, se = (q.D - d0 + 31) >> 5;
+    const int64_t ge = ((q.N - n0) * 2 + 3) & ~3LL, xe = (q.D - d0 + 3) & ~3LL, se = odd + ((q.D - d0 + 31) >> 5);
 
     // What it converts and reads.
     const int urow = w * K::WAVE_ROWS + lane / (K::TN / 8), unit = lane % (K::TN / 8);
-    const uint32_t raw = lds + K::Q0 + w * K::WAVE_ROWS * K::TN + lane * 8, raw_scale = lds + K::S0 + w * 256 + (lane / (K::TN / 8) * BLOCKS + unit / 4) * 4;
+    const uint32_t raw = lds + K::Q0 + w * K::WAVE_ROWS * K::TN + lane * 8;
+    uint32_t scale_at[K::UNITS];
+#pragma unroll
+    for (int j = 0; j < K::UNITS; ++j) {
+        const uint32_t r = urow + j * K::ROWS_PER_UNIT;
+        scale_at[j] = lds + K::S0 + r * 16 + ((odd + r * lds_s) & 3) + unit / 4;
+    }
     uint32_t put[2]; // units of even and odd number
 #pragma unroll
     for (int i = 0; i < 2; ++i) put[i] = lds + K::B0 + urow * K::RB + (((unit >> 2) ^ ((urow + i * K::ROWS_PER_UNIT) & 3)) * 64 + (unit & 3) * 16);
@@ -192,7 +203,7 @@ template <int MT, int NT, int RING> __global__ __launch_bounds__(256) void k_wgr
     const auto aim = [&] { // at the stage that is copied next
         rg = resource(gp, ahead > 0 ? (ahead - 1) * (int64_t)ld + ge : 0);
         rx = resource(xp, ahead > 0 ? (ahead - 1) * (int64_t)ldc + xe : 0);
-        rs = resource(sp, ahead > 0 ? (ahead - 1) * (int64_t)lds_s + se : 0);
+        rs = resource(sp, ahead > 0 ? ((ahead - 1) * (int64_t)lds_s + se + 3) & ~3LL : 0);
     };
     const auto copy = [&](int i) {
         if (i < K::COPIES) {
@@ -201,7 +212,7 @@ template <int MT, int NT, int RING> __global__ __launch_bounds__(256) void k_wgr
             const int j = i - K::COPIES;
             dma16_bounded(rx, qoff + j * K::ROWS_PER_CODE_COPY * ldc, lds + K::Q0 + slot_to * K::Q + (w * K::CODE_COPIES + j) * 1024);
         } else {
-            dma1_bounded(rs, soff, lds + K::S0 + slot_to * K::S + w * 256);
+            if (lane < 4 * K::WAVE_ROWS) dma4_bounded(rs, soff, lds + K::S0 + slot_to * K::S + w * K::WAVE_ROWS * 16);
         }
     };
     const auto copied = [&] {
@@ -215,7 +226,7 @@ template <int MT, int NT, int RING> __global__ __launch_bounds__(256) void k_wgr
     uint32_t scales[K::UNITS];
     const auto fetch = [&](int j) {
         codes[j] = *(__attribute__((address_space(3))) u32x2 *)(raw + slot_raw * K::Q + j * 512);
-        scales[j] = *(__attribute__((address_space(3))) uint32_t *)(raw_scale + slot_raw * K::S + j * K::ROWS_PER_UNIT * BLOCKS * 4);
+        scales[j] = *(__attribute__((address_space(3))) uint8_t *)(scale_at[j] + slot_raw * K::S);
     };
     const auto convert = [&](int j) {
         const float scale = __uint_as_float(scales[j] << 23);
@@ -295,10 +306,10 @@ template <int MT, int NT, int RING> __global__ __launch_bounds__(256) void k_wgr
                     if (slot < K::UNITS) fetch(slot);
                     constexpr int FIRST = SLOTS / 2 < K::UNITS ? SLOTS - K::UNITS : SLOTS / 2;
                     if (slot >= FIRST && slot < FIRST + K::UNITS) convert(slot - FIRST);
-                } else {
-#pragma unroll
-                    for (int i = slot * K::ISSUED / SLOTS; i < (slot + 1) * K::ISSUED / SLOTS; ++i) copy(i);
                 }
+                const int all = step * SLOTS + slot;
+#pragma unroll
+                for (int i = all * K::ISSUED / (2 * SLOTS); i < (all + 1) * K::ISSUED / (2 * SLOTS); ++i) copy(i);
                 ADAHOP_PIN();
             }
         }
@@ -400,9 +411,9 @@ int configure_wgrad8()
     int dev = 0;
     int rc = check_hip(hipGetDevice(&dev));
     if (rc != ADAHOP_OK || !g_once.need(dev)) return rc;
-    rc = check_hip(hipFuncSetAttribute(reinterpret_cast<const void *>(&k_wgrad8<4, 4, 5>), hipFuncAttributeMaxDynamicSharedMemorySize, tile_t<4, 4, 5>::LDS));
+    rc = check_hip(hipFuncSetAttribute(reinterpret_cast<const void *>(&k_wgrad8<4, 2, 2, 4, 5>), hipFuncAttributeMaxDynamicSharedMemorySize, tile_t<4, 2, 2, 4, 5>::LDS));
     if (rc == ADAHOP_OK)
-        rc = check_hip(hipFuncSetAttribute(reinterpret_cast<const void *>(&k_wgrad8<2, 2, 4>), hipFuncAttributeMaxDynamicSharedMemorySize, tile_t<2, 2, 4>::LDS));
+        rc = check_hip(hipFuncSetAttribute(reinterpret_cast<const void *>(&k_wgrad8<2, 2, 2, 2, 4>), hipFuncAttributeMaxDynamicSharedMemorySize, tile_t<2, 2, 2, 2, 4>::LDS));
     if (rc == ADAHOP_OK) g_once.mark(dev);
     return rc;
 }
@@ -423,10 +434,10 @@ int launch_wgrad8(int64_t T, int64_t N, int64_t D, const adahop_tensor_t &G, con
     if (q.part) q.col_scale = q.add = {}; // the slices' sums come first
     if (p.large) {
         q.nt = (uint32_t)ceil_div(N, 256), q.dt = (uint32_t)ceil_div(D, 256);
-        k_wgrad8<4, 4, 5><<<dim3(q.nt * q.dt, p.slices), 256, tile_t<4, 4, 5>::LDS, st>>>(q);
+        k_wgrad8<4, 2, 2, 4, 5><<<dim3(q.nt * q.dt, p.slices), 512, tile_t<4, 2, 2, 4, 5>::LDS, st>>>(q);
     } else {
         q.nt = (uint32_t)ceil_div(N, 128), q.dt = (uint32_t)ceil_div(D, 128);
-        k_wgrad8<2, 2, 4><<<dim3(q.nt * q.dt, p.slices), 256, tile_t<2, 2, 4>::LDS, st>>>(q);
+        k_wgrad8<2, 2, 2, 2, 4><<<dim3(q.nt * q.dt, p.slices), 256, tile_t<2, 2, 2, 2, 4>::LDS, st>>>(q);
     }
     rc = check_launch();
     if (rc != ADAHOP_OK || !q.part) return rc;
