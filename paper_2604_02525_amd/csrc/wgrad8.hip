@@ -15,6 +15,8 @@
 //
 // LDS layout: token t's row at t * row bytes, its pieces of 64 bytes exchanged by t's low two bits: the four rows that a transposing
 // read of half a wave touches lie in four different quarters of the banks.
+#include <type_traits>
+
 #include "ckpt8.h"
 #include "gemm_mx_common.h"
 
@@ -36,38 +38,34 @@ struct wgrad_t {
     uint32_t nt, dt;    // tiles along N and D
 };
 
-// What a workgroup reads: `bytes` from `base` on; beyond that zeros.
-__device__ __forceinline__ rsrc_t resource(const uint8_t *base, int64_t bytes)
+// What a workgroup reads: `bytes` from `base` on, below 2^31; beyond that zeros.
+__device__ __forceinline__ rsrc_t resource(const uint8_t *base, uint32_t bytes)
 {
     base = uniform_ptr(base);
-    const int64_t most = bytes > 0x80000000 ? 0x80000000 : bytes; // a stage's offsets are below 2^31
     rsrc_t r;
     r.x = (uint32_t)(uint64_t)base;
     r.y = (uint32_t)((uint64_t)base >> 32);
-    r.z = __builtin_amdgcn_readfirstlane((uint32_t)most);
+    r.z = __builtin_amdgcn_readfirstlane(bytes);
     r.w = 0x00027000u;
     return r;
 }
 
-// Lane i's 16 bytes at voff of the resource land at lds_addr + 16 i; zeros where they lie beyond its end.  (dma16 of gemm_mx_common.h
-// with bounds.)
-__device__ __forceinline__ void dma16_bounded(rsrc_t r, uint32_t voff, uint32_t lds_addr)
+// Lane i's 16 bytes (4 bytes) at voff of the resource land at lds + AT + 16 i (4 i); zeros where they lie beyond its end.  (dma16 of gemm_mx_common.h
+// with bounds.)  lds: wave-uniform.
+template <uint32_t AT> __device__ __forceinline__ void dma16_bounded(rsrc_t r, uint32_t voff, uint32_t lds)
 {
-    lds_addr = __builtin_amdgcn_readfirstlane(lds_addr);
-    asm volatile("s_mov_b32 m0, %2\n\ts_nop 0\n\tbuffer_load_dwordx4 %0, %1, 0 offen lds"
+    asm volatile("s_add_u32 m0, %2, %3\n\ts_nop 0\n\tbuffer_load_dwordx4 %0, %1, 0 offen lds"
                  :
-                 : "v"(voff), "s"(r), "s"(lds_addr)
-                 : "memory", "m0");
+                 : "v"(voff), "s"(r), "s"(lds), "n"(AT)
+                 : "memory", "m0", "scc");
 }
 
-// Lane i's word at voff lands at lds_addr + 4 i.
-__device__ __forceinline__ void dma4_bounded(rsrc_t r, uint32_t voff, uint32_t lds_addr)
+template <uint32_t AT> __device__ __forceinline__ void dma4_bounded(rsrc_t r, uint32_t voff, uint32_t lds)
 {
-    lds_addr = __builtin_amdgcn_readfirstlane(lds_addr);
-    asm volatile("s_mov_b32 m0, %2\n\ts_nop 0\n\tbuffer_load_dword %0, %1, 0 offen lds"
+    asm volatile("s_add_u32 m0, %2, %3\n\ts_nop 0\n\tbuffer_load_dword %0, %1, 0 offen lds"
                  :
-                 : "v"(voff), "s"(r), "s"(lds_addr)
-                 : "memory", "m0");
+                 : "v"(voff), "s"(r), "s"(lds), "n"(AT)
+                 : "memory", "m0", "scc");
 }
 
 __device__ __forceinline__ u32x2 transposed(uint32_t lds_addr)
@@ -126,19 +124,29 @@ __device__ __forceinline__ void put4(const adahop_tensor_t &to, const adahop_ten
 //
 // A stage of G (bf16), of X8's codes and of its scales is copied to a ring of RING slots in LDS, RING - 1 stages ahead of its use.  During a
 // stage, each wave converts the part of the next one's codes that it has copied itself (step 0: it waits for its own copies alone),
-// into one of two buffers of bf16 rows.  One barrier per stage, before its last step, in which the first operands of the next stage are
-// read; the operands of a step are always read during the step before it.  The slot that is copied to is that of the stage before, which every
-// wave has read at that stage's barrier.
+// into one of three buffers of bf16 rows.  One barrier per stage, early in its last step, behind which the first operands of the next stage are
+// read; the operands of a step are always read during the step before it.  At the barrier a wave waits for what it has converted, not
+// for the operands that it is reading: what lies in the slot and the buffer of the stage before has been read by every wave then, and
+// that slot is copied to (behind the barrier), that buffer converted to (in the next stage).
 template <int MT, int NT, int WN, int WD, int RING> struct tile_t {
     static constexpr int WAVES = WN * WD, TM = 32 * WN * MT, TN = 32 * WD * NT, RA = 2 * TM, RB = 2 * TN;      // columns; bytes of a row in LDS
     static constexpr uint32_t A = STAGE * RA, Q = STAGE * TN, S = STAGE * 16, B = STAGE * RB; // bytes of a stage: G, codes, scales, bf16 of X8
-    static constexpr uint32_t Q0 = RING * A, S0 = Q0 + RING * Q, B0 = S0 + RING * S, LDS = B0 + 2 * B;
+    static constexpr uint32_t Q0 = A, S0 = A + Q, SLOT = (S0 + S + 1023) / 1024 * 1024, B0 = RING * SLOT, LDS = B0 + 3 * B; // in a slot: G, codes, scales
     static constexpr int WAVE_ROWS = STAGE / WAVES;                                 // tokens whose codes and scales a wave copies and converts
     static constexpr int COPIES = A / 1024 / WAVES, ROWS_PER_COPY = 1024 / RA;          // of G: per wave and stage
     static constexpr int CODE_COPIES = Q / 1024 / WAVES, ROWS_PER_CODE_COPY = 1024 / TN;
     static constexpr int ISSUED = COPIES + CODE_COPIES + 1;                         // copies per wave and stage
     static constexpr int UNITS = WAVE_ROWS * TN / 8 / 64, ROWS_PER_UNIT = 512 / TN; // of 8 codes per lane
 };
+
+// f(i) for i = FROM .. TO - 1, i known at compile time.
+template <int FROM, int TO, class F> __device__ __forceinline__ void static_for(F &&f)
+{
+    if constexpr (FROM < TO) {
+        f(std::integral_constant<int, FROM>{});
+        static_for<FROM + 1, TO>(f);
+    }
+}
 
 template <int N> __device__ __forceinline__ void wait_for_copies() { asm volatile("s_waitcnt vmcnt(%0)" ::"n"(N) : "memory"); } // all but the last N
 
@@ -159,74 +167,83 @@ template <int MT, int NT, int WN, int WD, int RING> __global__ __launch_bounds__
 
     // What this wave and this lane copy of a stage.
     const uint32_t ld = (uint32_t)(q.G.ld * 2), ldc = (uint32_t)q.x.ld_codes, lds_s = (uint32_t)q.x.ld_scales;
-    const int row = w * K::COPIES * K::ROWS_PER_COPY + lane / (K::RA / 16), chunk = lane % (K::RA / 16);
-    uint32_t voff[2];
+    uint32_t voff[K::COPIES], qoff[K::CODE_COPIES];
 #pragma unroll
-    for (int i = 0; i < 2; ++i) // copies of even and odd number
-        voff[i] = (uint32_t)row * ld + (((chunk >> 2) ^ ((row + i * K::ROWS_PER_COPY) & 3)) * 64 + (chunk & 3) * 16);
-    const uint32_t qoff = (uint32_t)(w * K::WAVE_ROWS + lane / (K::TN / 16)) * ldc + lane % (K::TN / 16) * 16;
-    // Scales: at most eight bytes of a row, at any address: four whole words from the one on that holds the first (copying the bytes one by
-    // one takes the kernel a millisecond longer at 16384 x 28672 x 8192).
+    for (int i = 0; i < K::COPIES; ++i) {
+        const uint32_t row = (w * K::COPIES + i) * K::ROWS_PER_COPY + lane / (K::RA / 16), chunk = lane % (K::RA / 16);
+        voff[i] = row * ld + (((chunk >> 2) ^ (row & 3)) * 64 + (chunk & 3) * 16);
+    }
+#pragma unroll
+    for (int i = 0; i < K::CODE_COPIES; ++i) qoff[i] = ((w * K::CODE_COPIES + i) * K::ROWS_PER_CODE_COPY + lane / (K::TN / 16)) * ldc + lane % (K::TN / 16) * 16;
+    // Scales: at most eight bytes of a row, at any address: four whole words from the one on that holds the first.
     const uint8_t *sp = q.x.scales + begin * q.x.ld_scales + (d0 >> 5);
-    const uint32_t odd = (uint32_t)(uintptr_t)sp & 3; // the same in every stage
-    sp -= odd;
+    const uint32_t odd = __builtin_amdgcn_readfirstlane((uint32_t)(uintptr_t)sp & 3); // the same in every stage
     const uint32_t soff = ((odd + (w * K::WAVE_ROWS + lane / 4) * lds_s) & ~3u) + lane % 4 * 4;
-    const uint8_t *gp = reinterpret_cast<const uint8_t *>(q.G.data) + begin * q.G.ld * 2 + n0 * 2;
-    const uint8_t *xp = q.x.codes + begin * q.x.ld_codes + d0;
-    int64_t ahead = end - begin, left = ahead; // tokens from the stage that is copied next on, and from the one at hand on
-    // bytes of a row of the tile that exist, in whole words
-    const int64_t ge = ((q.N - n0) * 2 + 3) & ~3LL, xe = (q.D - d0 + 3) & ~3LL, se = odd + ((q.D - d0 + 31) >> 5);
+    // bytes of `rows` rows of a stage that exist, in whole words
+    const auto extent = [&](uint32_t rows, uint32_t pitch, int64_t last, int64_t most) {
+        return rows ? ((rows - 1) * pitch + (uint32_t)(last < most ? last : most) + 3) & ~3u : 0u;
+    };
+    const int64_t ge = (q.N - n0) * 2, xe = q.D - d0, se = odd + ((q.D - d0 + 31) >> 5);
+    const uint32_t gfull = extent(STAGE, ld, ge, K::RA), xfull = extent(STAGE, ldc, xe, K::TN), sfull = extent(STAGE, lds_s, se, 16);
+    rsrc_t rg = resource(reinterpret_cast<const uint8_t *>(q.G.data) + begin * q.G.ld * 2 + n0 * 2, gfull);
+    rsrc_t rx = resource(q.x.codes + begin * q.x.ld_codes + d0, xfull), rs = resource(sp - odd, sfull);
+    int32_t ahead = (int32_t)(end - begin), left = ahead; // tokens from the stage that is copied next on, and from the one at hand on
+    const uint32_t base = lds;
+    uint32_t to = base, raw = base, at = base; // slots: copied to next, converted, read
+    uint32_t buffer = base + K::B0;            // of the converted rows
+    const auto after = [&](uint32_t slot) { return slot == base + (RING - 1) * K::SLOT ? base : slot + K::SLOT; };
+    const auto trim = [&] { // the resources of the stage that is copied next, where it is not a whole one
+        if (ahead >= STAGE) return;
+        const uint32_t rows = ahead > 0 ? (uint32_t)ahead : 0;
+        rg.z = extent(rows, ld, ge, K::RA);
+        rx.z = extent(rows, ldc, xe, K::TN);
+        rs.z = extent(rows, lds_s, se, 16);
+    };
+    const auto forward = [](rsrc_t &r, uint32_t bytes) {
+        const uint64_t p = ((uint64_t)r.y << 32 | r.x) + bytes;
+        r.x = (uint32_t)p;
+        r.y = (uint32_t)(p >> 32);
+    };
+    const uint32_t gstep = STAGE * ld, xstep = STAGE * ldc, sstep = STAGE * lds_s;
+    const auto copied = [&] {
+        forward(rg, gstep);
+        forward(rx, xstep);
+        forward(rs, sstep);
+        ahead -= STAGE;
+        to = after(to);
+    };
+    const uint32_t own_g = w * K::COPIES * 1024, own_q = w * K::CODE_COPIES * 1024, own_s = w * K::WAVE_ROWS * 16;
+    const auto copy = [&](auto number) {
+        constexpr int i = decltype(number)::value;
+        if constexpr (i < K::COPIES)
+            dma16_bounded<i * 1024>(rg, voff[i], to + own_g);
+        else if constexpr (i < K::COPIES + K::CODE_COPIES)
+            dma16_bounded<K::Q0 + (i - K::COPIES) * 1024>(rx, qoff[i - K::COPIES], to + own_q);
+        else if (lane < 4 * K::WAVE_ROWS)
+            dma4_bounded<K::S0>(rs, soff, to + own_s);
+    };
 
     // What it converts and reads.
-    const int urow = w * K::WAVE_ROWS + lane / (K::TN / 8), unit = lane % (K::TN / 8);
-    const uint32_t raw = lds + K::Q0 + w * K::WAVE_ROWS * K::TN + lane * 8;
-    uint32_t scale_at[K::UNITS];
+    const uint32_t urow = w * K::WAVE_ROWS + lane / (K::TN / 8), unit = lane % (K::TN / 8);
+    const uint32_t raw_at = K::Q0 + w * K::WAVE_ROWS * K::TN + lane * 8;
+    uint32_t scale_at[K::UNITS], put[K::UNITS];
 #pragma unroll
     for (int j = 0; j < K::UNITS; ++j) {
         const uint32_t r = urow + j * K::ROWS_PER_UNIT;
-        scale_at[j] = lds + K::S0 + r * 16 + ((odd + r * lds_s) & 3) + unit / 4;
+        scale_at[j] = K::S0 + r * 16 + ((odd + r * lds_s) & 3) + unit / 4;
+        put[j] = r * K::RB + (((unit >> 2) ^ (r & 3)) * 64 + (unit & 3) * 16);
     }
-    uint32_t put[2]; // units of even and odd number
-#pragma unroll
-    for (int i = 0; i < 2; ++i) put[i] = lds + K::B0 + urow * K::RB + (((unit >> 2) ^ ((urow + i * K::ROWS_PER_UNIT) & 3)) * 64 + (unit & 3) * 16);
     const int s16 = lane & 15, h = lane >> 5;
     uint32_t ra[MT], rb[NT], va[MT], vb[NT];
 #pragma unroll
-    for (int m = 0; m < MT; ++m) va[m] = ra[m] = lds + (8 * h + (s16 >> 2)) * K::RA + (((wn * MT + m) ^ (s16 >> 2)) * 64) + 32 * ((lane >> 4) & 1) + 8 * (s16 & 3);
+    for (int m = 0; m < MT; ++m) ra[m] = (8 * h + (s16 >> 2)) * K::RA + (((wn * MT + m) ^ (s16 >> 2)) * 64) + 32 * ((lane >> 4) & 1) + 8 * (s16 & 3);
 #pragma unroll
-    for (int n = 0; n < NT; ++n)
-        vb[n] = rb[n] = lds + K::B0 + (8 * h + (s16 >> 2)) * K::RB + (((wd * NT + n) ^ (s16 >> 2)) * 64) + 32 * ((lane >> 4) & 1) + 8 * (s16 & 3);
-
-    uint32_t slot_to = 0, slot_raw = 0, slot_at = 0, buffer = 0; // ring slots: copied to next, converted next, read next; bf16 buffer of slot_raw
-    const auto after = [](uint32_t slot) { return slot + 1 == RING ? 0 : slot + 1; };
-    rsrc_t rg, rx, rs;
-    const auto aim = [&] { // at the stage that is copied next
-        rg = resource(gp, ahead > 0 ? (ahead - 1) * (int64_t)ld + ge : 0);
-        rx = resource(xp, ahead > 0 ? (ahead - 1) * (int64_t)ldc + xe : 0);
-        rs = resource(sp, ahead > 0 ? ((ahead - 1) * (int64_t)lds_s + se + 3) & ~3LL : 0);
-    };
-    const auto copy = [&](int i) {
-        if (i < K::COPIES) {
-            dma16_bounded(rg, voff[i & 1] + i * K::ROWS_PER_COPY * ld, lds + slot_to * K::A + (w * K::COPIES + i) * 1024);
-        } else if (i < K::COPIES + K::CODE_COPIES) {
-            const int j = i - K::COPIES;
-            dma16_bounded(rx, qoff + j * K::ROWS_PER_CODE_COPY * ldc, lds + K::Q0 + slot_to * K::Q + (w * K::CODE_COPIES + j) * 1024);
-        } else {
-            if (lane < 4 * K::WAVE_ROWS) dma4_bounded(rs, soff, lds + K::S0 + slot_to * K::S + w * K::WAVE_ROWS * 16);
-        }
-    };
-    const auto copied = [&] {
-        gp += (int64_t)STAGE * ld;
-        xp += (int64_t)STAGE * ldc;
-        sp += (int64_t)STAGE * lds_s;
-        ahead -= STAGE;
-        slot_to = after(slot_to);
-    };
+    for (int n = 0; n < NT; ++n) rb[n] = (8 * h + (s16 >> 2)) * K::RB + (((wd * NT + n) ^ (s16 >> 2)) * 64) + 32 * ((lane >> 4) & 1) + 8 * (s16 & 3);
     u32x2 codes[K::UNITS];
     uint32_t scales[K::UNITS];
     const auto fetch = [&](int j) {
-        codes[j] = *(__attribute__((address_space(3))) u32x2 *)(raw + slot_raw * K::Q + j * 512);
-        scales[j] = *(__attribute__((address_space(3))) uint8_t *)(scale_at[j] + slot_raw * K::S);
+        codes[j] = *(__attribute__((address_space(3))) u32x2 *)(raw + raw_at + j * 512);
+        scales[j] = *(__attribute__((address_space(3))) uint8_t *)(raw + scale_at[j]);
     };
     const auto convert = [&](int j) {
         const float scale = __uint_as_float(scales[j] << 23);
@@ -236,7 +253,7 @@ template <int MT, int NT, int WN, int WD, int RING> __global__ __launch_bounds__
             v[2 * i] = __builtin_bit_cast(uint32_t, __builtin_amdgcn_cvt_scalef32_pk_bf16_fp8(codes[j][i], scale, false));
             v[2 * i + 1] = __builtin_bit_cast(uint32_t, __builtin_amdgcn_cvt_scalef32_pk_bf16_fp8(codes[j][i], scale, true));
         }
-        *(__attribute__((address_space(3))) u32x4 *)(put[j & 1] + buffer * K::B + j * K::ROWS_PER_UNIT * K::RB) = v;
+        *(__attribute__((address_space(3))) u32x4 *)(buffer + put[j]) = v;
     };
 
     v16f acc[MT][NT];
@@ -245,31 +262,29 @@ template <int MT, int NT, int WN, int WD, int RING> __global__ __launch_bounds__
 #pragma unroll
         for (int n = 0; n < NT; ++n) acc[m][n] = {};
     u32x2 fa[2][MT][2], fb[2][NT][2];
-    // Read number i of a step's operands, in the order in which they are used: G's first tile, all of X's, G's others.
-    const auto read = [&](int set, int step, int i) {
+    // Read number i of a step's operands, in the order in which they are used: G's first tile, all of X's, G's others.  The first step's
+    // go to the stage whose slot and buffer are at hand.
+    const auto read = [&](int step, int i) {
         const int tile = i >> 1, part = i & 1;
-        if (tile == 0)
-            fa[set][0][part] = transposed(va[0] + (16 * step + 4 * part) * K::RA);
-        else if (tile <= NT)
-            fb[set][tile - 1][part] = transposed(vb[tile - 1] + (16 * step + 4 * part) * K::RB);
-        else
-            fa[set][tile - NT][part] = transposed(va[tile - NT] + (16 * step + 4 * part) * K::RA);
+        if (tile >= 1 && tile <= NT) {
+            if (step == 0 && part == 0) vb[tile - 1] = buffer + rb[tile - 1];
+            fb[step][tile - 1][part] = transposed(vb[tile - 1] + (16 * step + 4 * part) * K::RB);
+        } else {
+            const int m = tile ? tile - NT : 0;
+            if (step == 0 && part == 0) va[m] = at + ra[m];
+            fa[step][m][part] = transposed(va[m] + (16 * step + 4 * part) * K::RA);
+        }
     };
-    const auto turn = [&] { // reads go to the next stage
-#pragma unroll
-        for (int m = 0; m < MT; ++m) va[m] = ra[m] + slot_at * K::A;
-#pragma unroll
-        for (int n = 0; n < NT; ++n) vb[n] = rb[n] + buffer * K::B;
-    };
-    constexpr int READS = 2 * (MT + NT), SLOTS = MT * NT;
+    // A step's matrix instructions are slots, with what is issued beside each.  Step 0: all reads, conversions from slot FIRST on; step 1: the barrier
+    // behind slot BARRIER, reads and copies after it.
+    constexpr int READS = 2 * (MT + NT), SLOTS = MT * NT, FIRST = SLOTS / 2 < K::UNITS ? SLOTS - K::UNITS : SLOTS / 2, BARRIER = SLOTS > 4 ? 1 : 0;
     static_assert(STEPS == 2 && K::UNITS <= SLOTS, "a stage's work fits its two steps");
 
     if (left > 0) {
 #pragma unroll 1
         for (int i = 0; i < RING - 1; ++i) {
-            aim();
-#pragma unroll
-            for (int c = 0; c < K::ISSUED; ++c) copy(c);
+            trim();
+            static_for<0, K::ISSUED>(copy);
             copied();
         }
         wait_for_copies<(RING - 2) * K::ISSUED>();
@@ -279,44 +294,38 @@ template <int MT, int NT, int WN, int WD, int RING> __global__ __launch_bounds__
         for (int j = 0; j < K::UNITS; ++j) convert(j);
         asm volatile("s_waitcnt lgkmcnt(0)\n\ts_barrier" ::: "memory");
 #pragma unroll
-        for (int i = 0; i < READS; ++i) read(0, 0, i);
+        for (int i = 0; i < READS; ++i) read(0, i);
     }
     while (left > 0) {
-        slot_raw = after(slot_raw);
-        buffer ^= 1;
-        aim();
+        static_for<0, 2 * SLOTS>([&](auto number) {
+            constexpr int step = decltype(number)::value / SLOTS, slot = decltype(number)::value % SLOTS, m = slot / NT, n = slot % NT;
+            const auto whole = [](const u32x2 (&f)[2]) { return make_uint4(f[0].x, f[0].y, f[1].x, f[1].y); };
+            acc[m][n] = mfma_bf16(whole(fa[step][m]), whole(fb[step][n]), acc[m][n]);
+            if constexpr (step == 0) {
+                if constexpr (slot == 0) {
+                    wait_for_copies<(RING - 3) * K::ISSUED>(); // of the next stage, this wave's
+                    raw = after(raw);
+                    buffer = buffer == base + K::B0 + 2 * K::B ? base + K::B0 : buffer + K::B;
+                }
 #pragma unroll
-        for (int step = 0; step < STEPS; ++step) {
-            if (step == 0) {
-                wait_for_copies<(RING - 3) * K::ISSUED>(); // of the next stage, this wave's
-            } else {
-                asm volatile("s_waitcnt lgkmcnt(0)\n\ts_barrier" ::: "memory"); // everyone's, and its converted rows
-                slot_at = after(slot_at);
-                turn();
+                for (int i = slot * READS / SLOTS; i < (slot + 1) * READS / SLOTS; ++i) read(1, i);
+                if constexpr (slot < K::UNITS) fetch(slot);
+                if constexpr (slot >= FIRST && slot < FIRST + K::UNITS) convert(slot - FIRST);
+            } else if constexpr (slot == BARRIER) {
+                asm volatile("s_waitcnt lgkmcnt(%0)\n\ts_barrier" ::"n"(READS - (FIRST + K::UNITS) * READS / SLOTS) : "memory");
+                at = raw;
+                trim();
+            } else if constexpr (slot > BARRIER) {
+                constexpr int LEFT = SLOTS - 1 - BARRIER, place = slot - 1 - BARRIER;
+#pragma unroll
+                for (int i = place * READS / LEFT; i < (place + 1) * READS / LEFT; ++i) read(0, i);
+                static_for<place * K::ISSUED / LEFT, (place + 1) * K::ISSUED / LEFT>(copy);
             }
             ADAHOP_PIN();
-#pragma unroll
-            for (int slot = 0; slot < SLOTS; ++slot) {
-                const int m = slot / NT, n = slot % NT;
-                const auto whole = [](const u32x2 (&f)[2]) { return make_uint4(f[0].x, f[0].y, f[1].x, f[1].y); };
-                acc[m][n] = mfma_bf16(whole(fa[step][m]), whole(fb[step][n]), acc[m][n]);
-#pragma unroll
-                for (int i = slot * READS / SLOTS; i < (slot + 1) * READS / SLOTS; ++i) read(step ^ 1, step ^ 1, i);
-                if (step == 0) {
-                    if (slot < K::UNITS) fetch(slot);
-                    constexpr int FIRST = SLOTS / 2 < K::UNITS ? SLOTS - K::UNITS : SLOTS / 2;
-                    if (slot >= FIRST && slot < FIRST + K::UNITS) convert(slot - FIRST);
-                }
-                const int all = step * SLOTS + slot;
-#pragma unroll
-                for (int i = all * K::ISSUED / (2 * SLOTS); i < (all + 1) * K::ISSUED / (2 * SLOTS); ++i) copy(i);
-                ADAHOP_PIN();
-            }
-        }
+        });
         copied();
         left -= STAGE;
     }
-    wait_for_copies<0>(); // those past the end
 
     // C, 32 rows of a wave at a time by way of its own patch of LDS, so that a lane has four consecutive columns of a row: 16-byte stores of
     // whole rows, and little code.  In the accumulators a lane has column lane % 32 of a tile, rows 8 (i / 4) + 4 h + i % 4.
@@ -333,8 +342,8 @@ template <int MT, int NT, int WN, int WD, int RING> __global__ __launch_bounds__
         for (int i = 0; i < 4; ++i)
             if (i < have) scale[i] = element(q.col_scale, c + i);
     }
-    adahop_tensor_t to = q.C;
-    if (q.part) to = {q.part + (int64_t)blockIdx.y * q.N * q.D, q.D, 1};
+    adahop_tensor_t result = q.C;
+    if (q.part) result = {q.part + (int64_t)blockIdx.y * q.N * q.D, q.D, 1};
 #pragma unroll
     for (int m = 0; m < MT; ++m) {
         lds_between_lanes();
@@ -348,7 +357,7 @@ template <int MT, int NT, int WN, int WD, int RING> __global__ __launch_bounds__
 #pragma unroll 4
         for (int i = 0; i < 32; i += 64 / LANES) {
             const int64_t r = first + i;
-            if (r < q.N) put4(to, q.add, r, c, have, scale, *reinterpret_cast<const float4 *>(patch + (r0 + i) * PITCH + c4));
+            if (r < q.N) put4(result, q.add, r, c, have, scale, *reinterpret_cast<const float4 *>(patch + (r0 + i) * PITCH + c4));
         }
     }
 }
@@ -411,7 +420,7 @@ int configure_wgrad8()
     int dev = 0;
     int rc = check_hip(hipGetDevice(&dev));
     if (rc != ADAHOP_OK || !g_once.need(dev)) return rc;
-    rc = check_hip(hipFuncSetAttribute(reinterpret_cast<const void *>(&k_wgrad8<4, 2, 2, 4, 5>), hipFuncAttributeMaxDynamicSharedMemorySize, tile_t<4, 2, 2, 4, 5>::LDS));
+    rc = check_hip(hipFuncSetAttribute(reinterpret_cast<const void *>(&k_wgrad8<4, 2, 2, 4, 4>), hipFuncAttributeMaxDynamicSharedMemorySize, tile_t<4, 2, 2, 4, 4>::LDS));
     if (rc == ADAHOP_OK)
         rc = check_hip(hipFuncSetAttribute(reinterpret_cast<const void *>(&k_wgrad8<2, 2, 2, 2, 4>), hipFuncAttributeMaxDynamicSharedMemorySize, tile_t<2, 2, 2, 2, 4>::LDS));
     if (rc == ADAHOP_OK) g_once.mark(dev);
@@ -434,7 +443,7 @@ int launch_wgrad8(int64_t T, int64_t N, int64_t D, const adahop_tensor_t &G, con
     if (q.part) q.col_scale = q.add = {}; // the slices' sums come first
     if (p.large) {
         q.nt = (uint32_t)ceil_div(N, 256), q.dt = (uint32_t)ceil_div(D, 256);
-        k_wgrad8<4, 2, 2, 4, 5><<<dim3(q.nt * q.dt, p.slices), 512, tile_t<4, 2, 2, 4, 5>::LDS, st>>>(q);
+        k_wgrad8<4, 2, 2, 4, 4><<<dim3(q.nt * q.dt, p.slices), 512, tile_t<4, 2, 2, 4, 4>::LDS, st>>>(q);
     } else {
         q.nt = (uint32_t)ceil_div(N, 128), q.dt = (uint32_t)ceil_div(D, 128);
         k_wgrad8<2, 2, 2, 2, 4><<<dim3(q.nt * q.dt, p.slices), 256, tile_t<2, 2, 2, 2, 4>::LDS, st>>>(q);
