@@ -60,11 +60,13 @@ template <uint32_t AT> __device__ __forceinline__ void dma16_bounded(rsrc_t r, u
                  : "memory", "m0", "scc");
 }
 
-template <uint32_t AT> __device__ __forceinline__ void dma4_bounded(rsrc_t r, uint32_t voff, uint32_t lds)
+// The first LANES <= 32 lanes only, of a wave whose lanes are all active; without a branch, which would end the block that the instructions around
+// are scheduled in.
+template <uint32_t AT, int LANES> __device__ __forceinline__ void dma4_bounded(rsrc_t r, uint32_t voff, uint32_t lds)
 {
-    asm volatile("s_add_u32 m0, %2, %3\n\ts_nop 0\n\tbuffer_load_dword %0, %1, 0 offen lds"
+    asm volatile("s_add_u32 m0, %2, %3\n\ts_mov_b32 exec_lo, %4\n\ts_mov_b32 exec_hi, 0\n\tbuffer_load_dword %0, %1, 0 offen lds\n\ts_mov_b64 exec, -1"
                  :
-                 : "v"(voff), "s"(r), "s"(lds), "n"(AT)
+                 : "v"(voff), "s"(r), "s"(lds), "n"(AT), "n"((uint32_t)(((uint64_t)1 << LANES) - 1))
                  : "memory", "m0", "scc");
 }
 
@@ -122,16 +124,15 @@ __device__ __forceinline__ void put4(const adahop_tensor_t &to, const adahop_ten
 // Tiles of C by WN x WD waves of 32 MT x 32 NT.  Two waves per SIMD, in one workgroup or in two: a wave issues an instruction every four
 // cycles at most, and what it has to issue beside its matrix instructions does not fit between them.
 //
-// A stage of G (bf16), of X8's codes and of its scales is copied to a ring of RING slots in LDS, RING - 1 stages ahead of its use.  During a
-// stage, each wave converts the part of the next one's codes that it has copied itself (step 0: it waits for its own copies alone),
-// into one of three buffers of bf16 rows.  One barrier per stage, early in its last step, behind which the first operands of the next stage are
-// read; the operands of a step are always read during the step before it.  At the barrier a wave waits for what it has converted, not
-// for the operands that it is reading: what lies in the slot and the buffer of the stage before has been read by every wave then, and
-// that slot is copied to (behind the barrier), that buffer converted to (in the next stage).
+// A stage of G (bf16), of X8's codes and of its scales is copied to a ring of RING slots in LDS, RING - 1 stages ahead of its use.  Each
+// wave converts the codes that it has copied itself, so that it waits for its own copies alone: it reads those of the stage after the next in the
+// second half of a stage, and writes the bf16 rows, into one of two buffers, in the first half of the stage after.  One barrier per stage, in the middle of its
+// last step; behind it the first operands of the next stage are read.  The operands of a step are always read during the step before it.  At the
+// barrier no wave has reads of the stage at hand outstanding: its buffer is converted to, and its slot copied to, in the next stage.
 template <int MT, int NT, int WN, int WD, int RING> struct tile_t {
     static constexpr int WAVES = WN * WD, TM = 32 * WN * MT, TN = 32 * WD * NT, RA = 2 * TM, RB = 2 * TN;      // columns; bytes of a row in LDS
     static constexpr uint32_t A = STAGE * RA, Q = STAGE * TN, S = STAGE * 16, B = STAGE * RB; // bytes of a stage: G, codes, scales, bf16 of X8
-    static constexpr uint32_t Q0 = A, S0 = A + Q, SLOT = (S0 + S + 1023) / 1024 * 1024, B0 = RING * SLOT, LDS = B0 + 3 * B; // in a slot: G, codes, scales
+    static constexpr uint32_t Q0 = A, S0 = A + Q, SLOT = (S0 + S + 511) / 512 * 512, B0 = RING * SLOT, LDS = B0 + 2 * B; // in a slot: G, codes, scales
     static constexpr int WAVE_ROWS = STAGE / WAVES;                                 // tokens whose codes and scales a wave copies and converts
     static constexpr int COPIES = A / 1024 / WAVES, ROWS_PER_COPY = 1024 / RA;          // of G: per wave and stage
     static constexpr int CODE_COPIES = Q / 1024 / WAVES, ROWS_PER_CODE_COPY = 1024 / TN;
@@ -189,7 +190,7 @@ template <int MT, int NT, int WN, int WD, int RING> __global__ __launch_bounds__
     rsrc_t rx = resource(q.x.codes + begin * q.x.ld_codes + d0, xfull), rs = resource(sp - odd, sfull);
     int32_t ahead = (int32_t)(end - begin), left = ahead; // tokens from the stage that is copied next on, and from the one at hand on
     const uint32_t base = lds;
-    uint32_t to = base, raw = base, at = base; // slots: copied to next, converted, read
+    uint32_t to = base, raw = base, at = base; // slots: copied to next, whose codes are read next, whose operands are
     uint32_t buffer = base + K::B0;            // of the converted rows
     const auto after = [&](uint32_t slot) { return slot == base + (RING - 1) * K::SLOT ? base : slot + K::SLOT; };
     const auto trim = [&] { // the resources of the stage that is copied next, where it is not a whole one
@@ -219,8 +220,8 @@ template <int MT, int NT, int WN, int WD, int RING> __global__ __launch_bounds__
             dma16_bounded<i * 1024>(rg, voff[i], to + own_g);
         else if constexpr (i < K::COPIES + K::CODE_COPIES)
             dma16_bounded<K::Q0 + (i - K::COPIES) * 1024>(rx, qoff[i - K::COPIES], to + own_q);
-        else if (lane < 4 * K::WAVE_ROWS)
-            dma4_bounded<K::S0>(rs, soff, to + own_s);
+        else
+            dma4_bounded<K::S0, 4 * K::WAVE_ROWS>(rs, soff, to + own_s);
     };
 
     // What it converts and reads.
@@ -275,10 +276,17 @@ template <int MT, int NT, int WN, int WD, int RING> __global__ __launch_bounds__
             fa[step][m][part] = transposed(va[m] + (16 * step + 4 * part) * K::RA);
         }
     };
-    // A step's matrix instructions are slots, with what is issued beside each.  Step 0: all reads, conversions from slot FIRST on; step 1: the barrier
-    // behind slot BARRIER, reads and copies after it.
-    constexpr int READS = 2 * (MT + NT), SLOTS = MT * NT, FIRST = SLOTS / 2 < K::UNITS ? SLOTS - K::UNITS : SLOTS / 2, BARRIER = SLOTS > 4 ? 1 : 0;
-    static_assert(STEPS == 2 && K::UNITS <= SLOTS, "a stage's work fits its two steps");
+    // A step's matrix instructions are places, with what is issued beside each.  Step 0: conversions, and all reads of step 1; step 1: the barrier
+    // beside place BARRIER, behind it reads and codes.  The copies are spread over both steps.
+    constexpr int READS = 2 * (MT + NT), PLACES = MT * NT, BARRIER = PLACES / 2 - 1, FETCH = BARRIER + 1, EARLY = PLACES - PLACES / 4;
+    constexpr auto copy_at = [](int i) { return (2 * i + 1) * PLACES / K::ISSUED; }; // of 2 PLACES
+    constexpr auto copies_before = [](int place) {
+        int n = 0;
+        while (n < K::ISSUED && (2 * n + 1) * PLACES / K::ISSUED < place) ++n;
+        return n;
+    };
+    static_assert(STEPS == 2 && K::UNITS <= PLACES - FETCH && K::UNITS <= PLACES, "a stage's work fits its two steps");
+    const auto other = [&](uint32_t b) { return b == base + K::B0 ? base + K::B0 + K::B : base + K::B0; };
 
     if (left > 0) {
 #pragma unroll 1
@@ -287,43 +295,50 @@ template <int MT, int NT, int WN, int WD, int RING> __global__ __launch_bounds__
             static_for<0, K::ISSUED>(copy);
             copied();
         }
+        trim();
         wait_for_copies<(RING - 2) * K::ISSUED>();
 #pragma unroll
         for (int j = 0; j < K::UNITS; ++j) fetch(j);
 #pragma unroll
         for (int j = 0; j < K::UNITS; ++j) convert(j);
         asm volatile("s_waitcnt lgkmcnt(0)\n\ts_barrier" ::: "memory");
+        raw = after(raw);
+        wait_for_copies<(RING - 3) * K::ISSUED>();
+#pragma unroll
+        for (int j = 0; j < K::UNITS; ++j) fetch(j); // first, as in the loop: the compiler's waits go by how many reads may be behind these
+        ADAHOP_PIN();
 #pragma unroll
         for (int i = 0; i < READS; ++i) read(0, i);
     }
     while (left > 0) {
-        static_for<0, 2 * SLOTS>([&](auto number) {
-            constexpr int step = decltype(number)::value / SLOTS, slot = decltype(number)::value % SLOTS, m = slot / NT, n = slot % NT;
+        static_for<0, 2 * PLACES>([&](auto number) {
+            constexpr int all = decltype(number)::value, step = all / PLACES, place = all % PLACES, m = place / NT, n = place % NT;
             const auto whole = [](const u32x2 (&f)[2]) { return make_uint4(f[0].x, f[0].y, f[1].x, f[1].y); };
             acc[m][n] = mfma_bf16(whole(fa[step][m]), whole(fb[step][n]), acc[m][n]);
             if constexpr (step == 0) {
-                if constexpr (slot == 0) {
-                    wait_for_copies<(RING - 3) * K::ISSUED>(); // of the next stage, this wave's
-                    raw = after(raw);
-                    buffer = buffer == base + K::B0 + 2 * K::B ? base + K::B0 : buffer + K::B;
-                }
+                if constexpr (place == 0) buffer = other(buffer);
+                if constexpr (place < K::UNITS) convert(place);
 #pragma unroll
-                for (int i = slot * READS / SLOTS; i < (slot + 1) * READS / SLOTS; ++i) read(1, i);
-                if constexpr (slot < K::UNITS) fetch(slot);
-                if constexpr (slot >= FIRST && slot < FIRST + K::UNITS) convert(slot - FIRST);
-            } else if constexpr (slot == BARRIER) {
-                asm volatile("s_waitcnt lgkmcnt(%0)\n\ts_barrier" ::"n"(READS - (FIRST + K::UNITS) * READS / SLOTS) : "memory");
+                for (int i = place * READS / EARLY; i < (place + 1) * READS / EARLY && i < READS; ++i) read(1, i);
+            } else if constexpr (place == BARRIER) {
                 at = raw;
-                trim();
-            } else if constexpr (slot > BARRIER) {
-                constexpr int LEFT = SLOTS - 1 - BARRIER, place = slot - 1 - BARRIER;
+                raw = after(raw);
+                asm volatile("s_waitcnt lgkmcnt(0)\n\ts_barrier" ::: "memory");
+            } else if constexpr (place > BARRIER) {
+                constexpr int LEFT = PLACES - 1 - BARRIER, behind = place - 1 - BARRIER;
 #pragma unroll
-                for (int i = place * READS / LEFT; i < (place + 1) * READS / LEFT; ++i) read(0, i);
-                static_for<place * K::ISSUED / LEFT, (place + 1) * K::ISSUED / LEFT>(copy);
+                for (int i = behind * READS / LEFT; i < (behind + 1) * READS / LEFT; ++i) read(0, i);
+                // the codes of the stage after the next: all copies but those of the stage behind it and what this stage has issued so far are done
+                if constexpr (place == FETCH) wait_for_copies<(RING - 4) * K::ISSUED + copies_before(all)>();
+                if constexpr (place >= FETCH && place < FETCH + K::UNITS) fetch(place - FETCH);
             }
+            static_for<0, K::ISSUED>([&](auto i) {
+                if constexpr (copy_at(decltype(i)::value) == all) copy(i);
+            });
             ADAHOP_PIN();
         });
         copied();
+        trim();
         left -= STAGE;
     }
 
@@ -420,9 +435,9 @@ int configure_wgrad8()
     int dev = 0;
     int rc = check_hip(hipGetDevice(&dev));
     if (rc != ADAHOP_OK || !g_once.need(dev)) return rc;
-    rc = check_hip(hipFuncSetAttribute(reinterpret_cast<const void *>(&k_wgrad8<4, 2, 2, 4, 4>), hipFuncAttributeMaxDynamicSharedMemorySize, tile_t<4, 2, 2, 4, 4>::LDS));
+    rc = check_hip(hipFuncSetAttribute(reinterpret_cast<const void *>(&k_wgrad8<4, 2, 2, 4, 5>), hipFuncAttributeMaxDynamicSharedMemorySize, tile_t<4, 2, 2, 4, 5>::LDS));
     if (rc == ADAHOP_OK)
-        rc = check_hip(hipFuncSetAttribute(reinterpret_cast<const void *>(&k_wgrad8<2, 2, 2, 2, 4>), hipFuncAttributeMaxDynamicSharedMemorySize, tile_t<2, 2, 2, 2, 4>::LDS));
+        rc = check_hip(hipFuncSetAttribute(reinterpret_cast<const void *>(&k_wgrad8<2, 2, 2, 2, 5>), hipFuncAttributeMaxDynamicSharedMemorySize, tile_t<2, 2, 2, 2, 5>::LDS));
     if (rc == ADAHOP_OK) g_once.mark(dev);
     return rc;
 }
@@ -443,10 +458,10 @@ int launch_wgrad8(int64_t T, int64_t N, int64_t D, const adahop_tensor_t &G, con
     if (q.part) q.col_scale = q.add = {}; // the slices' sums come first
     if (p.large) {
         q.nt = (uint32_t)ceil_div(N, 256), q.dt = (uint32_t)ceil_div(D, 256);
-        k_wgrad8<4, 2, 2, 4, 4><<<dim3(q.nt * q.dt, p.slices), 512, tile_t<4, 2, 2, 4, 4>::LDS, st>>>(q);
+        k_wgrad8<4, 2, 2, 4, 5><<<dim3(q.nt * q.dt, p.slices), 512, tile_t<4, 2, 2, 4, 5>::LDS, st>>>(q);
     } else {
         q.nt = (uint32_t)ceil_div(N, 128), q.dt = (uint32_t)ceil_div(D, 128);
-        k_wgrad8<2, 2, 2, 2, 4><<<dim3(q.nt * q.dt, p.slices), 256, tile_t<2, 2, 2, 2, 4>::LDS, st>>>(q);
+        k_wgrad8<2, 2, 2, 2, 5><<<dim3(q.nt * q.dt, p.slices), 256, tile_t<2, 2, 2, 2, 5>::LDS, st>>>(q);
     }
     rc = check_launch();
     if (rc != ADAHOP_OK || !q.part) return rc;
