@@ -328,7 +328,7 @@ template <int MT, int NT, int WN, int WD, int RING> __global__ __launch_bounds__
 // The sums of the slices, in their order, and what the kernel above does with a single one's.  A lane has four columns.
 __global__ __launch_bounds__(256) void k_wgrad8_join(wgrad_t q, int slices)
 {
-    const int64_t c = ((int64_t)blockIdx.x * 64 + (threadIdx.x & 63)) * 4, r = (int64_t)blockIdx.y * 4 + (threadIdx.x >> 6);
+    const int64_t c = ((int64_t)blockIdx.y * 64 + (threadIdx.x & 63)) * 4, r = (int64_t)blockIdx.x * 4 + (threadIdx.x >> 6);
     if (c >= q.D || r >= q.N) return;
     const int have = (int)(q.D - c < 4 ? q.D - c : 4);
     float v[4] = {}, scale[4] = {1.0f, 1.0f, 1.0f, 1.0f};
@@ -361,17 +361,32 @@ struct plan_t {
     size_t part_at, bytes;
 };
 
+// Tile size and slices of the tokens by expected time, in microseconds, measured on 256 compute units.  A stage of a round of workgroups: 0.7 with the large
+// tiles, one workgroup per compute unit; with the small ones 0.5 where there are two per compute unit, 0.33 where there is one; a round's beginning and end
+// 4 and 2.5.  Slices cost their sums' way to memory and back and one launch more.  Both sides at 2048 x 2048, us: 1001 tokens, small tiles in one slice 23.6, in two 30.0,
+// large ones in four 36.9; 8192 tokens, 92.0, 82.0 and 81.2; 4096 x 2048 at 4096 tokens, small 74.2, large in two slices 80.6; at 16384 tokens 245 and 225.
 plan_t plan_of(int64_t T, int64_t N, int64_t D)
 {
-    const int64_t large = ceil_div(N, 256) * ceil_div(D, 256), small = ceil_div(N, 128) * ceil_div(D, 128), stages = ceil_div(T, STAGE);
+    const int64_t stages = ceil_div(T, STAGE), large = ceil_div(N, 256) * ceil_div(D, 256), small = ceil_div(N, 128) * ceil_div(D, 128);
     plan_t p;
-    p.large = large >= 256;
-    const int64_t tiles = p.large ? large : small, fit = 512 / tiles;
-    int64_t slices = p.large || fit < 2 ? 1 : fit;
-    if (slices > stages / 16) slices = stages / 16;
-    if (slices < 1) slices = 1;
-    p.slice = ceil_div(ceil_div(stages, slices), 2) * 2 * STAGE;
-    p.slices = T > 0 ? (int)ceil_div(T, p.slice) : 1;
+    double best = 0.0;
+    p.slices = 0;
+    for (int64_t slices = 1; slices <= 64 && (slices == 1 || stages / slices >= 8); ++slices) {
+        const int64_t each = ceil_div(ceil_div(stages, slices), 2) * 2; // stages per slice; the kernel takes them in pairs
+        const int64_t number = T > 0 ? ceil_div(stages, each) : 1;
+        const double join = number > 1 ? 6.0 + (double)number * N * D * 8 / 5e6 : 0.0;
+        const int64_t rounds = small * number / 512, over = small * number % 512;
+        const double in_large = ceil_div(large * number, 256) * (4.0 + 0.7 * each) + join;
+        const double in_small = (rounds + (over > 0)) * 2.5 + (rounds * 0.5 + (over > 256 ? 0.5 : over > 0 ? 0.33 : 0.0)) * each + join;
+        const double t = in_large < in_small ? in_large : in_small;
+        if (p.slices == 0 || t < best) {
+            best = t;
+            p.large = in_large < in_small;
+            p.slices = (int)number;
+            p.slice = each * STAGE;
+        }
+        if (join > best) break;
+    }
     p.ldx = ceil_div(D, 8) * 8;
     p.part_at = align_up((size_t)T * p.ldx * 2, 256);
     p.bytes = p.part_at + (p.slices > 1 ? (size_t)p.slices * N * D * sizeof(float) : 0);
@@ -420,8 +435,7 @@ int launch_wgrad8(int64_t T, int64_t N, int64_t D, const adahop_tensor_t &G, con
     rc = check_launch();
     if (rc != ADAHOP_OK || !part) return rc;
     q.col_scale = col_scale, q.add = add;
-    // slices are for few tiles, so N / 4 is far below the limit of a grid's second dimension
-    k_wgrad8_join<<<dim3((unsigned)ceil_div(D, 256), (unsigned)ceil_div(N, 4)), 256, 0, st>>>(q, p.slices);
+    k_wgrad8_join<<<dim3((unsigned)ceil_div(N, 4), (unsigned)ceil_div(D, 256)), 256, 0, st>>>(q, p.slices);
     return check_launch();
 }
 
