@@ -13,40 +13,53 @@ namespace adahop {
 
 namespace {
 
-// C: pieces of 8 columns per lane; SF32, YF32: the type of x and s, and of y.
+// C: pieces of 8 columns per lane; SF32, YF32: the type of x and s, and of y.  The next row's x and y are on their way while a row is summed.
 template <int C, bool SF32, bool YF32> __global__ __launch_bounds__(ROW_THREADS) void k_block_norm(adahop_block_norm_t q)
 {
     __shared__ row_sums_t<1> lds;
     const int threads = blockDim.x, waves = threads >> 6;
-    int turn = 0, n[C];
-    float wpost[C][8], wpre[C][8], gate[C][8];
+    int turn = 0;
+    const auto col = [&](int j) { return (int)(threadIdx.x + j * threads) * 8; };
+    const auto left = [&](int j) { return (int)q.cols - col(j); };
+    float wbranch[C][8], wpre[C][8]; // branch_scale w_post gate; w_pre
 #pragma unroll
     for (int j = 0; j < C; ++j) {
-        const int c = (threadIdx.x + j * threads) * 8;
-        n[j] = (int)q.cols - c;
 #pragma unroll
-        for (int i = 0; i < 8; ++i) wpost[j][i] = wpre[j][i] = gate[j][i] = 1.0f;
-        if (n[j] > 0) {
-            if (q.w_post.data) load8_any(q.w_post, c, n[j], wpost[j]);
-            if (q.w_pre.data) load8_any(q.w_pre, c, n[j], wpre[j]);
-        }
+        for (int i = 0; i < 8; ++i) wpre[j][i] = wbranch[j][i] = 1.0f;
+        if (q.w_pre.data && left(j) > 0) load8_any(q.w_pre, col(j), left(j), wpre[j]);
     }
-    const float over_cols = 1.0f / (float)q.cols;
-    int64_t gate_row = -1;
+    raw8<SF32> x[C];
+    raw8<YF32> y[C];
+    const auto load_row = [&](int64_t row) {
+#pragma unroll
+        for (int j = 0; j < C; ++j) {
+            x[j] = q.x.data && left(j) > 0 ? load8<SF32>(q.x.data, row * q.x.ld + col(j), left(j)) : zero8<SF32>();
+            y[j] = q.y.data && left(j) > 0 ? load8<YF32>(q.y.data, row * q.y.ld + col(j), left(j)) : zero8<YF32>();
+        }
+    };
+    const float over_cols = 1.0f / (float)q.cols, alpha = q.x.data ? q.residual_scale : 0.0f;
+    int64_t gate_until = 0; // first row of another gate row than the present one
+    if (blockIdx.x < q.rows) load_row(blockIdx.x);
     for (int64_t row = blockIdx.x; row < q.rows; row += gridDim.x) {
         float z[C][8], v[C][8], sum[1];
-        if (q.gate.data && row / q.gate_rows != gate_row) {
-            gate_row = row / q.gate_rows;
+        if (row >= gate_until) {
+            const int64_t gate_row = q.gate.data ? row / q.gate_rows : 0;
+            gate_until = q.gate.data ? (gate_row + 1) * q.gate_rows : q.rows;
 #pragma unroll
-            for (int j = 0; j < C; ++j)
-                if (n[j] > 0) load8_any(q.gate, gate_row * q.gate.ld + (threadIdx.x + j * threads) * 8, n[j], gate[j]);
+            for (int j = 0; j < C; ++j) {
+                float g[8] = {1.0f, 1.0f, 1.0f, 1.0f, 1.0f, 1.0f, 1.0f, 1.0f}, w[8] = {1.0f, 1.0f, 1.0f, 1.0f, 1.0f, 1.0f, 1.0f, 1.0f};
+                if (q.gate.data && left(j) > 0) load8_any(q.gate, gate_row * q.gate.ld + col(j), left(j), g);
+                if (q.w_post.data && left(j) > 0) load8_any(q.w_post, col(j), left(j), w);
+#pragma unroll
+                for (int i = 0; i < 8; ++i) wbranch[j][i] = q.branch_scale * w[i] * g[i];
+            }
         }
 #pragma unroll
         for (int j = 0; j < C; ++j) {
-            const int c = (threadIdx.x + j * threads) * 8;
-            widen8(q.x.data && n[j] > 0 ? load8<SF32>(q.x.data, row * q.x.ld + c, n[j]) : zero8<SF32>(), z[j]);
-            widen8(q.y.data && n[j] > 0 ? load8<YF32>(q.y.data, row * q.y.ld + c, n[j]) : zero8<YF32>(), v[j]);
+            widen8(x[j], z[j]);
+            widen8(y[j], v[j]);
         }
+        if (row + gridDim.x < q.rows) load_row(row + gridDim.x);
         if (q.post_norm) {
             sum[0] = 0.0f;
 #pragma unroll
@@ -65,7 +78,7 @@ template <int C, bool SF32, bool YF32> __global__ __launch_bounds__(ROW_THREADS)
 #pragma unroll
             for (int j = 0; j < C; ++j) {
                 const packed8 k = pack8(v[j]);
-                if (n[j] > 0) store_packed8(q.ckpt_y, row, (threadIdx.x + j * threads) * 8, n[j], k);
+                if (left(j) > 0) store_packed8(q.ckpt_y, row, col(j), left(j), k);
             }
         }
         sum[0] = 0.0f;
@@ -73,10 +86,10 @@ template <int C, bool SF32, bool YF32> __global__ __launch_bounds__(ROW_THREADS)
         for (int j = 0; j < C; ++j) {
 #pragma unroll
             for (int i = 0; i < 8; ++i) {
-                z[j][i] = (q.x.data ? q.residual_scale * z[j][i] : 0.0f) + q.branch_scale * (v[j][i] * wpost[j][i] * gate[j][i]);
+                z[j][i] = alpha * z[j][i] + v[j][i] * wbranch[j][i];
                 sum[0] = __builtin_fmaf(z[j][i], z[j][i], sum[0]);
             }
-            if (q.s.data && n[j] > 0) store8<SF32>(q.s.data, row * q.s.ld + (threadIdx.x + j * threads) * 8, n[j], z[j]);
+            if (q.s.data && left(j) > 0) store8<SF32>(q.s.data, row * q.s.ld + col(j), left(j), z[j]);
         }
         if (!q.h.data) continue;
         row_sums(lds, turn, waves, sum);
@@ -84,16 +97,15 @@ template <int C, bool SF32, bool YF32> __global__ __launch_bounds__(ROW_THREADS)
         if (q.rstd_pre && threadIdx.x == 0) q.rstd_pre[row] = r;
 #pragma unroll
         for (int j = 0; j < C; ++j) {
-            const int c = (threadIdx.x + j * threads) * 8;
 #pragma unroll
             for (int i = 0; i < 8; ++i) z[j][i] *= r;
             if (q.ckpt_s.codes) {
                 const packed8 k = pack8(z[j]);
-                if (n[j] > 0) store_packed8(q.ckpt_s, row, c, n[j], k);
+                if (left(j) > 0) store_packed8(q.ckpt_s, row, col(j), left(j), k);
             }
 #pragma unroll
             for (int i = 0; i < 8; ++i) z[j][i] *= wpre[j][i];
-            if (n[j] > 0) store8_any(q.h, row * q.h.ld + c, n[j], z[j]);
+            if (left(j) > 0) store8_any(q.h, row * q.h.ld + col(j), left(j), z[j]);
         }
     }
 }

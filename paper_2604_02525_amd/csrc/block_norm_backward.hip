@@ -70,6 +70,16 @@ template <bool KEPT, bool F32> __device__ __forceinline__ void load_saved(saved8
         o.r = load8<F32>(t.data, row * t.ld + c, n);
 }
 
+template <bool KEPT, bool F32> __device__ __forceinline__ void none(saved8<KEPT, F32> &o)
+{
+    if constexpr (KEPT) {
+        o.r.codes = 0;
+        o.r.scale = 0;
+    } else {
+        o.r = zero8<F32>();
+    }
+}
+
 template <bool KEPT, bool F32> __device__ __forceinline__ void widen_saved(const saved8<KEPT, F32> &o, float r, float (&v)[8])
 {
     if constexpr (KEPT) {
@@ -82,29 +92,46 @@ template <bool KEPT, bool F32> __device__ __forceinline__ void widen_saved(const
 }
 
 // C: pieces of 8 columns per lane; SF32: ds, dx and a saved s are fp32; YF32: dh, dy and a saved y are.
-template <int C, bool KEPT, bool SF32, bool YF32> __global__ __launch_bounds__(ROW_THREADS) void k_block_norm_backward(backward_t b)
+//
+// One accumulator serves both the gate and w_post: with A = sum(beta d yhat) over rows of one gate row, its gate gradient is w_post A and its part of
+// w_post's is gate A.  CUT: all rows of the run are of one gate row.  The row's values stay as they were loaded over the barrier and are widened again behind it
+// (half the registers).  Up to 8192 columns (C = 1) the weights stay in registers, and the next row is loaded meanwhile unless the saved tensors are
+// fp32; above that the sums do not all fit the registers.
+template <int C, bool KEPT, bool CUT, bool SF32, bool YF32> __global__ __launch_bounds__(ROW_THREADS) void k_block_norm_backward(backward_t b)
 {
+    // registers that a row takes as it lies in memory: two rows at a time where that leaves enough for the rest
+    constexpr int RAW = (SF32 ? 8 : 4) + (YF32 ? 8 : 4) + (KEPT ? 6 : (SF32 ? 8 : 4) + (YF32 ? 8 : 4));
+    constexpr bool AHEAD = C == 1 && RAW <= 22;
     __shared__ row_sums_t<3> lds;
     const adahop_block_norm_t &q = b.q;
     const int threads = blockDim.x, waves = threads >> 6;
     int turn = 0;
     const auto col = [&](int j) { return (int)(threadIdx.x + j * threads) * 8; };
     const auto left = [&](int j) { return (int)q.cols - col(j); };
-    float wpost[C][8], wpre[C][8], gate[C][8], apre[C][8], apost[C][8], agate[C][8];
+    const auto vector_of = [&](const adahop_tensor_t &t, int64_t at, int j, float (&v)[8]) { // ones where there is none
+#pragma unroll
+        for (int i = 0; i < 8; ++i) v[i] = 1.0f;
+        if (t.data && left(j) > 0) load8_any(t, at + col(j), left(j), v);
+    };
+    const auto branch_of = [&](int64_t gate_row, int j, float (&v)[8]) { // beta gate w_post
+        float g[8];
+        vector_of(q.gate, gate_row * q.gate.ld, j, g);
+        vector_of(q.w_post, 0, j, v);
+#pragma unroll
+        for (int i = 0; i < 8; ++i) v[i] *= q.branch_scale * g[i];
+    };
+    float wbranch[C][8], wpre[C][8], apre[C][8], apost[CUT ? 1 : C][8], agate[C][8]; // agate: A of the gate row at hand
 #pragma unroll
     for (int j = 0; j < C; ++j) {
 #pragma unroll
         for (int i = 0; i < 8; ++i) {
-            wpost[j][i] = wpre[j][i] = gate[j][i] = 1.0f;
-            apre[j][i] = apost[j][i] = agate[j][i] = 0.0f;
+            apre[j][i] = agate[j][i] = 0.0f;
+            if constexpr (!CUT) apost[j][i] = 0.0f;
         }
-        if (left(j) > 0) {
-            if (q.w_post.data) load8_any(q.w_post, col(j), left(j), wpost[j]);
-            if (q.w_pre.data) load8_any(q.w_pre, col(j), left(j), wpre[j]);
-        }
+        if constexpr (C == 1) vector_of(q.w_pre, 0, j, wpre[j]);
     }
     int64_t row = blockIdx.x * b.runs.rows, end = row + b.runs.rows;
-    if (b.runs.cuts) {
+    if constexpr (CUT) {
         const int64_t g = blockIdx.x / b.runs.cuts, cut = blockIdx.x % b.runs.cuts;
         row = g * b.runs.group + cut * b.runs.rows;
         end = row + b.runs.rows < (g + 1) * b.runs.group ? row + b.runs.rows : (g + 1) * b.runs.group;
@@ -112,71 +139,115 @@ template <int C, bool KEPT, bool SF32, bool YF32> __global__ __launch_bounds__(R
     if (end > q.rows) end = q.rows;
     const float over_cols = 1.0f / (float)q.cols;
     const bool has_h = q.d_h.data, has_y = KEPT ? q.ckpt_y.codes != nullptr : q.y.data != nullptr;
-    int64_t gate_row = -1;
-    for (; row < end; ++row) {
-        if (q.gate.data && row / q.gate_rows != gate_row) {
-            gate_row = row / q.gate_rows;
-#pragma unroll
-            for (int j = 0; j < C; ++j)
-                if (left(j) > 0) load8_any(q.gate, gate_row * q.gate.ld + col(j), left(j), gate[j]);
-        }
-        float ds[C][8], t[C][8], shat[C][8], yhat[C][8], sum[3] = {0.0f, 0.0f, 0.0f};
-        const float rs = has_h ? q.rstd_pre[row] : 0.0f, ry = q.post_norm ? q.rstd_post[row] : 1.0f;
+    raw8<SF32> ds[C];
+    raw8<YF32> dh[C];
+    saved8<KEPT, SF32> sk[C];
+    saved8<KEPT, YF32> yk[C];
+    float rs = 0.0f, ry = 1.0f;
+    const auto load_row = [&](int64_t r) {
+        if (has_h) rs = q.rstd_pre[r];
+        if (q.post_norm) ry = q.rstd_post[r];
 #pragma unroll
         for (int j = 0; j < C; ++j) {
-            raw8<SF32> rds = zero8<SF32>();
-            raw8<YF32> rdh = zero8<YF32>();
+            ds[j] = q.d_s.data && left(j) > 0 ? load8<SF32>(q.d_s.data, r * q.d_s.ld + col(j), left(j)) : zero8<SF32>();
+            dh[j] = has_h && left(j) > 0 ? load8<YF32>(q.d_h.data, r * q.d_h.ld + col(j), left(j)) : zero8<YF32>();
+            none(sk[j]);
+            none(yk[j]);
+            if (has_h && left(j) > 0) load_saved(sk[j], q.ckpt_s, q.s, r, col(j), left(j));
+            if (has_y && left(j) > 0) load_saved(yk[j], q.ckpt_y, q.y, r, col(j), left(j));
+        }
+    };
+    int64_t gate_row = 0, gate_until = row; // first row of another gate row than the present one
+    if (row < end) load_row(row);
+    while (row < end) {
+        if (row >= gate_until) {
+            gate_row = q.gate.data ? row / q.gate_rows : 0;
+            gate_until = q.gate.data ? (gate_row + 1) * q.gate_rows : end;
+            if constexpr (C == 1) {
 #pragma unroll
-            for (int i = 0; i < 8; ++i) shat[j][i] = yhat[j][i] = 0.0f;
-            if (left(j) > 0) {
-                if (q.d_s.data) rds = load8<SF32>(q.d_s.data, row * q.d_s.ld + col(j), left(j));
-                if (has_h) {
-                    rdh = load8<YF32>(q.d_h.data, row * q.d_h.ld + col(j), left(j));
-                    saved8<KEPT, SF32> k;
-                    load_saved(k, q.ckpt_s, q.s, row, col(j), left(j));
-                    widen_saved(k, rs, shat[j]);
-                }
-                if (has_y) {
-                    saved8<KEPT, YF32> k;
-                    load_saved(k, q.ckpt_y, q.y, row, col(j), left(j));
-                    widen_saved(k, ry, yhat[j]);
-                }
+                for (int j = 0; j < C; ++j) branch_of(gate_row, j, wbranch[j]);
             }
-            widen8(rds, ds[j]);
-            widen8(rdh, t[j]);
+        }
+        float sum[3] = {0.0f, 0.0f, 0.0f};
+#pragma unroll
+        for (int j = 0; j < C; ++j) {
+            float d[8], t[8], shat[8], yhat[8];
+            if constexpr (C > 1) {
+                vector_of(q.w_pre, 0, j, wpre[j]);
+                branch_of(gate_row, j, wbranch[j]);
+            }
+            widen8(ds[j], d);
+            widen8(dh[j], t);
+            widen_saved(sk[j], rs, shat);
+            widen_saved(yk[j], ry, yhat);
 #pragma unroll
             for (int i = 0; i < 8; ++i) {
-                apre[j][i] = __builtin_fmaf(t[j][i], shat[j][i], apre[j][i]);
-                t[j][i] *= wpre[j][i];
-                const float m = q.branch_scale * gate[j][i] * wpost[j][i] * yhat[j][i];
-                sum[0] = __builtin_fmaf(t[j][i], shat[j][i], sum[0]);
-                sum[1] = __builtin_fmaf(m, __builtin_fmaf(rs, t[j][i], ds[j][i]), sum[1]);
-                sum[2] = __builtin_fmaf(m, shat[j][i], sum[2]);
+                t[i] *= wpre[j][i];
+                const float m = wbranch[j][i] * yhat[i];
+                sum[0] = __builtin_fmaf(t[i], shat[i], sum[0]);
+                sum[1] = __builtin_fmaf(m, __builtin_fmaf(rs, t[i], d[i]), sum[1]);
+                sum[2] = __builtin_fmaf(m, shat[i], sum[2]);
             }
+        }
+        raw8<SF32> ds0[C];
+        raw8<YF32> dh0[C];
+        saved8<KEPT, SF32> sk0[C];
+        saved8<KEPT, YF32> yk0[C];
+        const float rs0 = rs, ry0 = ry;
+#pragma unroll
+        for (int j = 0; j < C; ++j) {
+            ds0[j] = ds[j], dh0[j] = dh[j], sk0[j] = sk[j], yk0[j] = yk[j];
+            keep_raw(ds0[j]), keep_raw(dh0[j]), keep_raw(sk0[j].r), keep_raw(yk0[j].r);
+        }
+        if constexpr (AHEAD) {
+            if (row + 1 < end) load_row(row + 1);
         }
         row_sums(lds, turn, waves, sum);
-        const float c1 = sum[0] * over_cols, c2 = q.post_norm ? (sum[1] - rs * c1 * sum[2]) * over_cols : 0.0f;
-        const bool gate_ends = !b.runs.cuts && (row + 1 == end || (row + 1) % b.runs.group == 0);
+        const float c1 = sum[0] * over_cols, c2 = q.post_norm ? (sum[1] - rs0 * c1 * sum[2]) * over_cols : 0.0f;
 #pragma unroll
         for (int j = 0; j < C; ++j) {
-            float dx[8], dy[8];
+            float d[8], t[8], shat[8], yhat[8], dx[8], dy[8];
+            if constexpr (C > 1) {
+                vector_of(q.w_pre, 0, j, wpre[j]);
+                branch_of(gate_row, j, wbranch[j]);
+            }
+            widen8(ds0[j], d);
+            widen8(dh0[j], t);
+            widen_saved(sk0[j], rs0, shat);
+            widen_saved(yk0[j], ry0, yhat);
 #pragma unroll
             for (int i = 0; i < 8; ++i) {
-                const float d = __builtin_fmaf(rs, __builtin_fmaf(-c1, shat[j][i], t[j][i]), ds[j][i]), u = q.branch_scale * d, uy = u * yhat[j][i];
-                dx[i] = q.residual_scale * d;
-                dy[i] = ry * __builtin_fmaf(-c2, yhat[j][i], u * gate[j][i] * wpost[j][i]);
-                apost[j][i] = __builtin_fmaf(uy, gate[j][i], apost[j][i]);
-                agate[j][i] = __builtin_fmaf(uy, wpost[j][i], agate[j][i]);
+                apre[j][i] = __builtin_fmaf(t[i], shat[i], apre[j][i]);
+                d[i] = __builtin_fmaf(rs0, __builtin_fmaf(-c1, shat[i], t[i] * wpre[j][i]), d[i]);
+                dx[i] = q.residual_scale * d[i];
+                dy[i] = ry0 * __builtin_fmaf(-c2, yhat[i], d[i] * wbranch[j][i]);
+                agate[j][i] = __builtin_fmaf(q.branch_scale * d[i], yhat[i], agate[j][i]);
             }
             if (left(j) > 0) {
                 if (q.d_x.data) store8<SF32>(q.d_x.data, row * q.d_x.ld + col(j), left(j), dx);
                 if (q.d_y.data) store8<YF32>(q.d_y.data, row * q.d_y.ld + col(j), left(j), dy);
-                if (gate_ends && q.d_gate.data) store8_any(q.d_gate, row / q.gate_rows * q.d_gate.ld + col(j), left(j), agate[j]);
             }
-            if (gate_ends) {
+        }
+        ++row;
+        if constexpr (!CUT) {
+            if (row == end || row == gate_until) { // the gate row is complete
 #pragma unroll
-                for (int i = 0; i < 8; ++i) agate[j][i] = 0.0f;
+                for (int j = 0; j < C; ++j) {
+                    float g[8], w[8];
+                    vector_of(q.gate, gate_row * q.gate.ld, j, g);
+                    vector_of(q.w_post, 0, j, w);
+#pragma unroll
+                    for (int i = 0; i < 8; ++i) {
+                        apost[j][i] = __builtin_fmaf(agate[j][i], g[i], apost[j][i]);
+                        w[i] *= agate[j][i];
+                        agate[j][i] = 0.0f;
+                    }
+                    if (q.d_gate.data && left(j) > 0) store8_any(q.d_gate, gate_row * q.d_gate.ld + col(j), left(j), w);
+                }
             }
+        }
+        if constexpr (!AHEAD) {
+            if (row < end) load_row(row);
         }
     }
     const int64_t one = b.runs.number * q.cols, at = blockIdx.x * q.cols;
@@ -184,13 +255,25 @@ template <int C, bool KEPT, bool SF32, bool YF32> __global__ __launch_bounds__(R
     for (int j = 0; j < C; ++j) {
         if (left(j) <= 0) continue;
         if (q.d_w_pre) store8<true>(b.part ? b.part + at : q.d_w_pre, col(j), left(j), apre[j]);
-        if (q.d_w_post) store8<true>(b.part ? b.part + one + at : q.d_w_post, col(j), left(j), apost[j]);
-        if (q.d_gate.data && b.runs.cuts) {
-            if (b.part)
-                store8<true>(b.part + 2 * one + at, col(j), left(j), agate[j]);
-            else
-                store8_any(q.d_gate, col(j), left(j), agate[j]);
+        float v[8];
+        if constexpr (CUT) {
+            vector_of(q.w_post, 0, j, v);
+#pragma unroll
+            for (int i = 0; i < 8; ++i) v[i] *= agate[j][i];
+            if (q.d_gate.data) {
+                if (b.part)
+                    store8<true>(b.part + 2 * one + at, col(j), left(j), v);
+                else
+                    store8_any(q.d_gate, col(j), left(j), v);
+            }
+            vector_of(q.gate, gate_row * q.gate.ld, j, v);
+#pragma unroll
+            for (int i = 0; i < 8; ++i) v[i] *= agate[j][i];
+        } else {
+#pragma unroll
+            for (int i = 0; i < 8; ++i) v[i] = apost[j][i];
         }
+        if (q.d_w_post) store8<true>(b.part ? b.part + one + at : q.d_w_post, col(j), left(j), v);
     }
 }
 
@@ -251,13 +334,21 @@ int zero_from(const adahop_block_norm_t &q, int64_t from, hipStream_t st)
     return check_launch();
 }
 
-template <int C, bool KEPT> void launch(const backward_t &b, bool s32, bool y32, int threads, hipStream_t st)
+template <int C, bool KEPT, bool CUT> void launch(const backward_t &b, bool s32, bool y32, int threads, hipStream_t st)
 {
     const unsigned n = (unsigned)b.runs.number;
     if (s32)
-        y32 ? k_block_norm_backward<C, KEPT, true, true><<<n, threads, 0, st>>>(b) : k_block_norm_backward<C, KEPT, true, false><<<n, threads, 0, st>>>(b);
+        y32 ? k_block_norm_backward<C, KEPT, CUT, true, true><<<n, threads, 0, st>>>(b) : k_block_norm_backward<C, KEPT, CUT, true, false><<<n, threads, 0, st>>>(b);
     else
-        y32 ? k_block_norm_backward<C, KEPT, false, true><<<n, threads, 0, st>>>(b) : k_block_norm_backward<C, KEPT, false, false><<<n, threads, 0, st>>>(b);
+        y32 ? k_block_norm_backward<C, KEPT, CUT, false, true><<<n, threads, 0, st>>>(b) : k_block_norm_backward<C, KEPT, CUT, false, false><<<n, threads, 0, st>>>(b);
+}
+
+template <int C> void launch(const backward_t &b, bool s32, bool y32, bool kept, int threads, hipStream_t st)
+{
+    if (kept)
+        b.runs.cuts ? launch<C, true, true>(b, s32, y32, threads, st) : launch<C, true, false>(b, s32, y32, threads, st);
+    else
+        b.runs.cuts ? launch<C, false, true>(b, s32, y32, threads, st) : launch<C, false, false>(b, s32, y32, threads, st);
 }
 
 } // namespace
@@ -277,9 +368,9 @@ int launch_block_norm_backward(const adahop_block_norm_t &q, bool s32, bool y32,
     if (b.runs.number > 1) b.part = static_cast<float *>(workspace);
     const int threads = threads_of(q.cols);
     if (q.cols > 8 * ROW_THREADS)
-        kept ? launch<2, true>(b, s32, y32, threads, st) : launch<2, false>(b, s32, y32, threads, st);
+        launch<2>(b, s32, y32, kept, threads, st);
     else
-        kept ? launch<1, true>(b, s32, y32, threads, st) : launch<1, false>(b, s32, y32, threads, st);
+        launch<1>(b, s32, y32, kept, threads, st);
     int rc = check_launch();
     if (rc == ADAHOP_OK && q.d_gate.data && q.gates > ceil_div(q.rows, q.gate_rows)) rc = zero_from(q, ceil_div(q.rows, q.gate_rows), st);
     if (rc != ADAHOP_OK || !b.part) return rc;

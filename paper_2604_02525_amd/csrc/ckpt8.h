@@ -68,6 +68,13 @@ template <bool F32> __device__ __forceinline__ void widen8(const raw8<F32> &r, f
     }
 }
 
+// Keeps eight elements as they lie in memory: what has been made of them so far is not kept in registers for later.
+template <bool F32> __device__ __forceinline__ void keep_raw(raw8<F32> &r)
+{
+    asm volatile("" : "+v"(r.w[0]));
+    if constexpr (F32) asm volatile("" : "+v"(r.w[1]));
+}
+
 // Eight elements of a tensor whose type is known at run time only: for what is read once, or seldom.
 __device__ __forceinline__ void load8_any(const adahop_tensor_t &t, int64_t at, int n, float (&v)[8])
 {
@@ -192,7 +199,7 @@ __device__ __forceinline__ void store_packed8(const adahop_ckpt8_t &k, int64_t r
 {
     uint8_t *const at = k.codes + row * k.ld_codes + c;
     if (n >= 8) {
-        *reinterpret_cast<u32x2 *>(at) = p.codes;
+        __builtin_nontemporal_store(p.codes, reinterpret_cast<u32x2 *>(at)); // read by the backward pass, not by what follows: out of the caches' way
     } else {
 #pragma unroll
         for (int i = 0; i < 7; ++i)
@@ -231,6 +238,8 @@ __device__ __forceinline__ void unpack8(const packed8 &p, float (&v)[8])
         v[4 * i + 3] = b.y * s;
     }
 }
+
+__device__ __forceinline__ void keep_raw(packed8 &p) { asm volatile("" : "+v"(p.codes)); }
 
 // ---- rows of any width, without regard to where they end ----------------------------------------------------------------
 // The blocks of 32 of all rows are numbered through: block b lies in row b / per_row.  Division by multiplication, exact for
