@@ -453,45 +453,36 @@ def adahop_select_strategy(pattern_a, pattern_b, level=1):
 # Tensors are 2-D on the GPU, bfloat16 or float32, with unit column stride and any row stride; weights are vectors.  An 8-bit
 # checkpoint is a pair (codes, scales) of uint8 tensors [rows, cols] and [rows, ceil(cols / 32)].
 
-def _tensor(t, rows, cols, device, what):
-    if t is None:
-        return adahop_tensor_t()
-    if t.dtype is not torch.bfloat16 and t.dtype is not torch.float32:
-        raise TypeError(f"{what}: bfloat16 or float32 wanted, not {t.dtype}")
-    if t.shape != (rows, cols) or (rows and cols > 1 and t.stride(1) != 1) or t.device != device:
-        raise ValueError(f"{what}: a [{rows}, {cols}] tensor with unit column stride on {device} wanted, not {tuple(t.shape)}, "
-                         f"strides {t.stride()}, on {t.device}")
-    return adahop_tensor_t(t.data_ptr(), t.stride(0) if rows > 1 else cols, t.element_size() == 4)
+_training_calls = None
 
 
-def _vector(t, cols, device, what):
-    if t is None:
-        return adahop_tensor_t()
-    if t.dtype is not torch.bfloat16 and t.dtype is not torch.float32:
-        raise TypeError(f"{what}: bfloat16 or float32 wanted, not {t.dtype}")
-    if t.shape != (cols,) or (cols > 1 and t.stride(0) != 1) or t.device != device:
-        raise ValueError(f"{what}: a dense vector of {cols} elements on {device} wanted, not {tuple(t.shape)}, strides {t.stride()}, on {t.device}")
-    return adahop_tensor_t(t.data_ptr(), cols, t.element_size() == 4)
+def _training():
+    """_call with the addresses of the training operators' entry points; raises where _call.so is not built."""
+    global _training_calls
+    if _training_calls is None:
+        L = lib()
+        try:
+            from . import _call
+        except ImportError as e:
+            raise RuntimeError("_call.so is missing or stale: run `python -c 'import __graft_entry__ as g; g.build()'`") from e
+        _call.init_training(lambda: _stream(None), *(C.cast(getattr(L, "adahop_" + n), C.c_void_p).value for n in (
+            "ckpt8_pack", "ckpt8_unpack", "swiglu", "swiglu_backward", "block_norm", "block_norm_backward",
+            "block_norm_backward_workspace_bytes", "ckpt8_wgrad", "ckpt8_wgrad_workspace_bytes")))
+        _training_calls = _call
+    return _training_calls
 
 
-def _floats(t, n, device, what):
-    if t is None:
+def _handle(stream):
+    return None if stream is None else _stream(stream)
+
+
+def _own_workspace(stream, need, device):
+    """Scratch for a call on a stream of its own, None on the current one (the call makes its own there)."""
+    if stream is None or not need:
         return None
-    if t.dtype is not torch.float32 or t.shape != (n,) or (n > 1 and t.stride(0) != 1) or t.device != device:
-        raise ValueError(f"{what}: a dense float32 vector of {n} elements on {device} wanted")
-    return t.data_ptr()
-
-
-def _ckpt8(pair, rows, cols, device, what):
-    if pair is None:
-        return adahop_ckpt8_t()
-    codes, scales = pair
-    blocks = (cols + 31) // 32
-    for t, width in ((codes, cols), (scales, blocks)):
-        if t.dtype is not torch.uint8 or t.shape != (rows, width) or (rows and width > 1 and t.stride(1) != 1) or t.device != device:
-            raise ValueError(f"{what}: uint8 tensors [{rows}, {cols}] and [{rows}, {blocks}] with unit column stride on {device} wanted")
-    return adahop_ckpt8_t(codes.data_ptr(), scales.data_ptr(), codes.stride(0) if rows > 1 else (cols + 15) // 16 * 16,
-                          scales.stride(0) if rows > 1 else blocks)
+    workspace = _u8((need,), device)
+    _hold(stream, workspace)
+    return workspace
 
 
 def adahop_ckpt8_empty(rows, cols, device="cuda"):
@@ -501,65 +492,34 @@ def adahop_ckpt8_empty(rows, cols, device="cuda"):
 
 def adahop_ckpt8_pack(x, out=None, stream=None):
     """The 8-bit checkpoint (codes, scales) of x."""
-    rows, cols = x.shape
-    out = adahop_ckpt8_empty(rows, cols, x.device) if out is None else out
-    _check(lib().adahop_ckpt8_pack(rows, cols, C.byref(_tensor(x, rows, cols, x.device, "x")), C.byref(_ckpt8(out, rows, cols, x.device, "out")),
-                                   _stream(stream)), "adahop_ckpt8_pack")
+    status, out = _training().pack(x, out, _handle(stream))
+    _check(status, "adahop_ckpt8_pack")
     return out
 
 
 def adahop_ckpt8_unpack(x8, col_scale=None, out=None, dtype=torch.bfloat16, stream=None):
-    """What a checkpoint stands for, times col_scale (a vector) if given, as `dtype`."""
-    rows, cols = x8[0].shape
-    dev = x8[0].device
-    out = torch.empty((rows, cols), dtype=dtype, device=dev) if out is None else out
-    _check(lib().adahop_ckpt8_unpack(rows, cols, C.byref(_ckpt8(x8, rows, cols, dev, "x8")), C.byref(_vector(col_scale, cols, dev, "col_scale")),
-                                     C.byref(_tensor(out, rows, cols, dev, "out")), _stream(stream)), "adahop_ckpt8_unpack")
+    """What a checkpoint stands for, times col_scale (a vector) if given, as `dtype` (bfloat16 or float32)."""
+    if dtype is not torch.bfloat16 and dtype is not torch.float32:
+        raise TypeError(f"dtype: bfloat16 or float32 wanted, not {dtype}")
+    status, out = _training().unpack(x8, col_scale, out, dtype is torch.float32, _handle(stream))
+    _check(status, "adahop_ckpt8_unpack")
     return out
 
 
 def adahop_swiglu(g, u, a=None, ckpt_g=None, ckpt_u=None, keep8=False, stream=None):
     """a = silu(g) * u (bfloat16 unless a is given).  keep8: g's and u's 8-bit checkpoints too.  Returns dict(a, ckpt_g, ckpt_u)."""
-    rows, cols = g.shape
-    dev = g.device
-    a = torch.empty((rows, cols), dtype=torch.bfloat16, device=dev) if a is None else a
-    if keep8:
-        ckpt_g = adahop_ckpt8_empty(rows, cols, dev) if ckpt_g is None else ckpt_g
-        ckpt_u = adahop_ckpt8_empty(rows, cols, dev) if ckpt_u is None else ckpt_u
-    p = adahop_swiglu_t(rows, cols, _tensor(g, rows, cols, dev, "g"), _tensor(u, rows, cols, dev, "u"), _tensor(a, rows, cols, dev, "a"),
-                        _ckpt8(ckpt_g, rows, cols, dev, "ckpt_g"), _ckpt8(ckpt_u, rows, cols, dev, "ckpt_u"))
-    _check(lib().adahop_swiglu(C.byref(p), _stream(stream)), "adahop_swiglu")
-    return dict(a=a, ckpt_g=ckpt_g, ckpt_u=ckpt_u)
+    status, out = _training().swiglu(g, u, a, ckpt_g, ckpt_u, keep8, _handle(stream))
+    _check(status, "adahop_swiglu")
+    return out
 
 
 def adahop_swiglu_backward(g, u, d_a, d_g=None, d_u=None, a=None, stream=None):
     """Gradients of adahop_swiglu's inputs.  g, u: tensors, or their 8-bit checkpoints.  a: where silu(g) * u is written again, a
     tensor or room for an 8-bit checkpoint; None: it is not.  d_g and d_u are by default the halves of one new bfloat16 tensor, the output
     gradient of a product that computed [g | u].  Returns dict(d_g, d_u, a)."""
-    rows, cols = d_a.shape
-    dev = d_a.device
-    if d_g is None and d_u is None:
-        both = torch.empty((rows, 2 * cols), dtype=torch.bfloat16, device=dev)
-        d_g, d_u = both[:, :cols], both[:, cols:]
-    d_g, d_u = (torch.empty((rows, cols), dtype=torch.bfloat16, device=dev) if t is None else t for t in (d_g, d_u))
-    p = adahop_swiglu_t(rows, cols)
-    for name, t in (("g", g), ("u", u), ("a", a)):
-        if isinstance(t, tuple):
-            setattr(p, "ckpt_" + name, _ckpt8(t, rows, cols, dev, name))
-        else:
-            setattr(p, name, _tensor(t, rows, cols, dev, name))
-    p.d_a, p.d_g, p.d_u = _tensor(d_a, rows, cols, dev, "d_a"), _tensor(d_g, rows, cols, dev, "d_g"), _tensor(d_u, rows, cols, dev, "d_u")
-    _check(lib().adahop_swiglu_backward(C.byref(p), _stream(stream)), "adahop_swiglu_backward")
-    return dict(d_g=d_g, d_u=d_u, a=a)
-
-
-def _set_gate(p, gate, gate_rows, rows, cols, dev):
-    if gate is None:
-        return
-    if gate.dim() == 1:
-        p.gate, p.gates, p.gate_rows = _vector(gate, cols, dev, "gate"), 1, max(rows, 1)
-    else:
-        p.gate, p.gates, p.gate_rows = _tensor(gate, gate.shape[0], cols, dev, "gate"), gate.shape[0], int(gate_rows)
+    status, out = _training().swiglu_backward(g, u, d_a, d_g, d_u, a, _handle(stream))
+    _check(status, "adahop_swiglu_backward")
+    return out
 
 
 def adahop_block_norm(x=None, y=None, w_post=None, w_pre=None, gate=None, gate_rows=1, residual_scale=1.0, branch_scale=1.0, eps=1e-6,
@@ -571,34 +531,12 @@ def adahop_block_norm(x=None, y=None, w_post=None, w_pre=None, gate=None, gate_r
     as it is; pre_norm=False: no h.  gate: a vector, or [n, cols] with each row standing for gate_rows rows.  s is of x's type
     and h bfloat16 unless they are given; s may be x.  keep: what the backward pass takes -- "stats": rstd_post and rstd_pre (beside y and s
     themselves), "ckpt8": these and 8-bit checkpoints of norm(y) and norm(s).  Returns dict(s, h, rstd_post, rstd_pre, ckpt_y, ckpt_s)."""
-    some = y if x is None else x
-    rows, cols = some.shape
-    dev = some.device
-    post_norm = post_norm and y is not None
-    f32 = lambda: torch.empty(rows, dtype=torch.float32, device=dev)  # noqa: E731
-    same = y is None and residual_scale == 1.0 and (s is None or s is x)      # s = x is there already
-    if s is None:
-        s = x if same else torch.empty((rows, cols), dtype=some.dtype, device=dev)
-    if pre_norm and h is None:
-        h = torch.empty((rows, cols), dtype=torch.bfloat16, device=dev)
-    if keep is not None:
-        if keep not in ("stats", "ckpt8"):
-            raise ValueError(f"keep: None, 'stats' or 'ckpt8', not {keep!r}")
-        rstd_post = f32() if post_norm and rstd_post is None else rstd_post
-        rstd_pre = f32() if pre_norm and rstd_pre is None else rstd_pre
-        if keep == "ckpt8":
-            ckpt_y = adahop_ckpt8_empty(rows, cols, dev) if y is not None and ckpt_y is None else ckpt_y
-            ckpt_s = adahop_ckpt8_empty(rows, cols, dev) if pre_norm and ckpt_s is None else ckpt_s
-    p = adahop_block_norm_t(rows, cols, int(post_norm), eps, residual_scale, branch_scale, _tensor(x, rows, cols, dev, "x"),
-                            _tensor(y, rows, cols, dev, "y"), _vector(w_post, cols, dev, "w_post"), _vector(w_pre, cols, dev, "w_pre"))
-    _set_gate(p, gate, gate_rows, rows, cols, dev)
-    if not same:
-        p.s = _tensor(s, rows, cols, dev, "s")
-    p.h = _tensor(h if pre_norm else None, rows, cols, dev, "h")
-    p.rstd_post, p.rstd_pre = _floats(rstd_post, rows, dev, "rstd_post"), _floats(rstd_pre, rows, dev, "rstd_pre")
-    p.ckpt_y, p.ckpt_s = _ckpt8(ckpt_y, rows, cols, dev, "ckpt_y"), _ckpt8(ckpt_s, rows, cols, dev, "ckpt_s")
-    _check(lib().adahop_block_norm(C.byref(p), _stream(stream)), "adahop_block_norm")
-    return dict(s=s, h=h, rstd_post=rstd_post, rstd_pre=rstd_pre, ckpt_y=ckpt_y, ckpt_s=ckpt_s)
+    if keep is not None and keep != "stats" and keep != "ckpt8":
+        raise ValueError(f"keep: None, 'stats' or 'ckpt8', not {keep!r}")
+    status, out = _training().block_norm(x, y, w_post, w_pre, gate, gate_rows, residual_scale, branch_scale, eps, post_norm, pre_norm, s, h, rstd_post,
+                                         rstd_pre, ckpt_y, ckpt_s, keep == "stats", keep == "ckpt8", _handle(stream))
+    _check(status, "adahop_block_norm")
+    return out
 
 
 def adahop_block_norm_backward(d_s, d_h, s, y, rstd_pre, rstd_post, w_post=None, w_pre=None, gate=None, gate_rows=1, residual_scale=1.0,
@@ -607,57 +545,22 @@ def adahop_block_norm_backward(d_s, d_h, s, y, rstd_pre, rstd_post, w_post=None,
     """Gradients of adahop_block_norm's inputs from those of s and h (either may be None).  s, y: the tensors, or their
     8-bit checkpoints ckpt_s, ckpt_y; y None: there was no block output.  Gradients of weights (float32) and of the gate are computed for those that
     are given; the others' places are None.  d_x may be d_s, d_y may be d_h.  Returns dict(d_x, d_y, d_w_post, d_w_pre, d_gate)."""
-    some = d_h if d_s is None else d_s
-    rows, cols = some.shape
-    dev = some.device
-    post_norm = post_norm and y is not None
-    if d_x is None:
-        d_x = torch.empty((rows, cols), dtype=some.dtype if d_s is not None or isinstance(s, tuple) or s is None else s.dtype, device=dev)
-    if y is not None and d_y is None:
-        d_y = torch.empty((rows, cols), dtype=d_h.dtype if d_h is not None else torch.bfloat16 if isinstance(y, tuple) else y.dtype, device=dev)
-    vector = lambda: torch.empty(cols, dtype=torch.float32, device=dev)  # noqa: E731
-    d_w_post = vector() if w_post is not None and d_w_post is None else d_w_post
-    d_w_pre = vector() if w_pre is not None and d_h is not None and d_w_pre is None else d_w_pre
-    d_gate = torch.empty_like(gate, memory_format=torch.contiguous_format) if gate is not None and d_gate is None else d_gate
-    p = adahop_block_norm_t(rows, cols, int(post_norm), 0.0, residual_scale, branch_scale)
-    p.w_post, p.w_pre = _vector(w_post, cols, dev, "w_post"), _vector(w_pre, cols, dev, "w_pre")
-    _set_gate(p, gate, gate_rows, rows, cols, dev)
-    for name, t in (("s", s), ("y", y)):
-        if isinstance(t, tuple):
-            setattr(p, "ckpt_" + name, _ckpt8(t, rows, cols, dev, name))
-        else:
-            setattr(p, name, _tensor(t, rows, cols, dev, name))
-    p.rstd_post, p.rstd_pre = _floats(rstd_post, rows, dev, "rstd_post"), _floats(rstd_pre, rows, dev, "rstd_pre")
-    for name, t in (("d_s", d_s), ("d_h", d_h), ("d_x", d_x), ("d_y", d_y)):
-        setattr(p, name, _tensor(t, rows, cols, dev, name))
-    if d_gate is not None:
-        p.d_gate = _vector(d_gate, cols, dev, "d_gate") if d_gate.dim() == 1 else _tensor(d_gate, p.gates, cols, dev, "d_gate")
-    p.d_w_post, p.d_w_pre = _floats(d_w_post, cols, dev, "d_w_post"), _floats(d_w_pre, cols, dev, "d_w_pre")
-    if workspace is None:
-        need = int(lib().adahop_block_norm_backward_workspace_bytes(rows, cols, p.gate_rows))
-        if need:
-            workspace = _u8((need,), dev)
-            _hold(stream, workspace)
-    _check(lib().adahop_block_norm_backward(C.byref(p), _ptr(workspace), 0 if workspace is None else workspace.numel(), _stream(stream)),
-           "adahop_block_norm_backward")
-    return dict(d_x=d_x, d_y=d_y, d_w_post=d_w_post, d_w_pre=d_w_pre, d_gate=d_gate)
+    if workspace is None and stream is not None:
+        some = d_h if d_s is None else d_s
+        rows = some.shape[0]
+        every = 0 if gate is None else max(rows, 1) if gate.dim() == 1 else int(gate_rows)
+        workspace = _own_workspace(stream, int(lib().adahop_block_norm_backward_workspace_bytes(rows, some.shape[1], every)), some.device)
+    status, out = _training().block_norm_backward(d_s, d_h, s, y, rstd_pre, rstd_post, w_post, w_pre, gate, gate_rows, residual_scale, branch_scale,
+                                                  post_norm, d_x, d_y, d_w_post, d_w_pre, d_gate, workspace, _handle(stream))
+    _check(status, "adahop_block_norm_backward")
+    return out
 
 
 def adahop_ckpt8_wgrad(G, x8, col_scale=None, add=None, Cout=None, c_bf16=False, workspace=None, stream=None):
     """Weight gradient [d_out, d_in] of a linear layer from its output gradient G (bfloat16 [tokens, d_out]) and the 8-bit checkpoint
     of its input: G^T x, times col_scale per input feature, plus add.  float32 unless c_bf16 or Cout say otherwise; add may be Cout."""
-    tokens, d_out = G.shape
-    d_in, dev = x8[0].shape[1], G.device
-    Cout = torch.empty((d_out, d_in), dtype=torch.bfloat16 if c_bf16 else torch.float32, device=dev) if Cout is None else Cout
-    if workspace is None:
-        need = int(lib().adahop_ckpt8_wgrad_workspace_bytes(tokens, d_out, d_in))
-        if need:
-            workspace = _u8((need,), dev)
-            _hold(stream, workspace)
-    g = _tensor(G, tokens, d_out, dev, "G")
-    g.ld = g.ld if tokens > 1 else (d_out + 7) // 8 * 8
-    _check(lib().adahop_ckpt8_wgrad(tokens, d_out, d_in, C.byref(g), C.byref(_ckpt8(x8, tokens, d_in, dev, "x8")),
-                                    C.byref(_vector(col_scale, d_in, dev, "col_scale")), C.byref(_tensor(add, d_out, d_in, dev, "add")),
-                                    C.byref(_tensor(Cout, d_out, d_in, dev, "Cout")), _ptr(workspace), 0 if workspace is None else workspace.numel(),
-                                    _stream(stream)), "adahop_ckpt8_wgrad")
-    return Cout
+    if workspace is None and stream is not None:
+        workspace = _own_workspace(stream, int(lib().adahop_ckpt8_wgrad_workspace_bytes(*G.shape, x8[0].shape[1])), G.device)
+    status, out = _training().wgrad(G, x8, col_scale, add, Cout, c_bf16, workspace, _handle(stream))
+    _check(status, "adahop_ckpt8_wgrad")
+    return out

@@ -22,13 +22,13 @@ def hipcc():
 
 
 def call_command():
-    """The command that builds csrc/call.cpp, a Python module against torch's own headers and libraries."""
+    """The command that builds csrc/call.cpp and call_training.cpp, a Python module against torch's own headers and libraries."""
     import torch
     from torch.utils import cpp_extension
     root = os.path.dirname(torch.__file__)
     include = [f"-I{p}" for p in cpp_extension.include_paths() + [sysconfig.get_paths()["include"]]]
     return ([os.environ.get("CXX", "g++"), "-O2", "-std=c++17", "-fPIC", "-shared", "-Wall", f"-D_GLIBCXX_USE_CXX11_ABI={int(torch._C._GLIBCXX_USE_CXX11_ABI)}"]
-            + include + [os.path.join(CSRC, "call.cpp"), "-o", CALL, "-L" + os.path.join(root, "lib"), "-ltorch_python", "-ltorch_cpu", "-lc10"])
+            + include + [os.path.join(CSRC, "call.cpp"), os.path.join(CSRC, "call_training.cpp"), "-o", CALL, "-L" + os.path.join(root, "lib"), "-ltorch_python", "-ltorch_cpu", "-lc10"])
 
 
 def build(verbose: bool = False) -> str:

@@ -169,6 +169,8 @@ PyModuleDef module = {PyModuleDef_HEAD_INIT, "_call", nullptr, -1, methods, null
 
 } // namespace
 
+int add_training_calls(PyObject *module); // call_training.cpp
+
 PyMODINIT_FUNC PyInit__call(void)
 {
     struct {
@@ -177,5 +179,10 @@ PyMODINIT_FUNC PyInit__call(void)
     } const names[] = {{&n_tensor, "tensor"}, {&n_outer, "outer"}, {&n_K, "K"}, {&n_ld, "ld"}, {&n_k_contig, "k_contig"}};
     for (const auto &x : names)
         if (!(*x.name = PyUnicode_InternFromString(x.text))) return nullptr;
-    return PyModule_Create(&module);
+    PyObject *const m = PyModule_Create(&module);
+    if (m && add_training_calls(m) < 0) {
+        Py_DECREF(m);
+        return nullptr;
+    }
+    return m;
 }
