@@ -29,13 +29,14 @@ template <bool F32> __device__ __forceinline__ raw8<F32> zero8()
     return r;
 }
 
-// The n >= 1 elements at element `at` of `base`; those from n on count as zero.
-template <bool F32> __device__ __forceinline__ raw8<F32> load8(const void *base, int64_t at, int n)
+// The n >= 1 elements at element `at` of `base`; those from n on count as zero.  ODD = false: n is 8, as
+// everywhere in rows of whole pieces.
+template <bool F32, bool ODD = true> __device__ __forceinline__ raw8<F32> load8(const void *base, int64_t at, int n)
 {
     raw8<F32> r;
     if constexpr (F32) {
         const uint32_t *const p = static_cast<const uint32_t *>(base) + at;
-        if (n >= 8) {
+        if (!ODD || n >= 8) {
             r.w[0] = *reinterpret_cast<const u32x4_e4 *>(p);
             r.w[1] = *reinterpret_cast<const u32x4_e4 *>(p + 4);
         } else {
@@ -44,7 +45,7 @@ template <bool F32> __device__ __forceinline__ raw8<F32> load8(const void *base,
         }
     } else {
         const uint16_t *const p = static_cast<const uint16_t *>(base) + at;
-        if (n >= 8) {
+        if (!ODD || n >= 8) {
             r.w[0] = *reinterpret_cast<const u32x4_e2 *>(p);
         } else {
             uint32_t e[8];
@@ -76,12 +77,12 @@ template <bool F32> __device__ __forceinline__ void keep_raw(raw8<F32> &r)
 }
 
 // Eight elements of a tensor whose type is known at run time only: for what is read once, or seldom.
-__device__ __forceinline__ void load8_any(const adahop_tensor_t &t, int64_t at, int n, float (&v)[8])
+template <bool ODD = true> __device__ __forceinline__ void load8_any(const adahop_tensor_t &t, int64_t at, int n, float (&v)[8])
 {
     if (t.f32) {
-        widen8<true>(load8<true>(t.data, at, n), v);
+        widen8<true>(load8<true, ODD>(t.data, at, n), v);
     } else {
-        widen8<false>(load8<false>(t.data, at, n), v);
+        widen8<false>(load8<false, ODD>(t.data, at, n), v);
     }
 }
 
@@ -92,11 +93,11 @@ __device__ __forceinline__ uint32_t bf16_pair(float a, float b) // round to near
 }
 
 // The first n >= 1 of eight values, rounded once where the tensor is bf16.
-template <bool F32> __device__ __forceinline__ void store8(void *base, int64_t at, int n, const float (&v)[8])
+template <bool F32, bool ODD = true> __device__ __forceinline__ void store8(void *base, int64_t at, int n, const float (&v)[8])
 {
     if constexpr (F32) {
         float *const p = static_cast<float *>(base) + at;
-        if (n >= 8) {
+        if (!ODD || n >= 8) {
             u32x4 lo, hi;
 #pragma unroll
             for (int i = 0; i < 4; ++i) {
@@ -115,7 +116,7 @@ template <bool F32> __device__ __forceinline__ void store8(void *base, int64_t a
         u32x4 w;
 #pragma unroll
         for (int i = 0; i < 4; ++i) w[i] = bf16_pair(v[2 * i], v[2 * i + 1]);
-        if (n >= 8) {
+        if (!ODD || n >= 8) {
             *reinterpret_cast<u32x4_e2 *>(p) = w;
         } else {
 #pragma unroll
@@ -125,12 +126,12 @@ template <bool F32> __device__ __forceinline__ void store8(void *base, int64_t a
     }
 }
 
-__device__ __forceinline__ void store8_any(const adahop_tensor_t &t, int64_t at, int n, const float (&v)[8])
+template <bool ODD = true> __device__ __forceinline__ void store8_any(const adahop_tensor_t &t, int64_t at, int n, const float (&v)[8])
 {
     if (t.f32)
-        store8<true>(t.data, at, n, v);
+        store8<true, ODD>(t.data, at, n, v);
     else
-        store8<false>(t.data, at, n, v);
+        store8<false, ODD>(t.data, at, n, v);
 }
 
 template <int CTRL> __device__ __forceinline__ uint32_t max_with(uint32_t m)
@@ -195,10 +196,10 @@ __device__ __forceinline__ packed8 pack8(const float (&v)[8])
 }
 
 // Of the piece of n elements that begins at column c (a multiple of 8) of a row.
-__device__ __forceinline__ void store_packed8(const adahop_ckpt8_t &k, int64_t row, int c, int n, const packed8 &p)
+template <bool ODD = true> __device__ __forceinline__ void store_packed8(const adahop_ckpt8_t &k, int64_t row, int c, int n, const packed8 &p)
 {
     uint8_t *const at = k.codes + row * k.ld_codes + c;
-    if (n >= 8) {
+    if (!ODD || n >= 8) {
         __builtin_nontemporal_store(p.codes, reinterpret_cast<u32x2 *>(at)); // read by the backward pass, not by what follows: out of the caches' way
     } else {
 #pragma unroll
@@ -208,11 +209,11 @@ __device__ __forceinline__ void store_packed8(const adahop_ckpt8_t &k, int64_t r
     if ((c & 31) == 0) k.scales[row * k.ld_scales + (c >> 5)] = p.scale;
 }
 
-__device__ __forceinline__ packed8 load_packed8(const adahop_ckpt8_t &k, int64_t row, int c, int n)
+template <bool ODD = true> __device__ __forceinline__ packed8 load_packed8(const adahop_ckpt8_t &k, int64_t row, int c, int n)
 {
     packed8 p;
     const uint8_t *const at = k.codes + row * k.ld_codes + c;
-    if (n >= 8) {
+    if (!ODD || n >= 8) {
         p.codes = *reinterpret_cast<const u32x2 *>(at);
     } else {
         p.codes = 0;
