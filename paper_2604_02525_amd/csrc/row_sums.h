@@ -1,4 +1,4 @@
-// Sums over a workgroup that holds one row of a matrix: every thread gets them.
+// Sums over the waves of a workgroup that hold one row of a matrix: every thread of them gets them.
 #pragma once
 #include "common.h"
 
@@ -31,13 +31,13 @@ __device__ __forceinline__ float sum64(float v)
     return __uint_as_float(r.x) + __uint_as_float(r.y);
 }
 
-// The sums of N values over the workgroup's threads, in one order whatever the timing.  Two buffers in turn: a wave that writes into
+// The sums of N values over `waves` waves from `first` on, in one order whatever the timing; all waves of the workgroup take part, each for its row.  Two buffers in turn: a wave that writes into
 // one has passed the barrier of the sums in the other, which no wave reaches before it has read these ones' predecessors.
 template <int N> struct row_sums_t {
     float part[2][N][ROW_THREADS / 64];
 };
 
-template <int N> __device__ __forceinline__ void row_sums(row_sums_t<N> &lds, int &turn, int waves, float (&v)[N])
+template <int N> __device__ __forceinline__ void row_sums(row_sums_t<N> &lds, int &turn, int waves, float (&v)[N], int first = 0)
 {
 #pragma unroll
     for (int i = 0; i < N; ++i) v[i] = sum64(v[i]);
@@ -50,7 +50,7 @@ template <int N> __device__ __forceinline__ void row_sums(row_sums_t<N> &lds, in
     }
     __syncthreads();
 #pragma unroll
-    for (int i = 0; i < N; ++i) v[i] = sum16((lane & 15) < waves ? lds.part[turn][i][lane & 15] : 0.0f);
+    for (int i = 0; i < N; ++i) v[i] = sum16((lane & 15) < waves ? lds.part[turn][i][first + (lane & 15)] : 0.0f);
 }
 
 } // namespace
