@@ -5,9 +5,9 @@
 // on the BF16 matrix cores: an E4M3 element times its power of two is a bf16 number, so nothing is rounded on the way there.  The checkpoint is expanded
 // to bf16 rows in the workspace (3 bytes per element moved), then both operands are bf16.  For 28672 columns of G the expansion is 1.6 % of the time, for 4096
 // 8 %.  Converting in the product itself takes longer: codes converted once per workgroup, by way of LDS, took 6.4 ms at 16384 x 28672 x 8192
-// (writing 1024 bytes to LDS takes 13 cycles, reading them 4), in the registers of each wave that needs them 6.9 ms; this takes 5.35 ms.
+// (writing 1024 bytes to LDS takes 13 cycles, reading them 4), in the registers of each wave that needs them 6.9 ms; this takes 5.4 ms.
 //
-// Bound by the matrix cores and the power that they draw: the product runs at 1.45 PFLOP/s with the clock down to 1.78 GHz (2.4 GHz on operands of
+// Bound by the matrix cores and the power that they draw: the product runs at 1.44 PFLOP/s with the clock down to 1.78 GHz (2.4 GHz on operands of
 // zeros), a library product of operands that have the contraction contiguous at 1.58.  The 16 x 16 x 32 instructions draw less than those of 32 x 32 x 16
 // (alone, on random operands, 2.06 against 1.85 PFLOP/s).
 //
@@ -356,14 +356,16 @@ __global__ __launch_bounds__(256) void k_wgrad8_join(wgrad_t q, int slices)
 
 struct plan_t {
     bool large;     // tiles of 256 x 256, else 128 x 128
+    bool alone;     // one workgroup at most per compute unit
     int slices;
     int64_t slice, ldx;
     size_t part_at, bytes;
 };
 
 // Tile size and slices of the tokens by expected time, in microseconds, measured on 256 compute units.  A stage of a round of workgroups: 0.7 with the large
-// tiles, one workgroup per compute unit; with the small ones 0.5 where there are two per compute unit, 0.33 where there is one; a round's beginning and end
-// 4 and 2.5.  Slices cost their sums' way to memory and back and one launch more.  Both sides at 2048 x 2048, us: 1001 tokens, small tiles in one slice 23.6, in two 30.0,
+// tiles, one workgroup per compute unit; with the small ones 0.5 where there are two per compute unit, 0.3 where there is one; a round's beginning and end
+// 4 and 2.5.  Where no compute unit has two, small tiles have eight waves in place of four (two per SIMD in either case) and a longer ring: 1001
+// tokens of 2048 x 2048 in 21.3 us instead of 22.9, of 1024 x 2048 18.5 instead of 20.8; 4096 of 2048 x 4096, two per compute unit, 89 instead of 76.  Slices cost their sums' way to memory and back and one launch more.  Both sides at 2048 x 2048, us: 1001 tokens, small tiles in one slice 23.6, in two 30.0,
 // large ones in four 36.9; 8192 tokens, 92.0, 82.0 and 81.2; 4096 x 2048 at 4096 tokens, small 74.2, large in two slices 80.6; at 16384 tokens 245 and 225.
 plan_t plan_of(int64_t T, int64_t N, int64_t D)
 {
@@ -377,11 +379,12 @@ plan_t plan_of(int64_t T, int64_t N, int64_t D)
         const double join = number > 1 ? 6.0 + (double)number * N * D * 8 / 5e6 : 0.0;
         const int64_t rounds = small * number / 512, over = small * number % 512;
         const double in_large = ceil_div(large * number, 256) * (4.0 + 0.7 * each) + join;
-        const double in_small = (rounds + (over > 0)) * 2.5 + (rounds * 0.5 + (over > 256 ? 0.5 : over > 0 ? 0.33 : 0.0)) * each + join;
+        const double in_small = (rounds + (over > 0)) * 2.5 + (rounds * 0.5 + (over > 256 ? 0.5 : over > 0 ? 0.3 : 0.0)) * each + join;
         const double t = in_large < in_small ? in_large : in_small;
         if (p.slices == 0 || t < best) {
             best = t;
             p.large = in_large < in_small;
+            p.alone = small * number <= 256;
             p.slices = (int)number;
             p.slice = each * STAGE;
         }
@@ -397,6 +400,24 @@ device_once_t g_once;
 
 typedef tile_t<8, 4, 2, 4, 4> large_t;
 typedef tile_t<4, 4, 2, 2, 4> small_t;
+typedef tile_t<2, 4, 4, 2, 6> small_alone_t; // of the same tile
+
+// tile_t's kernel
+template <class K> struct kernel_of;
+template <int MT, int NT, int WN, int WD, int RING> struct kernel_of<tile_t<MT, NT, WN, WD, RING>> {
+    static int configure()
+    {
+        return check_hip(hipFuncSetAttribute(reinterpret_cast<const void *>(&k_wgrad8<MT, NT, WN, WD, RING>), hipFuncAttributeMaxDynamicSharedMemorySize,
+                                             tile_t<MT, NT, WN, WD, RING>::LDS));
+    }
+    static void launch(wgrad_t &q, int slices, hipStream_t st)
+    {
+        typedef tile_t<MT, NT, WN, WD, RING> K;
+        static_assert(K::WAVES * 32 * (16 * NT + 4) * sizeof(float) <= K::LDS, "the waves' patches fit");
+        q.nt = (uint32_t)ceil_div(q.N, K::TM), q.dt = (uint32_t)ceil_div(q.D, K::TN);
+        k_wgrad8<MT, NT, WN, WD, RING><<<dim3(q.nt * q.dt, slices), 64 * K::WAVES, K::LDS, st>>>(q);
+    }
+};
 
 } // namespace
 
@@ -405,9 +426,9 @@ int configure_wgrad8()
     int dev = 0;
     int rc = check_hip(hipGetDevice(&dev));
     if (rc != ADAHOP_OK || !g_once.need(dev)) return rc;
-    rc = check_hip(hipFuncSetAttribute(reinterpret_cast<const void *>(&k_wgrad8<8, 4, 2, 4, 4>), hipFuncAttributeMaxDynamicSharedMemorySize, large_t::LDS));
-    if (rc == ADAHOP_OK)
-        rc = check_hip(hipFuncSetAttribute(reinterpret_cast<const void *>(&k_wgrad8<4, 4, 2, 2, 4>), hipFuncAttributeMaxDynamicSharedMemorySize, small_t::LDS));
+    rc = kernel_of<large_t>::configure();
+    if (rc == ADAHOP_OK) rc = kernel_of<small_t>::configure();
+    if (rc == ADAHOP_OK) rc = kernel_of<small_alone_t>::configure();
     if (rc == ADAHOP_OK) g_once.mark(dev);
     return rc;
 }
@@ -425,13 +446,12 @@ int launch_wgrad8(int64_t T, int64_t N, int64_t D, const adahop_tensor_t &G, con
     float *const part = p.slices > 1 ? reinterpret_cast<float *>(static_cast<char *>(workspace) + p.part_at) : nullptr;
     wgrad_t q = {G, X, col_scale, add, C, T, N, D, part, p.slice, 0, 0};
     if (part) q.col_scale = q.add = {}; // the slices' sums come first
-    if (p.large) {
-        q.nt = (uint32_t)ceil_div(N, large_t::TM), q.dt = (uint32_t)ceil_div(D, large_t::TN);
-        k_wgrad8<8, 4, 2, 4, 4><<<dim3(q.nt * q.dt, p.slices), 64 * large_t::WAVES, large_t::LDS, st>>>(q);
-    } else {
-        q.nt = (uint32_t)ceil_div(N, small_t::TM), q.dt = (uint32_t)ceil_div(D, small_t::TN);
-        k_wgrad8<4, 4, 2, 2, 4><<<dim3(q.nt * q.dt, p.slices), 64 * small_t::WAVES, small_t::LDS, st>>>(q);
-    }
+    if (p.large)
+        kernel_of<large_t>::launch(q, p.slices, st);
+    else if (p.alone)
+        kernel_of<small_alone_t>::launch(q, p.slices, st);
+    else
+        kernel_of<small_t>::launch(q, p.slices, st);
     rc = check_launch();
     if (rc != ADAHOP_OK || !part) return rc;
     q.col_scale = col_scale, q.add = add;
