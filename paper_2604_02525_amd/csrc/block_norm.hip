@@ -4,8 +4,9 @@
 //     shat = s / sqrt(mean(s^2) + eps),   h = w_pre * shat
 //
 // in one pass: a workgroup holds a row in registers, eight consecutive elements per lane and piece, and sums its squares
-// twice.  Bound by the memory: x and y are read once, s, h and the 8-bit checkpoints of yhat and shat are written once.  The sums are in fp32; h and
-// the checkpoints are formed from s before its rounding to bf16, so that each output is rounded once.
+// twice.  Bound by the memory: x and y are read once, s, h and the 8-bit checkpoints of yhat and shat are written once; for a single row of 4096 by
+// its latency, 4.5 us of which some 2 are the launch.  The sums are in fp32; h and the checkpoints are formed from s before its rounding to bf16,
+// so that each output is rounded once.
 #include "ckpt8.h"
 #include "row_sums.h"
 
@@ -25,8 +26,8 @@ __device__ __forceinline__ float over_root(float m)
 
 // C: pieces of 8 columns per lane; ODD: the last one may be a part; SF32, YF32: the type of x and s, and of y.  The next
 // row's x and y are on their way while a row is summed.  Rows of whole pieces have kernels of their own, without the
-// paths for a part: 8192 x 4096 in 53.4 us instead of 56.5, 16384 x 8192 with both checkpoints in 243 us (5.55 TB/s)
-// instead of 248.
+// paths for a part: 8192 x 4096 in 53.4 us instead of 56.5, 16384 x 8192 with both checkpoints in 239 us (5.65 TB/s)
+// instead of 244.
 template <int C, bool ODD, bool SF32, bool YF32> __global__ __launch_bounds__(ROW_THREADS) void k_block_norm(adahop_block_norm_t q)
 {
     __shared__ row_sums_t<1> lds;

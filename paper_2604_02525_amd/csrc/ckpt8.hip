@@ -1,5 +1,7 @@
 // 8-bit activation checkpoints (packing, unpacking) and the gated activation a = silu(g) u that writes and reads them.
-// All four are elementwise but for the scale of 32 features: bound by the memory, one pass over it.
+// All four are elementwise but for the scale of 32 features: bound by the memory, one pass over it.  A lane has one piece of 8 elements (16-byte
+// accesses in bf16), four neighbouring lanes have a block of 32 and find its largest magnitude by two lane exchanges.  One piece per lane and very many
+// workgroups, not a loop: the hardware keeps the loads of thousands of waves on their way by itself.
 #include "ckpt8.h"
 
 namespace adahop {
@@ -24,6 +26,7 @@ __device__ __forceinline__ piece_t piece_of(const blocks_t &g, int cols, uint32_
     return p;
 }
 
+// 8192 x 4096 bf16: 17.4 us, 5.8 TB/s (the input of 67 MB lies in the 256 MB cache).
 template <bool F32> __global__ __launch_bounds__(PIECES) void k_ckpt8_pack(adahop_tensor_t x, adahop_ckpt8_t out, blocks_t g, int cols)
 {
     const piece_t p = piece_of(g, cols, blockIdx.x * PIECES + threadIdx.x);
@@ -33,6 +36,7 @@ template <bool F32> __global__ __launch_bounds__(PIECES) void k_ckpt8_pack(adaho
     if (p.n > 0) store_packed8(out, p.row, p.c, p.n, k);
 }
 
+// 16384 x 8192 to bf16: 68.8 us, 5.9 TB/s.
 template <bool F32> __global__ __launch_bounds__(PIECES) void k_ckpt8_unpack(adahop_ckpt8_t x, adahop_tensor_t scale, adahop_tensor_t out, blocks_t g, int cols)
 {
     const piece_t p = piece_of(g, cols, blockIdx.x * PIECES + threadIdx.x);
@@ -48,8 +52,10 @@ template <bool F32> __global__ __launch_bounds__(PIECES) void k_ckpt8_unpack(ada
     store8<F32>(out.data, p.row * out.ld + p.c, p.n, v);
 }
 
+// The exponential and the reciprocal as the hardware has them, each within two steps of fp32: far below the rounding to bf16 or to 8 bits that follows.
 __device__ __forceinline__ float sigmoid(float g) { return __builtin_amdgcn_rcpf(1.0f + __expf(-g)); }
 
+// 8192 x 11008 bf16 with both checkpoints: 122.5 us, 5.9 TB/s (127 before the codes went past the caches).
 template <bool F32> __global__ __launch_bounds__(PIECES) void k_swiglu(adahop_swiglu_t q, blocks_t b, int cols)
 {
     const piece_t p = piece_of(b, cols, blockIdx.x * PIECES + threadIdx.x);
@@ -69,7 +75,8 @@ template <bool F32> __global__ __launch_bounds__(PIECES) void k_swiglu(adahop_sw
     }
 }
 
-// silu'(g) = sigma + g sigma (1 - sigma)
+// silu'(g) = sigma + g sigma (1 - sigma).  8192 x 11008 from both checkpoints, a handed back in 8 bits: 137 us, 6.0 TB/s; 301 x 14333 from bf16, the gradient in
+// fp32: 12.6 us, 4.8 TB/s (no row but the first begins at a multiple of 16 bytes).
 template <bool KEPT, bool F32> __global__ __launch_bounds__(PIECES) void k_swiglu_backward(adahop_swiglu_t q, blocks_t b, int cols)
 {
     const piece_t p = piece_of(b, cols, blockIdx.x * PIECES + threadIdx.x);
