@@ -84,22 +84,29 @@ template <int FROM, int TO, class F> __device__ __forceinline__ void static_for(
     }
 }
 
-// C[r, c .. c + have) = v times scale, plus what is added.
-__device__ __forceinline__ void put4(const adahop_tensor_t &to, const adahop_tensor_t &add, int64_t r, int64_t c, int have, const float (&scale)[4], float4 v)
+// add[r, c .. c + have), zeros where there is none
+__device__ __forceinline__ float4 get4(const adahop_tensor_t &add, int64_t r, int64_t c, int have)
 {
-    float o[4] = {v.x * scale[0], v.y * scale[1], v.z * scale[2], v.w * scale[3]};
+    float o[4] = {};
     if (add.data) {
         const int64_t at = r * add.ld + c;
         if (have == 4 && add.f32) {
             const u32x4 a = *reinterpret_cast<const u32x4_e4 *>(static_cast<const uint32_t *>(add.data) + at);
 #pragma unroll
-            for (int i = 0; i < 4; ++i) o[i] += __uint_as_float(a[i]);
+            for (int i = 0; i < 4; ++i) o[i] = __uint_as_float(a[i]);
         } else {
 #pragma unroll
             for (int i = 0; i < 4; ++i)
-                if (i < have) o[i] += element(add, at + i);
+                if (i < have) o[i] = element(add, at + i);
         }
     }
+    return make_float4(o[0], o[1], o[2], o[3]);
+}
+
+// C[r, c .. c + have) = v times scale, plus more.
+__device__ __forceinline__ void put4(const adahop_tensor_t &to, int64_t r, int64_t c, int have, const float (&scale)[4], float4 v, float4 more)
+{
+    const float o[4] = {v.x * scale[0] + more.x, v.y * scale[1] + more.y, v.z * scale[2] + more.z, v.w * scale[3] + more.w};
     const int64_t at = r * to.ld + c;
     if (to.f32) {
         uint32_t *const p = static_cast<uint32_t *>(to.data) + at;
@@ -291,38 +298,53 @@ template <int MT, int NT, int WN, int WD, int RING> __global__ __launch_bounds__
     }
 
     // C, 32 rows of a wave at a time by way of its own patch of LDS, so that a lane has four consecutive columns of a row: 16-byte stores of
-    // whole rows, and little code.  In the accumulators a lane has column lane % 32 of a tile, rows 8 (i / 4) + 4 h + i % 4.
-    wait_for_copies<0>();
-    asm volatile("s_barrier" ::: "memory"); // no wave reads or copies any more
-    constexpr int PITCH = 16 * NT + 4, LANES = 4 * NT;
-    float *const patch = reinterpret_cast<float *>(smem) + w * 32 * PITCH;
+    // whole rows, and little code.  In the accumulators a lane has column lane % 16 of a tile, rows 4 (lane / 16) + i.  What is added is read 32 rows
+    // ahead: no load passes a store that it might depend on (8192 tokens of 4096 x 4096, added to: 228 us, without 238).
+    constexpr int PITCH = 16 * NT + 4, LANES = 4 * NT, STEPS = LANES / 2;
     const int c4 = lane % LANES * 4, r0 = lane / LANES;
     const int64_t c = d0 + wd * NT * 16 + c4;
     const int have = (int)(q.D - c < 4 ? q.D - c : 4);
+    const auto row_at = [&](int m, int i) { return n0 + (wn * MT + m) * 16 + r0 + i * (64 / LANES); };
     float scale[4] = {1.0f, 1.0f, 1.0f, 1.0f};
     if (q.col_scale.data) {
 #pragma unroll
         for (int i = 0; i < 4; ++i)
             if (i < have) scale[i] = element(q.col_scale, c + i);
     }
+    float *const patch = reinterpret_cast<float *>(smem) + w * 32 * PITCH;
     adahop_tensor_t result = q.C;
     if (q.part) result = {q.part + (int64_t)blockIdx.y * q.N * q.D, q.D, 1};
+    const auto finish = [&](auto adds) {
+        constexpr bool ADDS = decltype(adds)::value;
+        float4 more[2][STEPS];
+        const auto get = [&](int m) {
 #pragma unroll
-    for (int m = 0; m < MT; m += 2) {
-        lds_between_lanes();
+            for (int i = 0; i < STEPS; ++i)
+                more[m / 2 & 1][i] = have > 0 && row_at(m, i) < q.N ? get4(q.add, row_at(m, i), c, have) : make_float4(0.0f, 0.0f, 0.0f, 0.0f);
+        };
+        if constexpr (ADDS) get(0);
+        wait_for_copies<0>();
+        asm volatile("s_barrier" ::: "memory"); // no wave reads or copies any more
 #pragma unroll
-        for (int n = 0; n < NT; ++n)
+        for (int m = 0; m < MT; m += 2) {
+            lds_between_lanes();
 #pragma unroll
-            for (int i = 0; i < 8; ++i) patch[(16 * (i >> 2) + 4 * (lane >> 4) + (i & 3)) * PITCH + 16 * n + (lane & 15)] = acc[m + (i >> 2)][n][i & 3];
-        lds_between_lanes();
-        const int64_t first = n0 + (wn * MT + m) * 16 + r0;
-        if (have <= 0) continue;
-#pragma unroll 4
-        for (int i = 0; i < 32; i += 64 / LANES) {
-            const int64_t r = first + i;
-            if (r < q.N) put4(result, q.add, r, c, have, scale, *reinterpret_cast<const float4 *>(patch + (r0 + i) * PITCH + c4));
+            for (int n = 0; n < NT; ++n)
+#pragma unroll
+                for (int i = 0; i < 8; ++i) patch[(16 * (i >> 2) + 4 * (lane >> 4) + (i & 3)) * PITCH + 16 * n + (lane & 15)] = acc[m + (i >> 2)][n][i & 3];
+            lds_between_lanes();
+            if (have <= 0) continue;
+            if constexpr (ADDS) {
+                if (m + 2 < MT) get(m + 2);
+            }
+#pragma unroll(ADDS ? STEPS : 4)
+            for (int i = 0; i < STEPS; ++i)
+                if (row_at(m, i) < q.N)
+                    put4(result, row_at(m, i), c, have, scale, *reinterpret_cast<const float4 *>(patch + (r0 + i * (64 / LANES)) * PITCH + c4),
+                         ADDS ? more[m / 2 & 1][i] : make_float4(0.0f, 0.0f, 0.0f, 0.0f));
         }
-    }
+    };
+    q.add.data ? finish(std::true_type{}) : finish(std::false_type{});
 }
 
 // The sums of the slices, in their order, and what the kernel above does with a single one's.  A lane has four columns.
@@ -351,7 +373,7 @@ __global__ __launch_bounds__(256) void k_wgrad8_join(wgrad_t q, int slices)
         for (int i = 0; i < 4; ++i)
             if (i < have) scale[i] = element(q.col_scale, c + i);
     }
-    put4(q.C, q.add, r, c, have, scale, make_float4(v[0], v[1], v[2], v[3]));
+    put4(q.C, r, c, have, scale, make_float4(v[0], v[1], v[2], v[3]), get4(q.add, r, c, have));
 }
 
 struct plan_t {
