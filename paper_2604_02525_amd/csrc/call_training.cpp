@@ -210,9 +210,11 @@ struct workspace_t {
 
 PyObject *current_stream = nullptr; // a callable: the handle of torch's current stream
 
-// The handle that the caller has given, or None: the current stream's, asked for when the arguments have been checked.
-void *stream_of(PyObject *o)
+// The handle that the caller has given, or None: the current stream's, asked for when the arguments have been checked.  What the frame's tensors
+// hold has to be where a kernel can read it.
+void *stream_of(PyObject *o, const frame_t &f)
 {
+    if (!f.device.is_cuda()) refuse(PyExc_ValueError, "tensors on a GPU wanted, not on " + f.device.str());
     if (o != Py_None) return reinterpret_cast<void *>((uintptr_t)PyLong_AsUnsignedLongLongMask(o));
     const object_t handle(PyObject_CallNoArgs(current_stream));
     return reinterpret_cast<void *>((uintptr_t)PyLong_AsUnsignedLongLongMask(handle.p));
@@ -253,7 +255,7 @@ PyObject *pack(PyObject *, PyObject *const *v, Py_ssize_t n)
     const adahop_tensor_t x = matrix(v[0], f, "x");
     const object_t out(given_or(v[1], [&] { return empty_checkpoint(f); }));
     const adahop_ckpt8_t k = checkpoint(out.p, f, "out");
-    return answer(entry.pack(f.rows, f.cols, &x, &k, stream_of(v[2])), out.p);
+    return answer(entry.pack(f.rows, f.cols, &x, &k, stream_of(v[2], f)), out.p);
     END_HANDLE_TH_ERRORS
 }
 
@@ -267,7 +269,7 @@ PyObject *unpack(PyObject *, PyObject *const *v, Py_ssize_t n)
     const adahop_tensor_t scale = vector(v[1], f, "col_scale");
     const object_t out(given_or(v[2], [&] { return empty({f.rows, f.cols}, truth(v[3]) ? at::kFloat : at::kBFloat16, f); }));
     const adahop_tensor_t o = matrix(out.p, f, "out");
-    return answer(entry.unpack(f.rows, f.cols, &x, &scale, &o, stream_of(v[4])), out.p);
+    return answer(entry.unpack(f.rows, f.cols, &x, &scale, &o, stream_of(v[4], f)), out.p);
     END_HANDLE_TH_ERRORS
 }
 
@@ -284,7 +286,7 @@ PyObject *swiglu(PyObject *, PyObject *const *v, Py_ssize_t n)
     const object_t a(given_or(v[2], [&] { return empty({f.rows, f.cols}, at::kBFloat16, f); }));
     const object_t kg(given_or(v[3], [&] { return keep ? empty_checkpoint(f) : none(); })), ku(given_or(v[4], [&] { return keep ? empty_checkpoint(f) : none(); }));
     p.a = matrix(a.p, f, "a"), p.ckpt_g = checkpoint(kg.p, f, "ckpt_g"), p.ckpt_u = checkpoint(ku.p, f, "ckpt_u");
-    return answer(entry.swiglu(&p, stream_of(v[6])), {{name.a, a.p}, {name.ckpt_g, kg.p}, {name.ckpt_u, ku.p}});
+    return answer(entry.swiglu(&p, stream_of(v[6], f)), {{name.a, a.p}, {name.ckpt_g, kg.p}, {name.ckpt_u, ku.p}});
     END_HANDLE_TH_ERRORS
 }
 
@@ -313,7 +315,7 @@ PyObject *swiglu_backward(PyObject *, PyObject *const *v, Py_ssize_t n)
     const auto half = [&](int64_t from) { return both.defined() ? THPVariable_Wrap(both.narrow(1, from, f.cols)) : empty({f.rows, f.cols}, at::kBFloat16, f); };
     const object_t dg(given_or(v[3], [&] { return half(0); })), du(given_or(v[4], [&] { return half(f.cols); }));
     p.d_a = matrix(v[2], f, "d_a"), p.d_g = matrix(dg.p, f, "d_g"), p.d_u = matrix(du.p, f, "d_u");
-    return answer(entry.swiglu_backward(&p, stream_of(v[6])), {{name.d_g, dg.p}, {name.d_u, du.p}, {name.a, v[5]}});
+    return answer(entry.swiglu_backward(&p, stream_of(v[6], f)), {{name.d_g, dg.p}, {name.d_u, du.p}, {name.a, v[5]}});
     END_HANDLE_TH_ERRORS
 }
 
@@ -358,7 +360,7 @@ PyObject *block_norm(PyObject *, PyObject *const *v, Py_ssize_t n)
     p.h = matrix(h.p, f, "h");
     p.rstd_post = floats(r_post.p, f.rows, f, "rstd_post"), p.rstd_pre = floats(r_pre.p, f.rows, f, "rstd_pre");
     p.ckpt_y = checkpoint(ky.p, f, "ckpt_y"), p.ckpt_s = checkpoint(ks.p, f, "ckpt_s");
-    return answer(entry.norm(&p, stream_of(v[19])), {{name.s, s.p}, {name.h, h.p}, {name.rstd_post, r_post.p}, {name.rstd_pre, r_pre.p}, {name.ckpt_y, ky.p}, {name.ckpt_s, ks.p}});
+    return answer(entry.norm(&p, stream_of(v[19], f)), {{name.s, s.p}, {name.h, h.p}, {name.rstd_post, r_post.p}, {name.rstd_pre, r_pre.p}, {name.ckpt_y, ky.p}, {name.ckpt_s, ks.p}});
     END_HANDLE_TH_ERRORS
 }
 
@@ -397,7 +399,7 @@ PyObject *block_norm_backward(PyObject *, PyObject *const *v, Py_ssize_t n)
     p.d_w_post = floats(dwpost.p, f.cols, f, "d_w_post"), p.d_w_pre = floats(dwpre.p, f.cols, f, "d_w_pre");
     if (dgate.p != Py_None) p.d_gate = tensor_of(dgate.p, "d_gate").dim() == 1 ? vector(dgate.p, f, "d_gate") : matrix(dgate.p, f, p.gates, "d_gate");
     const workspace_t ws(v[18], entry.norm_backward_bytes(f.rows, f.cols, p.gate.data ? p.gate_rows : 0), f);
-    return answer(entry.norm_backward(&p, ws.data, ws.bytes, stream_of(v[19])),
+    return answer(entry.norm_backward(&p, ws.data, ws.bytes, stream_of(v[19], f)),
                   {{name.d_x, dx.p}, {name.d_y, dy.p}, {name.d_w_post, dwpost.p}, {name.d_w_pre, dwpre.p}, {name.d_gate, dgate.p}});
     END_HANDLE_TH_ERRORS
 }
@@ -415,7 +417,7 @@ PyObject *wgrad(PyObject *, PyObject *const *v, Py_ssize_t n)
     const object_t out(given_or(v[4], [&] { return empty({c.rows, c.cols}, truth(v[5]) ? at::kBFloat16 : at::kFloat, c); }));
     const adahop_tensor_t C = matrix(out.p, c, "Cout");
     const workspace_t ws(v[6], entry.wgrad_bytes(g.rows, g.cols, x.cols), g);
-    return answer(entry.wgrad(g.rows, g.cols, x.cols, &G, &k, &scale, &add, &C, ws.data, ws.bytes, stream_of(v[7])), out.p);
+    return answer(entry.wgrad(g.rows, g.cols, x.cols, &G, &k, &scale, &add, &C, ws.data, ws.bytes, stream_of(v[7], g)), out.p);
     END_HANDLE_TH_ERRORS
 }
 

@@ -212,3 +212,13 @@ def test_binding_refuses_shapes_and_types():
         ah.adahop_ckpt8_pack(x.to(torch.float64))
     with pytest.raises(ValueError):
         ah.adahop_block_norm_backward(x, y, x, y, torch.zeros(3), torch.zeros(4))
+
+
+def test_binding_refuses_tensors_in_host_memory():
+    x, r = torch.zeros(4, 64, dtype=torch.bfloat16), torch.zeros(4)
+    pair = ah.adahop_ckpt8_empty(4, 64, "cpu")
+    for call in (lambda: ah.adahop_ckpt8_pack(x), lambda: ah.adahop_ckpt8_unpack(pair), lambda: ah.adahop_swiglu(x, x),
+                 lambda: ah.adahop_swiglu_backward(x, x, x), lambda: ah.adahop_block_norm(x, x),
+                 lambda: ah.adahop_block_norm_backward(x, x, x, x, r, r), lambda: ah.adahop_ckpt8_wgrad(x, pair)):
+        with pytest.raises(ValueError, match="on a GPU"):
+            call()
