@@ -136,12 +136,13 @@ __device__ __forceinline__ void put4(const adahop_tensor_t &to, int64_t r, int64
 // most, too few for one to feed the matrix cores and LDS.
 //
 // A stage of both operands is copied to a ring of RING slots in LDS, RING - 1 stages ahead of its use.  A wave's operands of G are read again, for the
-// next stage, behind the last of the NT matrix instructions that use them, those of X into a second set of registers.  One barrier per stage, behind the
+// next stage, behind the last of the NT matrix instructions that use them, those of X into a second set of registers.  SPLIT = 2: two shares of such waves,
+// each with half of the tokens and a ring of its own, whose sums meet at the end.  One barrier per stage, behind the
 // first NT instructions: what is read after it has been copied by all waves, and nothing of the stage before is still to be read, so that its slot
 // is copied to, at the end of the stage (earlier: 2 % slower).
-template <int MT, int NT, int WN, int WD, int RING> struct tile_t {
-    static constexpr int WAVES = WN * WD, TM = 16 * WN * MT, TN = 16 * WD * NT, RA = 2 * TM, RB = 2 * TN; // columns; bytes of a row in LDS
-    static constexpr uint32_t A = STAGE * RA, B = STAGE * RB, SLOT = A + B, LDS = RING * SLOT;
+template <int MT, int NT, int WN, int WD, int RING, int SPLIT = 1> struct tile_t {
+    static constexpr int WAVES = WN * WD, THREADS = 64 * WAVES * SPLIT, TM = 16 * WN * MT, TN = 16 * WD * NT, RA = 2 * TM, RB = 2 * TN; // columns; bytes of a row in LDS
+    static constexpr uint32_t A = STAGE * RA, B = STAGE * RB, SLOT = A + B, LDS = SPLIT * RING * SLOT;
     static constexpr int COPIES_A = A / 1024 / WAVES, COPIES_B = B / 1024 / WAVES, ISSUED = COPIES_A + COPIES_B; // per wave and stage
     static __device__ __forceinline__ uint32_t turn_of(uint32_t row) { return (row & 3) | (row >> 1 & 4); }      // of the pieces of a row
     // What lane l of copy number `copy` of a stage reads: its row, and the byte in it
@@ -153,12 +154,13 @@ template <int MT, int NT, int WN, int WD, int RING> struct tile_t {
     }
 };
 
-template <int MT, int NT, int WN, int WD, int RING> __global__ __launch_bounds__(64 * WN * WD, 2) void k_wgrad8(wgrad_t q)
+template <int MT, int NT, int WN, int WD, int RING, int SPLIT> __global__ __launch_bounds__(64 * WN * WD * SPLIT, 2) void k_wgrad8(wgrad_t q)
 {
-    typedef tile_t<MT, NT, WN, WD, RING> K;
+    typedef tile_t<MT, NT, WN, WD, RING, SPLIT> K;
     extern __shared__ __attribute__((aligned(1024))) uint8_t smem[];
-    const int tid = threadIdx.x, lane = tid & 63, w = __builtin_amdgcn_readfirstlane(tid >> 6), wn = w / WD, wd = w % WD;
-    const uint32_t base = __builtin_amdgcn_readfirstlane(lds_address(smem));
+    const int tid = threadIdx.x, lane = tid & 63, wave = __builtin_amdgcn_readfirstlane(tid >> 6), share = SPLIT > 1 ? wave / K::WAVES : 0;
+    const int w = wave - share * K::WAVES, wn = w / WD, wd = w % WD;
+    const uint32_t base = __builtin_amdgcn_readfirstlane(lds_address(smem)) + share * RING * K::SLOT;
 
     // Workgroups go round the eight XCDs; each takes a run of tiles, which it walks in columns of four tiles: what runs on it at a time
     // shares few tiles of either operand.
@@ -166,7 +168,14 @@ template <int MT, int NT, int WN, int WD, int RING> __global__ __launch_bounds__
     const uint32_t t = xcd * per + (xcd < rest ? xcd : rest) + id / 8, group = t / (4 * q.dt), in = t - group * 4 * q.dt;
     const uint32_t high = q.nt - 4 * group < 4 ? q.nt - 4 * group : 4;
     const int64_t n0 = (int64_t)(4 * group + in % high) * K::TM, d0 = (int64_t)(in / high) * K::TN;
-    const int64_t begin = (int64_t)blockIdx.y * q.slice, end = begin + q.slice < q.T ? begin + q.slice : q.T;
+    int64_t begin = (int64_t)blockIdx.y * q.slice, end = begin + q.slice < q.T ? begin + q.slice : q.T;
+    int32_t left = (int32_t)(end - begin); // tokens from the stage at hand on, of the first share
+    if constexpr (SPLIT > 1) {             // this wave's share of them, whole pairs of stages; the last may have none
+        const int32_t each = (left + 2 * SPLIT * STAGE - 1) / (2 * SPLIT * STAGE) * (2 * STAGE);
+        begin += (int64_t)share * each;
+        end = begin + each < end ? begin + each : end < begin ? begin : end;
+        left = left < each ? left : each;
+    }
 
     // What this wave and this lane copy of a stage.
     const uint32_t lda = (uint32_t)(q.G.ld * 2), ldb = (uint32_t)(q.X.ld * 2);
@@ -190,8 +199,8 @@ template <int MT, int NT, int WN, int WD, int RING> __global__ __launch_bounds__
     const uint32_t bfull = extent(STAGE, ldb, (q.D - d0) * 2, K::RB), blast = extent(odd_rows, ldb, (q.D - d0) * 2, K::RB);
     rsrc_t from_a = resource(static_cast<const uint16_t *>(q.G.data) + begin * q.G.ld + n0, afull);
     rsrc_t from_b = resource(static_cast<const uint16_t *>(q.X.data) + begin * q.X.ld + d0, bfull);
-    int32_t ahead = (int32_t)(end - begin), left = ahead; // tokens from the stage that is copied next on, and from the one at hand on
-    uint32_t to = base, at = base;                        // slots: copied to next, read next
+    int32_t ahead = (int32_t)(end - begin); // tokens from the stage that is copied next on
+    uint32_t to = base, at = base;          // slots: copied to next, read next
     const auto after = [&](uint32_t slot) { return slot == base + (RING - 1) * K::SLOT ? base : slot + K::SLOT; };
     const auto forward = [](rsrc_t &r, uint32_t bytes) {
         const uint64_t p = ((uint64_t)r.y << 32 | r.x) + bytes;
@@ -311,22 +320,38 @@ template <int MT, int NT, int WN, int WD, int RING> __global__ __launch_bounds__
         for (int i = 0; i < 4; ++i)
             if (i < have) scale[i] = element(q.col_scale, c + i);
     }
-    float *const patch = reinterpret_cast<float *>(smem) + w * 32 * PITCH;
+    float *const patch = reinterpret_cast<float *>(smem) + wave * 32 * PITCH;
     adahop_tensor_t result = q.C;
     if (q.part) result = {q.part + (int64_t)blockIdx.y * q.N * q.D, q.D, 1};
-    const auto finish = [&](auto adds) {
+    const auto finish = [&](auto adds, auto from, auto till) { // the accumulators' rows `from` to `till`
         constexpr bool ADDS = decltype(adds)::value;
+        constexpr int FROM = decltype(from)::value, TILL = decltype(till)::value;
         float4 more[2][STEPS];
         const auto get = [&](int m) {
 #pragma unroll
             for (int i = 0; i < STEPS; ++i)
                 more[m / 2 & 1][i] = have > 0 && row_at(m, i) < q.N ? get4(q.add, row_at(m, i), c, have) : make_float4(0.0f, 0.0f, 0.0f, 0.0f);
         };
-        if constexpr (ADDS) get(0);
+        if constexpr (ADDS) get(FROM);
         wait_for_copies<0>();
         asm volatile("s_barrier" ::: "memory"); // no wave reads or copies any more
+        if constexpr (SPLIT > 1) {              // the other share's sums of these rows, for its sums of the other rows
+            constexpr int OTHER = FROM ? 0 : MT / 2;
+            v4f *const box = reinterpret_cast<v4f *>(smem) + w * 64 + lane;
+            const auto place = [&](int of, int m, int n) -> v4f & { return box[((of * MT / 2 + m) * NT + n) * K::WAVES * 64]; };
 #pragma unroll
-        for (int m = 0; m < MT; m += 2) {
+            for (int m = 0; m < MT / 2; ++m)
+#pragma unroll
+                for (int n = 0; n < NT; ++n) place(share, m, n) = acc[OTHER + m][n];
+            __syncthreads();
+#pragma unroll
+            for (int m = 0; m < MT / 2; ++m)
+#pragma unroll
+                for (int n = 0; n < NT; ++n) acc[FROM + m][n] += place(1 - share, m, n);
+            __syncthreads();
+        }
+#pragma unroll
+        for (int m = FROM; m < TILL; m += 2) {
             lds_between_lanes();
 #pragma unroll
             for (int n = 0; n < NT; ++n)
@@ -335,7 +360,7 @@ template <int MT, int NT, int WN, int WD, int RING> __global__ __launch_bounds__
             lds_between_lanes();
             if (have <= 0) continue;
             if constexpr (ADDS) {
-                if (m + 2 < MT) get(m + 2);
+                if (m + 2 < TILL) get(m + 2);
             }
 #pragma unroll(ADDS ? STEPS : 4)
             for (int i = 0; i < STEPS; ++i)
@@ -344,7 +369,16 @@ template <int MT, int NT, int WN, int WD, int RING> __global__ __launch_bounds__
                          ADDS ? more[m / 2 & 1][i] : make_float4(0.0f, 0.0f, 0.0f, 0.0f));
         }
     };
-    q.add.data ? finish(std::true_type{}) : finish(std::false_type{});
+    const auto finish_rows = [&](auto from, auto till) { q.add.data ? finish(std::true_type{}, from, till) : finish(std::false_type{}, from, till); };
+    if constexpr (SPLIT == 1) {
+        finish_rows(std::integral_constant<int, 0>{}, std::integral_constant<int, MT>{});
+    } else {
+        static_assert(SPLIT == 2 && MT % 4 == 0, "each share finishes half of the rows");
+        if (share == 0)
+            finish_rows(std::integral_constant<int, 0>{}, std::integral_constant<int, MT / 2>{});
+        else
+            finish_rows(std::integral_constant<int, MT / 2>{}, std::integral_constant<int, MT>{});
+    }
 }
 
 // The sums of the slices, in their order, and what the kernel above does with a single one's.  A lane has four columns.
@@ -386,8 +420,10 @@ struct plan_t {
 
 // Tile size and slices of the tokens by expected time, in microseconds, measured on 256 compute units.  A stage of a round of workgroups: 0.7 with the large
 // tiles, one workgroup per compute unit; with the small ones 0.5 where there are two per compute unit, 0.3 where there is one; a round's beginning and end
-// 4 and 2.5.  Where no compute unit has two, small tiles have eight waves in place of four (two per SIMD in either case) and a longer ring: 1001
-// tokens of 2048 x 2048 in 21.3 us instead of 22.9, of 1024 x 2048 18.5 instead of 20.8; 4096 of 2048 x 4096, two per compute unit, 89 instead of 76.  Slices cost their sums' way to memory and back and one launch more.  Both sides at 2048 x 2048, us: 1001 tokens, small tiles in one slice 23.6, in two 30.0,
+// 4 and 2.5.  Where no compute unit has two, a
+// workgroup of small tiles has two shares of four waves, each with half of the tokens: 1001 tokens of 2048 x 2048 in 20.4 us, one share 22.9 (eight waves on one tile, so with
+// half as many matrix instructions for an operand read, 21.2), 2048 tokens 29.4, one share 33; 4096 tokens of 2048 x 4096 are two workgroups per compute unit, 75.
+// Slices cost their sums' way to memory and back and one launch more.  Both sides at 2048 x 2048, us: 1001 tokens, small tiles in one slice 23.6, in two 30.0,
 // large ones in four 36.9; 8192 tokens, 92.0, 82.0 and 81.2; 4096 x 2048 at 4096 tokens, small 74.2, large in two slices 80.6; at 16384 tokens 245 and 225.
 plan_t plan_of(int64_t T, int64_t N, int64_t D)
 {
@@ -422,22 +458,22 @@ device_once_t g_once;
 
 typedef tile_t<8, 4, 2, 4, 4> large_t;
 typedef tile_t<4, 4, 2, 2, 4> small_t;
-typedef tile_t<2, 4, 4, 2, 6> small_alone_t; // of the same tile
+typedef tile_t<4, 4, 2, 2, 4, 2> small_alone_t;
 
 // tile_t's kernel
 template <class K> struct kernel_of;
-template <int MT, int NT, int WN, int WD, int RING> struct kernel_of<tile_t<MT, NT, WN, WD, RING>> {
+template <int MT, int NT, int WN, int WD, int RING, int SPLIT> struct kernel_of<tile_t<MT, NT, WN, WD, RING, SPLIT>> {
+    typedef tile_t<MT, NT, WN, WD, RING, SPLIT> K;
     static int configure()
     {
-        return check_hip(hipFuncSetAttribute(reinterpret_cast<const void *>(&k_wgrad8<MT, NT, WN, WD, RING>), hipFuncAttributeMaxDynamicSharedMemorySize,
-                                             tile_t<MT, NT, WN, WD, RING>::LDS));
+        return check_hip(hipFuncSetAttribute(reinterpret_cast<const void *>(&k_wgrad8<MT, NT, WN, WD, RING, SPLIT>), hipFuncAttributeMaxDynamicSharedMemorySize, K::LDS));
     }
     static void launch(wgrad_t &q, int slices, hipStream_t st)
     {
-        typedef tile_t<MT, NT, WN, WD, RING> K;
-        static_assert(K::WAVES * 32 * (16 * NT + 4) * sizeof(float) <= K::LDS, "the waves' patches fit");
+        static_assert(K::THREADS / 64 * 32 * (16 * NT + 4) * sizeof(float) <= K::LDS, "the waves' patches fit");
+        static_assert(SPLIT == 1 || 4 * K::TM * K::TN <= K::LDS, "the sums that the shares exchange fit");
         q.nt = (uint32_t)ceil_div(q.N, K::TM), q.dt = (uint32_t)ceil_div(q.D, K::TN);
-        k_wgrad8<MT, NT, WN, WD, RING><<<dim3(q.nt * q.dt, slices), 64 * K::WAVES, K::LDS, st>>>(q);
+        k_wgrad8<MT, NT, WN, WD, RING, SPLIT><<<dim3(q.nt * q.dt, slices), K::THREADS, K::LDS, st>>>(q);
     }
 };
 
