@@ -420,11 +420,12 @@ struct plan_t {
 
 // Tile size and slices of the tokens by expected time, in microseconds, measured on 256 compute units.  A stage of a round of workgroups: 0.7 with the large
 // tiles, one workgroup per compute unit; with the small ones 0.5 where there are two per compute unit, 0.3 where there is one; a round's beginning and end
-// 4 and 2.5.  Where no compute unit has two, a
-// workgroup of small tiles has two shares of four waves, each with half of the tokens: 1001 tokens of 2048 x 2048 in 20.4 us, one share 22.9 (eight waves on one tile, so with
-// half as many matrix instructions for an operand read, 21.2), 2048 tokens 29.4, one share 33; 4096 tokens of 2048 x 4096 are two workgroups per compute unit, 75.
-// Slices cost their sums' way to memory and back and one launch more.  Both sides at 2048 x 2048, us: 1001 tokens, small tiles in one slice 23.6, in two 30.0,
-// large ones in four 36.9; 8192 tokens, 92.0, 82.0 and 81.2; 4096 x 2048 at 4096 tokens, small 74.2, large in two slices 80.6; at 16384 tokens 245 and 225.
+// 4 and 2.5.  Slices cost their sums' way to memory and back and one launch more.  Both sides at 2048 x 2048, us: 1001 tokens, small tiles in one slice 20.4, in two
+// 28.3, large ones in four 36.4; 8192 tokens 72, 78 and 80, 16384 tokens 162, 174 and 132; 4096 tokens of 4096 x 2048, small 67, large in two slices 75, at 16384
+// tokens 308 and 220; 16384 tokens of 1024 x 1024, small in one, two and four slices 101, 63 and 49.
+//
+// Where no compute unit has two workgroups, one of small tiles has two shares of four waves, each with half of the tokens: 1001 tokens of 2048 x 2048 in 20.4 us, with one
+// share 22.9 (eight waves on one tile, with half as many matrix instructions for an operand read, 21.2), 2048 tokens 28.5, with one share 33.
 plan_t plan_of(int64_t T, int64_t N, int64_t D)
 {
     const int64_t stages = ceil_div(T, STAGE), large = ceil_div(N, 256) * ceil_div(D, 256), small = ceil_div(N, 128) * ceil_div(D, 128);
