@@ -47,8 +47,9 @@ template <int C, bool ODD, bool SF32, bool YF32> __global__ __launch_bounds__(RO
     const auto load_row = [&](int64_t row) {
 #pragma unroll
         for (int j = 0; j < C; ++j) {
-            x[j] = q.x.data && left(j) > 0 ? load8<SF32, ODD>(q.x.data, row * q.x.ld + col(j), left(j)) : zero8<SF32>();
-            y[j] = q.y.data && left(j) > 0 ? load8<YF32, ODD>(q.y.data, row * q.y.ld + col(j), left(j)) : zero8<YF32>();
+            const int n = to_load(left(j), row + 1 < q.rows, q.cols);
+            x[j] = q.x.data && n > 0 ? load8<SF32, ODD>(q.x.data, row * q.x.ld + col(j), n) : zero8<SF32>();
+            y[j] = q.y.data && n > 0 ? load8<YF32, ODD>(q.y.data, row * q.y.ld + col(j), n) : zero8<YF32>();
         }
     };
     const float over = 1.0f / (float)q.cols, rest = __builtin_fmaf(-over, (float)q.cols, 1.0f) * over; // together 1 / cols
@@ -64,7 +65,8 @@ template <int C, bool ODD, bool SF32, bool YF32> __global__ __launch_bounds__(RO
 #pragma unroll
             for (int j = 0; j < C; ++j) {
                 float g[8] = {1.0f, 1.0f, 1.0f, 1.0f, 1.0f, 1.0f, 1.0f, 1.0f}, w[8] = {1.0f, 1.0f, 1.0f, 1.0f, 1.0f, 1.0f, 1.0f, 1.0f};
-                if (q.gate.data && left(j) > 0) load8_any<ODD>(q.gate, gate_row * q.gate.ld + col(j), left(j), g);
+                const int n = to_load(left(j), gate_row + 1 < q.gates, q.cols);
+                if (q.gate.data && n > 0) load8_any<ODD>(q.gate, gate_row * q.gate.ld + col(j), n, g);
                 if (q.w_post.data && left(j) > 0) load8_any<ODD>(q.w_post, col(j), left(j), w);
 #pragma unroll
                 for (int i = 0; i < 8; ++i) wbranch[j][i] = q.branch_scale * w[i] * g[i];
@@ -74,6 +76,7 @@ template <int C, bool ODD, bool SF32, bool YF32> __global__ __launch_bounds__(RO
         for (int j = 0; j < C; ++j) {
             widen8(x[j], z[j]);
             widen8(y[j], v[j]);
+            if (ODD && left(j) < 8) zero_from(left(j), v[j]);
         }
         if (row + gridDim.x < q.rows) load_row(row + gridDim.x);
         if (q.post_norm) {
@@ -101,10 +104,10 @@ template <int C, bool ODD, bool SF32, bool YF32> __global__ __launch_bounds__(RO
 #pragma unroll
         for (int j = 0; j < C; ++j) {
 #pragma unroll
-            for (int i = 0; i < 8; ++i) {
-                z[j][i] = alpha * z[j][i] + v[j][i] * wbranch[j][i];
-                sum[0] = __builtin_fmaf(z[j][i], z[j][i], sum[0]);
-            }
+            for (int i = 0; i < 8; ++i) z[j][i] = alpha * z[j][i] + v[j][i] * wbranch[j][i];
+            if (ODD && left(j) < 8) zero_from(left(j), z[j]);
+#pragma unroll
+            for (int i = 0; i < 8; ++i) sum[0] = __builtin_fmaf(z[j][i], z[j][i], sum[0]);
             if (q.s.data && left(j) > 0) store8<SF32, ODD>(q.s.data, row * q.s.ld + col(j), left(j), z[j]);
         }
         if (!q.h.data) continue;

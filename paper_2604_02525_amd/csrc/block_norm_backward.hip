@@ -85,12 +85,12 @@ template <bool F32> struct saved8<true, F32> {
     packed8 r;
 };
 
-template <bool KEPT, bool F32> __device__ __forceinline__ void load_saved(saved8<KEPT, F32> &o, const adahop_ckpt8_t &k, const adahop_tensor_t &t, int64_t row, int c, int n)
+template <bool ODD, bool KEPT, bool F32> __device__ __forceinline__ void load_saved(saved8<KEPT, F32> &o, const adahop_ckpt8_t &k, const adahop_tensor_t &t, int64_t row, int c, int n)
 {
     if constexpr (KEPT)
-        o.r = load_packed8(k, row, c, n);
+        o.r = load_packed8<ODD>(k, row, c, n);
     else
-        o.r = load8<F32>(t.data, row * t.ld + c, n);
+        o.r = load8<F32, ODD>(t.data, row * t.ld + c, n);
 }
 
 template <bool KEPT, bool F32> __device__ __forceinline__ void none(saved8<KEPT, F32> &o)
@@ -115,25 +115,26 @@ template <bool KEPT, bool F32> __device__ __forceinline__ void widen_saved(const
 }
 
 // v = t's eight elements from `at` on, n of which exist; ones where there is no t.
-__device__ __forceinline__ void vector_of(const adahop_tensor_t &t, int64_t at, int n, float (&v)[8])
+template <bool ODD> __device__ __forceinline__ void vector_of(const adahop_tensor_t &t, int64_t at, int n, float (&v)[8])
 {
 #pragma unroll
     for (int i = 0; i < 8; ++i) v[i] = 1.0f;
-    if (t.data && n > 0) load8_any(t, at, n, v);
+    if (t.data && n > 0) load8_any<ODD>(t, at, n, v);
 }
 
 // v = beta gate w_post at column c
-__device__ __forceinline__ void branch_of(const adahop_block_norm_t &q, int64_t gate_row, int c, int n, float (&v)[8])
+template <bool ODD> __device__ __forceinline__ void branch_of(const adahop_block_norm_t &q, int64_t gate_row, int c, int n, float (&v)[8])
 {
     float g[8];
-    vector_of(q.gate, gate_row * q.gate.ld + c, n, g);
-    vector_of(q.w_post, c, n, v);
+    vector_of<ODD>(q.gate, gate_row * q.gate.ld + c, to_load(n, gate_row + 1 < q.gates, q.cols), g);
+    vector_of<ODD>(q.w_post, c, n, v);
 #pragma unroll
     for (int i = 0; i < 8; ++i) v[i] *= q.branch_scale * g[i];
+    if (ODD && n < 8) zero_from(n, v);
 }
 
 // What a lane reads of a row.
-template <bool KEPT, bool SF32, bool YF32> struct piece_t {
+template <bool ODD, bool KEPT, bool SF32, bool YF32> struct piece_t {
     raw8<SF32> ds;
     raw8<YF32> dh;
     saved8<KEPT, SF32> s;
@@ -141,21 +142,23 @@ template <bool KEPT, bool SF32, bool YF32> struct piece_t {
 
     __device__ __forceinline__ void load(const adahop_block_norm_t &q, int64_t row, int c, int n)
     {
-        ds = q.d_s.data && n > 0 ? load8<SF32>(q.d_s.data, row * q.d_s.ld + c, n) : zero8<SF32>();
-        dh = q.d_h.data && n > 0 ? load8<YF32>(q.d_h.data, row * q.d_h.ld + c, n) : zero8<YF32>();
+        n = to_load(n, row + 1 < q.rows, q.cols);
+        ds = q.d_s.data && n > 0 ? load8<SF32, ODD>(q.d_s.data, row * q.d_s.ld + c, n) : zero8<SF32>();
+        dh = q.d_h.data && n > 0 ? load8<YF32, ODD>(q.d_h.data, row * q.d_h.ld + c, n) : zero8<YF32>();
         none(s);
         none(y);
-        if (q.d_h.data && n > 0) load_saved(s, q.ckpt_s, q.s, row, c, n);
-        if ((KEPT ? q.ckpt_y.codes != nullptr : q.y.data != nullptr) && n > 0) load_saved(y, q.ckpt_y, q.y, row, c, n);
+        if (q.d_h.data && n > 0) load_saved<ODD>(s, q.ckpt_s, q.s, row, c, n);
+        if ((KEPT ? q.ckpt_y.codes != nullptr : q.y.data != nullptr) && n > 0) load_saved<ODD>(y, q.ckpt_y, q.y, row, c, n);
     }
-    // The piece's share of the three sums.
-    __device__ __forceinline__ void add(float rs, float ry, const float (&wpre)[8], const float (&wbranch)[8], float (&sum)[3]) const
+    // The share in the three sums of the n elements that exist.
+    __device__ __forceinline__ void add(int n, float rs, float ry, const float (&wpre)[8], const float (&wbranch)[8], float (&sum)[3]) const
     {
         float d[8], t[8], shat[8], yhat[8];
         widen8(ds, d);
         widen8(dh, t);
         widen_saved(s, rs, shat);
         widen_saved(y, ry, yhat);
+        if (ODD && n < 8) zero_from(n, d), zero_from(n, t), zero_from(n, shat), zero_from(n, yhat);
 #pragma unroll
         for (int i = 0; i < 8; ++i) {
             t[i] *= wpre[i];
@@ -187,29 +190,33 @@ template <bool KEPT, bool SF32, bool YF32> __global__ __launch_bounds__(ROW_THRE
 #pragma unroll 1
         for (int c = threadIdx.x * 8; c < (int)q.cols; c += 8 * ROW_THREADS) {
             const int n = (int)q.cols - c;
-            piece_t<KEPT, SF32, YF32> p;
+            constexpr bool ODD = true;
+            piece_t<ODD, KEPT, SF32, YF32> p;
             float wpre[8], wbranch[8];
             p.load(q, row, c, n);
-            vector_of(q.w_pre, c, n, wpre);
-            branch_of(q, gate_row, c, n, wbranch);
-            p.add(rs, ry, wpre, wbranch, sum);
+            vector_of<ODD>(q.w_pre, c, n, wpre);
+            branch_of<ODD>(q, gate_row, c, n, wbranch);
+            p.add(n, rs, ry, wpre, wbranch, sum);
         }
         row_sums(lds, turn, ROW_THREADS / 64, sum);
         if (threadIdx.x == 0) means[row] = means_of(q, rs, sum);
     }
 }
 
-// BESIDE: several runs per workgroup; STRIPS: rows wider than a workgroup, whose means are there already: blockIdx.y is the strip; SF32: ds, dx
+// BESIDE: several runs per workgroup; STRIPS: rows wider than a workgroup, whose means are there already: blockIdx.y is the strip; ODD: a row's last piece may
+// be a part (whole pieces without the paths for a part: 8192 x 4096 with token gates 119 us instead of
+// 128, 8192 x 2048 66 instead of 75); SF32: ds, dx
 // and a saved s are fp32; YF32: dh, dy and a saved y are.
 //
 // One accumulator serves both the gate and w_post: with A = sum(beta d yhat) over rows of one gate row, its gate gradient is w_post A and its part of
 // w_post's is gate A.  CUT: all rows of the run are of one gate row.  The row's values stay as they were loaded over the barrier and are widened again behind it
-// (half the registers).  The next row is loaded meanwhile unless the saved tensors are fp32.
-template <bool BESIDE, bool STRIPS, bool KEPT, bool CUT, bool SF32, bool YF32> __global__ __launch_bounds__(ROW_THREADS) void k_block_norm_backward(backward_t b)
+// (half the registers).  The next row is loaded meanwhile if its registers are to be had: 8192 x 4096 with token gates, the stream in fp32 and 8-bit checkpoints, took 174 us
+// with the next row and spills, 140 without.
+template <bool BESIDE, bool STRIPS, bool ODD, bool KEPT, bool CUT, bool SF32, bool YF32> __global__ __launch_bounds__(ROW_THREADS) void k_block_norm_backward(backward_t b)
 {
     // registers that a row takes as it lies in memory: two rows at a time where that leaves enough for the rest
     constexpr int RAW = (SF32 ? 8 : 4) + (YF32 ? 8 : 4) + (KEPT ? 6 : (SF32 ? 8 : 4) + (YF32 ? 8 : 4));
-    constexpr bool AHEAD = RAW <= 22;
+    constexpr bool AHEAD = RAW <= (CUT ? 22 : 16);
     __shared__ row_sums_t<3> lds;
     __shared__ float patch[BESIDE ? 8 * ROW_THREADS : 1];
     const adahop_block_norm_t &q = b.q;
@@ -219,7 +226,7 @@ template <bool BESIDE, bool STRIPS, bool KEPT, bool CUT, bool SF32, bool YF32> _
     float wbranch[8], wpre[8], apre[8], apost[8], agate[8]; // agate: A of the gate row at hand
 #pragma unroll
     for (int i = 0; i < 8; ++i) apre[i] = apost[i] = agate[i] = 0.0f;
-    vector_of(q.w_pre, col, left, wpre);
+    vector_of<ODD>(q.w_pre, col, left, wpre);
     const int64_t run = BESIDE ? (int64_t)blockIdx.x * b.runs.beside + sub : blockIdx.x;
     int64_t row = run * b.runs.rows, end = row + b.runs.rows;
     if constexpr (CUT) {
@@ -230,7 +237,7 @@ template <bool BESIDE, bool STRIPS, bool KEPT, bool CUT, bool SF32, bool YF32> _
     if (end > q.rows) end = q.rows;
     const bool any = row < end; // or there is no such run
     const int64_t fewer = b.runs.rows - (any ? end - row : 0); // rows than other runs of the workgroup may have
-    piece_t<KEPT, SF32, YF32> next;
+    piece_t<ODD, KEPT, SF32, YF32> next;
     float rs = 0.0f, ry = 1.0f;
     const auto load_row = [&](int64_t r) {
         if (q.d_h.data) rs = q.rstd_pre[r];
@@ -243,11 +250,11 @@ template <bool BESIDE, bool STRIPS, bool KEPT, bool CUT, bool SF32, bool YF32> _
         if (row >= gate_until) {
             gate_row = q.gate.data ? row / q.gate_rows : 0;
             gate_until = q.gate.data ? (gate_row + 1) * q.gate_rows : end;
-            branch_of(q, gate_row, col, left, wbranch);
+            branch_of<ODD>(q, gate_row, col, left, wbranch);
         }
         float sum[3] = {0.0f, 0.0f, 0.0f};
-        if constexpr (!STRIPS) next.add(rs, ry, wpre, wbranch, sum);
-        piece_t<KEPT, SF32, YF32> at = next;
+        if constexpr (!STRIPS) next.add(left, rs, ry, wpre, wbranch, sum);
+        piece_t<ODD, KEPT, SF32, YF32> at = next;
         keep_raw(at.ds), keep_raw(at.dh), keep_raw(at.s.r), keep_raw(at.y.r);
         const float rs0 = rs, ry0 = ry;
         if constexpr (AHEAD) {
@@ -274,22 +281,22 @@ template <bool BESIDE, bool STRIPS, bool KEPT, bool CUT, bool SF32, bool YF32> _
             agate[i] = __builtin_fmaf(q.branch_scale * d[i], yhat[i], agate[i]);
         }
         if (left > 0) {
-            if (q.d_x.data) store8<SF32>(q.d_x.data, row * q.d_x.ld + col, left, dx);
-            if (q.d_y.data) store8<YF32>(q.d_y.data, row * q.d_y.ld + col, left, dy);
+            if (q.d_x.data) store8<SF32, ODD>(q.d_x.data, row * q.d_x.ld + col, left, dx);
+            if (q.d_y.data) store8<YF32, ODD>(q.d_y.data, row * q.d_y.ld + col, left, dy);
         }
         ++row;
         if constexpr (!CUT) {
             if (row == end || row == gate_until) { // the gate row is complete
                 float g[8], w[8];
-                vector_of(q.gate, gate_row * q.gate.ld + col, left, g);
-                vector_of(q.w_post, col, left, w);
+                vector_of<ODD>(q.gate, gate_row * q.gate.ld + col, to_load(left, gate_row + 1 < q.gates, q.cols), g);
+                vector_of<ODD>(q.w_post, col, left, w);
 #pragma unroll
                 for (int i = 0; i < 8; ++i) {
                     apost[i] = __builtin_fmaf(agate[i], g[i], apost[i]);
                     w[i] *= agate[i];
                     agate[i] = 0.0f;
                 }
-                if (q.d_gate.data && left > 0) store8_any(q.d_gate, gate_row * q.d_gate.ld + col, left, w);
+                if (q.d_gate.data && left > 0) store8_any<ODD>(q.d_gate, gate_row * q.d_gate.ld + col, left, w);
             }
         }
         if constexpr (!AHEAD) {
@@ -303,9 +310,9 @@ template <bool BESIDE, bool STRIPS, bool KEPT, bool CUT, bool SF32, bool YF32> _
         if constexpr (!BESIDE) {
             if (left <= 0) return;
             if (to)
-                store8<true>(to, col, left, v);
+                store8<true, ODD>(to, col, left, v);
             else
-                store8_any(q.d_gate, col, left, v);
+                store8_any<ODD>(q.d_gate, col, left, v);
         } else {
             __syncthreads(); // no wave reads the one before any more
             float4 *const mine = reinterpret_cast<float4 *>(patch + 8 * threadIdx.x);
@@ -328,15 +335,15 @@ template <bool BESIDE, bool STRIPS, bool KEPT, bool CUT, bool SF32, bool YF32> _
     if constexpr (CUT) {
         float v[8];
         if (q.d_gate.data) {
-            vector_of(q.w_post, col, left, v);
+            vector_of<ODD>(q.w_post, col, left, v);
 #pragma unroll
             for (int i = 0; i < 8; ++i) v[i] = any ? v[i] * agate[i] : 0.0f;
             if (!BESIDE || b.runs.joined)
                 hand_over(v, part ? part + 2 * one : nullptr);
             else if (run < b.runs.number && left > 0)
-                store8<true>(b.part + 2 * one, run * q.cols + col, left, v);
+                store8<true, ODD>(b.part + 2 * one, run * q.cols + col, left, v);
         }
-        vector_of(q.gate, gate_row * q.gate.ld + col, left, v);
+        vector_of<ODD>(q.gate, gate_row * q.gate.ld + col, left, v);
 #pragma unroll
         for (int i = 0; i < 8; ++i) apost[i] = any ? v[i] * agate[i] : 0.0f;
     }
@@ -394,31 +401,31 @@ __global__ __launch_bounds__(256) void k_block_norm_zero(adahop_block_norm_t q, 
     for (int64_t g = from + blockIdx.y; g < q.gates; g += gridDim.y) put(q.d_gate, g * q.d_gate.ld + c, 0.0f);
 }
 
-int zero_from(const adahop_block_norm_t &q, int64_t from, hipStream_t st)
+int zero_gates_from(const adahop_block_norm_t &q, int64_t from, hipStream_t st)
 {
     const int64_t gates = q.d_gate.data ? q.gates - from : 0;
     k_block_norm_zero<<<dim3((unsigned)ceil_div(q.cols, 256), (unsigned)(gates < 1 ? 1 : gates > 1024 ? 1024 : gates)), 256, 0, st>>>(q, from);
     return check_launch();
 }
 
-template <bool BESIDE, bool STRIPS, bool KEPT, bool CUT> void launch(const backward_t &b, bool s32, bool y32, hipStream_t st)
+template <bool BESIDE, bool STRIPS, bool ODD, bool KEPT, bool CUT> void launch(const backward_t &b, bool s32, bool y32, hipStream_t st)
 {
     const dim3 n((unsigned)b.workgroups, (unsigned)strips_of(b.q.cols));
     const unsigned threads = b.threads * b.runs.beside;
     if (s32)
-        y32 ? k_block_norm_backward<BESIDE, STRIPS, KEPT, CUT, true, true><<<n, threads, 0, st>>>(b)
-            : k_block_norm_backward<BESIDE, STRIPS, KEPT, CUT, true, false><<<n, threads, 0, st>>>(b);
+        y32 ? k_block_norm_backward<BESIDE, STRIPS, ODD, KEPT, CUT, true, true><<<n, threads, 0, st>>>(b)
+            : k_block_norm_backward<BESIDE, STRIPS, ODD, KEPT, CUT, true, false><<<n, threads, 0, st>>>(b);
     else
-        y32 ? k_block_norm_backward<BESIDE, STRIPS, KEPT, CUT, false, true><<<n, threads, 0, st>>>(b)
-            : k_block_norm_backward<BESIDE, STRIPS, KEPT, CUT, false, false><<<n, threads, 0, st>>>(b);
+        y32 ? k_block_norm_backward<BESIDE, STRIPS, ODD, KEPT, CUT, false, true><<<n, threads, 0, st>>>(b)
+            : k_block_norm_backward<BESIDE, STRIPS, ODD, KEPT, CUT, false, false><<<n, threads, 0, st>>>(b);
 }
 
-template <bool BESIDE, bool STRIPS> void launch(const backward_t &b, bool s32, bool y32, bool kept, hipStream_t st)
+template <bool BESIDE, bool STRIPS, bool ODD> void launch(const backward_t &b, bool s32, bool y32, bool kept, hipStream_t st)
 {
     if (kept)
-        b.runs.cuts ? launch<BESIDE, STRIPS, true, true>(b, s32, y32, st) : launch<BESIDE, STRIPS, true, false>(b, s32, y32, st);
+        b.runs.cuts ? launch<BESIDE, STRIPS, ODD, true, true>(b, s32, y32, st) : launch<BESIDE, STRIPS, ODD, true, false>(b, s32, y32, st);
     else
-        b.runs.cuts ? launch<BESIDE, STRIPS, false, true>(b, s32, y32, st) : launch<BESIDE, STRIPS, false, false>(b, s32, y32, st);
+        b.runs.cuts ? launch<BESIDE, STRIPS, ODD, false, true>(b, s32, y32, st) : launch<BESIDE, STRIPS, ODD, false, false>(b, s32, y32, st);
 }
 
 template <bool KEPT> void launch_means(const adahop_block_norm_t &q, float2 *means, bool s32, bool y32, hipStream_t st)
@@ -444,7 +451,7 @@ size_t block_norm_backward_workspace_bytes(int64_t rows, int64_t cols, int64_t g
     return means_bytes(rows, cols) + (one_workgroup(r) ? 0 : (size_t)(2 * r.workgroups() + r.gate_parts()) * cols * sizeof(float));
 }
 
-int launch_block_norm_no_rows(const adahop_block_norm_t &q, hipStream_t st) { return zero_from(q, 0, st); }
+int launch_block_norm_no_rows(const adahop_block_norm_t &q, hipStream_t st) { return zero_gates_from(q, 0, st); }
 
 int launch_block_norm_backward(const adahop_block_norm_t &q, bool s32, bool y32, bool kept, void *workspace, hipStream_t st)
 {
@@ -456,12 +463,14 @@ int launch_block_norm_backward(const adahop_block_norm_t &q, bool s32, bool y32,
         kept ? launch_means<true>(q, means, s32, y32, st) : launch_means<false>(q, means, s32, y32, st);
         const int rc = check_launch();
         if (rc != ADAHOP_OK) return rc;
-        launch<false, true>(b, s32, y32, kept, st);
+        launch<false, true, true>(b, s32, y32, kept, st);
+    } else if (r.beside > 1) {
+        q.cols % 8 ? launch<true, false, true>(b, s32, y32, kept, st) : launch<true, false, false>(b, s32, y32, kept, st);
     } else {
-        r.beside > 1 ? launch<true, false>(b, s32, y32, kept, st) : launch<false, false>(b, s32, y32, kept, st);
+        q.cols % 8 ? launch<false, false, true>(b, s32, y32, kept, st) : launch<false, false, false>(b, s32, y32, kept, st);
     }
     int rc = check_launch();
-    if (rc == ADAHOP_OK && q.d_gate.data && q.gates > ceil_div(q.rows, q.gate_rows)) rc = zero_from(q, ceil_div(q.rows, q.gate_rows), st);
+    if (rc == ADAHOP_OK && q.d_gate.data && q.gates > ceil_div(q.rows, q.gate_rows)) rc = zero_gates_from(q, ceil_div(q.rows, q.gate_rows), st);
     if (rc != ADAHOP_OK || !b.part) return rc;
     const int64_t gates = q.d_gate.data && b.runs.cuts ? ceil_div(q.rows, b.runs.group) : 0;
     if (!q.d_w_pre && !q.d_w_post && !gates) return ADAHOP_OK;

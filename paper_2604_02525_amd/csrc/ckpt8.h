@@ -69,6 +69,18 @@ template <bool F32> __device__ __forceinline__ void widen8(const raw8<F32> &r, f
     }
 }
 
+// How many elements to load of a row's last piece, of which n exist: where another row of the tensor follows, all eight can be read at once and
+// those from n on be taken out later.  Element by element the loads of that piece keep the whole workgroup waiting: 8192 x 4091 with both
+// checkpoints forward 109 us instead of 91, backward 123 instead of 88.
+__device__ __forceinline__ int to_load(int n, bool row_follows, int64_t cols) { return row_follows && cols >= 8 && n > 0 ? 8 : n; }
+
+// Values from the n-th of eight on are zero, whatever they were.
+__device__ __forceinline__ void zero_from(int n, float (&v)[8])
+{
+#pragma unroll
+    for (int i = 0; i < 8; ++i) v[i] = i < n ? v[i] : 0.0f;
+}
+
 // Keeps eight elements as they lie in memory: what has been made of them so far is not kept in registers for later.
 template <bool F32> __device__ __forceinline__ void keep_raw(raw8<F32> &r)
 {
