@@ -12,7 +12,7 @@
 // weight gradients in registers.  At the end its runs are added up by way of LDS and go to the workspace, and k_block_norm_reduce adds the
 // workgroups' parts up, all in one order: the same bits every time.  Bound by the memory: 16384 x 8192 from 8-bit checkpoints takes 256 to 272 us in
 // all, 5.0 to 5.3 TB/s; 16384 x 4096 148 us (two workgroups per compute unit, 17 MB of parts to the workspace and back); 777 x 4091 with a gate for
-// every row, the residual stream in fp32, 28.5 us: two rows one after the other, each waiting for its loads.
+// every row, the residual stream in fp32, 27.2 us: two rows one after the other, each waiting for its loads.
 #include "ckpt8.h"
 #include "row_sums.h"
 
