@@ -362,7 +362,8 @@ int adahop_swiglu_backward(const adahop_swiglu_t *p, void *stream);
  *   yhat = y / sqrt(mean(y^2) + eps)            (post_norm = 0: yhat = y)
  *   s    = residual_scale x + branch_scale gate * w_post * yhat
  *   shat = s / sqrt(mean(s^2) + eps),  h = w_pre * shat
- * with the means over a row.
+ * with the means over a row.  Where a row's sum of squares is infinite (an infinity in the row, or squares beyond fp32), the factor 1 / sqrt(...) is
+ * 0, as in fp32 arithmetic: the row's finite elements become 0 under that norm, its infinities NaN.
  *   forward   x absent: s is the branch alone; y absent (post_norm = 0, no gate): s = residual_scale x, as before the
  *             first block.  s absent: not stored; h absent: no second norm.  w_post, w_pre, gate absent: 1.
  *             gate: row r of the operand takes gate row r / gate_rows of `gates` (gates * gate_rows >= rows): one

@@ -21,7 +21,7 @@ __device__ __forceinline__ float over_root(float m)
 {
     const float r = 1.0f / sqrtf(m), p = m * r;
     const float e = __builtin_fmaf(-__builtin_fmaf(m, r, -p), r, __builtin_fmaf(-p, r, 1.0f));
-    return fabsf(e) < 1.0f ? __builtin_fmaf(0.5f * r, e, r) : r; // 0, infinity and NaN as they are
+    return fabsf(e) < 1.0f ? __builtin_fmaf(0.5f * r, e, r) : r; // of an infinity 0, of NaN NaN
 }
 
 // C: pieces of 8 columns per lane; ODD: the last one may be a part; SF32, YF32: the type of x and s, and of y.  The next
@@ -53,7 +53,8 @@ template <int C, bool ODD, bool SF32, bool YF32> __global__ __launch_bounds__(RO
         }
     };
     const float over = 1.0f / (float)q.cols, rest = __builtin_fmaf(-over, (float)q.cols, 1.0f) * over; // together 1 / cols
-    const auto rstd = [&](float squares) { return over_root(__builtin_fmaf(squares, over, __builtin_fmaf(squares, rest, q.eps))); };
+    // An infinite sum (an infinity in the row, or squares past fp32) takes part in the larger of the two products alone: `rest` is 0 or negative at most widths.
+    const auto rstd = [&](float squares) { return over_root(__builtin_fmaf(squares, over, squares < INFINITY ? __builtin_fmaf(squares, rest, q.eps) : q.eps)); };
     const float alpha = q.x.data ? q.residual_scale : 0.0f;
     int64_t gate_until = 0; // first row of another gate row than the present one
     if (blockIdx.x < q.rows) load_row(blockIdx.x);
