@@ -1,0 +1,57 @@
+"""The training operators where sums leave fp32, codes mean no number, and sizes end what can be numbered."""
+import numpy as np
+import pytest
+
+import test_gpu_training_ops as small
+from oracle import training as orc
+
+pytestmark = pytest.mark.gpu
+torch = pytest.importorskip("torch")
+ah = small.ah
+
+
+def rest_of(cols):
+    """What 1 / cols in fp32 leaves of the true quotient: the kernel adds it, and an infinite sum must not meet it."""
+    over = np.float32(1) / np.float32(cols)
+    return 1.0 - float(over) * cols
+
+
+@pytest.mark.parametrize("cols,sign", [(64, 0), (8192, 0), (1000, -1), (4091, -1), (8200, -1), (3000, 1), (1023, 1), (12000, 1)])
+@pytest.mark.parametrize("f32", [False, True])
+def test_rows_with_an_infinite_sum_of_squares(ah, cols, sign, f32):
+    """Whatever the width: the factor of such a row is 0, so that its finite elements count as 0 under that norm and its infinities as NaN."""
+    assert np.sign(rest_of(cols)) == sign
+    rng = np.random.default_rng(cols)
+    rows, at, alpha = 7, cols // 3, 0.5
+    x, y = rng.normal(size=(rows, cols)), rng.normal(size=(rows, cols))
+    y[5] = 0
+    clean_x, clean_y = small.up(x, f32), small.up(y, f32)
+    clean_y[1], clean_y[2] = 0, 0                   # what rows 1 and 2 come to where their y counts as nothing
+    bad_x, bad_y = small.up(x, f32), small.up(y, f32)
+    bad_y[1, at], bad_y[2, at] = 3e38, float("inf")
+    bad_x[3, at], bad_x[4, at] = 3e38, float("-inf")
+    bad_y[5, at] = float("nan")
+    more = dict(residual_scale=alpha, keep="ckpt8")
+    small.say("infinite sums of squares", cols, f32)
+    want = ah.adahop_block_norm(clean_x, clean_y, **more)
+    got = ah.adahop_block_norm(bad_x, bad_y, **more)
+    others = [c for c in range(cols) if c != at]
+    for row in (0, 6):
+        for name in ("s", "h", "rstd_post", "rstd_pre"):
+            assert torch.equal(got[name][row], want[name][row]), name
+    # y's squares pass fp32: its norm is 0, the residual alone is left
+    assert float(got["rstd_post"][1]) == 0 and torch.equal(got["s"][1], want["s"][1]) and torch.equal(got["h"][1], want["h"][1])
+    assert bool(torch.all(got["ckpt_y"][0][1] & 127 == 0)) and torch.equal(got["ckpt_s"][0][1], want["ckpt_s"][0][1])
+    # an infinity in y: NaN in its own place, and by way of it under the second norm
+    assert float(got["rstd_post"][2]) == 0 and torch.equal(got["s"][2][others], want["s"][2][others]) and bool(got["s"][2, at].isnan())
+    assert bool(got["rstd_pre"][2].isnan()) and bool(got["h"][2].isnan().all())
+    codes = got["ckpt_y"][0][2] & 127
+    assert int(codes[at]) == 127 and bool(torch.all(codes[others] == 0)) and bool(torch.all(got["ckpt_s"][0][2] & 127 == 127))
+    # s's squares pass fp32, and an infinity in s
+    for row in (3, 4):
+        assert float(got["rstd_post"][row]) == float(want["rstd_post"][row]) and float(got["rstd_pre"][row]) == 0
+        assert torch.equal(got["s"][row][others], want["s"][row][others]) and bool(torch.all(got["h"][row][others] == 0))
+        assert bool(torch.all(got["ckpt_s"][0][row][others] & 127 == 0))
+    assert float(got["h"][3, at]) == 0 and bool(got["h"][4, at].isnan()) and float(got["s"][4, at]) == float("-inf")
+    # NaN stays NaN
+    assert all(bool(got[n][5].isnan().all()) for n in ("rstd_post", "rstd_pre", "s", "h"))
