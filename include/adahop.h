@@ -315,7 +315,7 @@ int adahop_select_strategy(adahop_pattern_t pattern_a, adahop_pattern_t pattern_
  * aligned, ld_codes >= cols and a multiple of 16; bytes past cols are not written, and what they hold does not matter).
  * scales: E8M0 biased by 127, one per 32 consecutive columns (the last ones of an odd width fewer),
  * row r at scales + r * ld_scales, ld_scales >= ceil(cols / 32).  Scale = 127 + floor(log2(amax)) - 8,
- * not below 0; 0 for a block of zeros; amax is that of the finite elements.  Elements: round to
+ * not below 0; 0 for a block of zeros; amax is that of the finite elements.  255, which is never written, reads as NaN.  Elements: round to
  * nearest even, saturating at 448; infinities and NaN become NaN.  codes = NULL: absent.
  *
  * Sizes: 0 <= rows <= 2^21 (0: nothing is done, sums over rows are 0), 1 <= cols <= 2^21,

@@ -50,8 +50,8 @@ def ckpt8_pack(x):
 
 
 def ckpt8_unpack(codes, scales):
-    each = np.repeat(np.exp2(scales.astype(F64) - 127.0), 32, axis=1)[:, :codes.shape[1]]
-    return E4M3[codes] * each
+    value = np.where(scales == 255, np.nan, np.exp2(scales.astype(F64) - 127.0))        # E8M0: 255 is NaN
+    return E4M3[codes] * np.repeat(value, 32, axis=1)[:, :codes.shape[1]]
 
 
 # ---- gated activation ------------------------------------------------------------------------------------------------------

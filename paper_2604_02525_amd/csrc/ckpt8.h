@@ -237,7 +237,8 @@ template <bool ODD = true> __device__ __forceinline__ packed8 load_packed8(const
     return p;
 }
 
-__device__ __forceinline__ float scale_of(uint8_t s) { return __uint_as_float(s ? (uint32_t)s << 23 : 0x00400000u); }
+// 2^(s - 127); 255 is NaN (E8M0 has no infinity).  The same mantissa bit makes 0 2^-127 and 255 NaN.
+__device__ __forceinline__ float scale_of(uint8_t s) { return __uint_as_float((uint32_t)s << 23 | (((s + 1u) & 255u) < 2 ? 0x00400000u : 0u)); }
 
 __device__ __forceinline__ void unpack8(const packed8 &p, float (&v)[8])
 {

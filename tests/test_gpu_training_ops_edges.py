@@ -55,3 +55,34 @@ def test_rows_with_an_infinite_sum_of_squares(ah, cols, sign, f32):
     assert float(got["h"][3, at]) == 0 and bool(got["h"][4, at].isnan()) and float(got["s"][4, at]) == float("-inf")
     # NaN stays NaN
     assert all(bool(got[n][5].isnan().all()) for n in ("rstd_post", "rstd_pre", "s", "h"))
+
+
+def test_a_scale_that_is_no_number(ah):
+    """E8M0's 255 is NaN: so is whatever it scales, in every reader of a checkpoint, and nothing beside it."""
+    rows, cols = 40, 256
+    codes = torch.arange(256, dtype=torch.uint8, device="cuda").repeat(rows, 1)
+    codes[:, 127], codes[:, 255] = 0, 0             # the codes that are NaN by themselves
+    scales = torch.full((rows, 8), 120, dtype=torch.uint8, device="cuda")
+    clean = (codes, scales.clone())
+    scales[3, 2] = 255
+    there = torch.zeros(rows, cols, dtype=torch.bool, device="cuda")
+    there[3, 64:96] = True
+    value = codes.view(torch.float8_e4m3fn).float() * scales.view(torch.float8_e8m0fnu).float().repeat_interleave(32, dim=1)
+    assert torch.equal(value.isnan(), there)        # torch's reading of the two types
+    assert np.array_equal(orc.ckpt8_unpack(codes.cpu().numpy(), scales.cpu().numpy()), value.double().cpu().numpy(), equal_nan=True)
+    small.say("a scale of 255")
+    for dtype in (torch.float32, torch.bfloat16):
+        got = ah.adahop_ckpt8_unpack((codes, scales), dtype=dtype)
+        assert torch.equal(got.isnan(), there) and torch.equal(got[~there], value.to(dtype)[~there])
+    G = torch.randn(rows, 64, device="cuda").to(torch.bfloat16)
+    got, want = ah.adahop_ckpt8_wgrad(G, (codes, scales)), ah.adahop_ckpt8_wgrad(G, clean)
+    assert torch.equal(got.isnan(), there[3].expand(64, cols)) and torch.equal(got[:, ~there[3]], want[:, ~there[3]])
+    d_a = torch.randn(rows, cols, device="cuda").to(torch.bfloat16)
+    got, want = ah.adahop_swiglu_backward(clean, (codes, scales), d_a), ah.adahop_swiglu_backward(clean, clean, d_a)
+    assert torch.equal(got["d_g"].isnan(), there) and torch.equal(got["d_g"][~there], want["d_g"][~there]) and torch.equal(got["d_u"], want["d_u"])
+    one = torch.ones(rows, device="cuda")
+    back = lambda s: ah.adahop_block_norm_backward(d_a, d_a, s, clean, one, one, w_pre=d_a[0])  # noqa: E731
+    got, want = back((codes, scales)), back(clean)
+    rest = [r for r in range(rows) if r != 3]
+    assert torch.equal(got["d_x"][rest], want["d_x"][rest]) and bool(got["d_x"][3, 64:96].isnan().all())
+    assert torch.equal(got["d_w_pre"].isnan(), there[3])
