@@ -258,8 +258,11 @@ __device__ __forceinline__ void keep_raw(packed8 &p) { asm volatile("" : "+v"(p.
 // ---- rows of any width, without regard to where they end ----------------------------------------------------------------
 // The blocks of 32 of all rows are numbered through: block b lies in row b / per_row.  Division by multiplication, exact for
 // b < 2^31: with 2^(l - 1) < per_row <= 2^l and mul = ceil(2^(31 + l) / per_row), 2 b mul / 2^(32 + l) exceeds b / per_row by less than 1 / per_row.
+// Workgroups of PIECES lanes, each with eight elements, lie in rows of `across`: a launch takes fewer than 2^32 lanes along one dimension.
+constexpr int PIECES = 256;
+
 struct blocks_t {
-    uint32_t total, per_row, mul;
+    uint32_t total, per_row, mul, across;
     int shift;
 };
 
@@ -279,6 +282,8 @@ inline blocks_t blocks_of(int64_t rows, int64_t cols)
     g.shift = 0;
     while (((uint32_t)1 << g.shift) < g.per_row) ++g.shift;
     g.mul = (uint32_t)((((uint64_t)1 << (31 + g.shift)) + g.per_row - 1) / g.per_row);
+    const int64_t groups = ceil_div((int64_t)g.total * 4, PIECES);
+    g.across = (uint32_t)ceil_div(groups, ceil_div(groups, (int64_t)1 << 23));
     return g;
 }
 

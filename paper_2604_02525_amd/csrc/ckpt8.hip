@@ -8,28 +8,28 @@ namespace adahop {
 
 namespace {
 
-constexpr int PIECES = 256; // lanes of a workgroup, each with a piece of 8 elements at a time
-
-// The lane's piece number `at`: its row, its first column, and how many of its 8 elements exist (none: <= 0).
+// The lane's piece: its row, its first column, and how many of its 8 elements exist (none: <= 0).
 struct piece_t {
     uint32_t row;
     int c, n;
 };
 
-__device__ __forceinline__ piece_t piece_of(const blocks_t &g, int cols, uint32_t at)
+// Blocks are numbered, not pieces: up to 2^30 + 2^21 blocks there may be, four times as many pieces pass 32 bits.
+__device__ __forceinline__ piece_t piece_of(const blocks_t &g, int cols)
 {
+    const uint32_t at = (blockIdx.y * g.across + blockIdx.x) * (PIECES / 4) + (threadIdx.x >> 2);
     piece_t p;
     uint32_t b;
-    block_at(g, at >> 2, &p.row, &b);
-    p.c = (int)(b * 32 + (at & 3) * 8);
-    p.n = at >> 2 < g.total ? cols - p.c : 0;
+    block_at(g, at, &p.row, &b);
+    p.c = (int)(b * 32 + (threadIdx.x & 3) * 8);
+    p.n = at < g.total ? cols - p.c : 0;
     return p;
 }
 
 // 8192 x 4096 bf16: 17.4 us, 5.8 TB/s (the input of 67 MB lies in the 256 MB cache).
 template <bool F32> __global__ __launch_bounds__(PIECES) void k_ckpt8_pack(adahop_tensor_t x, adahop_ckpt8_t out, blocks_t g, int cols)
 {
-    const piece_t p = piece_of(g, cols, blockIdx.x * PIECES + threadIdx.x);
+    const piece_t p = piece_of(g, cols);
     float v[8];
     widen8(p.n > 0 ? load8<F32>(x.data, p.row * x.ld + p.c, p.n) : zero8<F32>(), v);
     const packed8 k = pack8(v);
@@ -39,7 +39,7 @@ template <bool F32> __global__ __launch_bounds__(PIECES) void k_ckpt8_pack(adaho
 // 16384 x 8192 to bf16: 68.8 us, 5.9 TB/s.
 template <bool F32> __global__ __launch_bounds__(PIECES) void k_ckpt8_unpack(adahop_ckpt8_t x, adahop_tensor_t scale, adahop_tensor_t out, blocks_t g, int cols)
 {
-    const piece_t p = piece_of(g, cols, blockIdx.x * PIECES + threadIdx.x);
+    const piece_t p = piece_of(g, cols);
     if (p.n <= 0) return;
     float v[8];
     unpack8(load_packed8(x, p.row, p.c, p.n), v);
@@ -58,7 +58,7 @@ __device__ __forceinline__ float sigmoid(float g) { return __builtin_amdgcn_rcpf
 // 8192 x 11008 bf16 with both checkpoints: 122.5 us, 5.9 TB/s (127 before the codes went past the caches).
 template <bool F32> __global__ __launch_bounds__(PIECES) void k_swiglu(adahop_swiglu_t q, blocks_t b, int cols)
 {
-    const piece_t p = piece_of(b, cols, blockIdx.x * PIECES + threadIdx.x);
+    const piece_t p = piece_of(b, cols);
     float g[8], u[8], a[8];
     widen8(p.n > 0 ? load8<F32>(q.g.data, p.row * q.g.ld + p.c, p.n) : zero8<F32>(), g);
     widen8(p.n > 0 ? load8<F32>(q.u.data, p.row * q.u.ld + p.c, p.n) : zero8<F32>(), u);
@@ -79,7 +79,7 @@ template <bool F32> __global__ __launch_bounds__(PIECES) void k_swiglu(adahop_sw
 // fp32: 12.6 us, 4.8 TB/s (no row but the first begins at a multiple of 16 bytes).
 template <bool KEPT, bool F32> __global__ __launch_bounds__(PIECES) void k_swiglu_backward(adahop_swiglu_t q, blocks_t b, int cols)
 {
-    const piece_t p = piece_of(b, cols, blockIdx.x * PIECES + threadIdx.x);
+    const piece_t p = piece_of(b, cols);
     float g[8] = {}, u[8] = {}, da[8], dg[8], du[8], a[8];
     widen8(p.n > 0 ? load8<F32>(q.d_a.data, p.row * q.d_a.ld + p.c, p.n) : zero8<F32>(), da);
     if (p.n > 0) {
@@ -110,7 +110,7 @@ template <bool KEPT, bool F32> __global__ __launch_bounds__(PIECES) void k_swigl
     }
 }
 
-inline unsigned groups_of(const blocks_t &g) { return (unsigned)ceil_div((int64_t)g.total * 4, PIECES); }
+inline dim3 groups_of(const blocks_t &g) { return dim3(g.across, (unsigned)ceil_div(ceil_div((int64_t)g.total * 4, PIECES), g.across)); }
 
 } // namespace
 
@@ -147,7 +147,7 @@ int launch_swiglu(const adahop_swiglu_t &q, hipStream_t st)
 int launch_swiglu_backward(const adahop_swiglu_t &q, hipStream_t st)
 {
     const blocks_t g = blocks_of(q.rows, q.cols);
-    const unsigned n = groups_of(g);
+    const dim3 n = groups_of(g);
     const int cols = (int)q.cols;
     if (q.ckpt_g.codes)
         q.d_a.f32 ? k_swiglu_backward<true, true><<<n, PIECES, 0, st>>>(q, g, cols) : k_swiglu_backward<true, false><<<n, PIECES, 0, st>>>(q, g, cols);

@@ -86,3 +86,49 @@ def test_a_scale_that_is_no_number(ah):
     rest = [r for r in range(rows) if r != 3]
     assert torch.equal(got["d_x"][rest], want["d_x"][rest]) and bool(got["d_x"][3, 64:96].isnan().all())
     assert torch.equal(got["d_w_pre"].isnan(), there[3])
+
+
+def test_more_pieces_than_32_bits_number(ah):
+    """Just below 2^35 elements with a nearly empty last block in every row: 2^30 blocks of 32 columns and 2 031 488 more, above 2^32 pieces of 8. 173 GB."""
+    rows, cols = 2097024, 16385
+    assert rows * cols < 2 ** 35 and 4 * rows * -(-cols // 32) > 2 ** 32
+    torch.cuda.empty_cache()
+    if torch.cuda.mem_get_info()[0] < 185e9:
+        pytest.skip("185 GB of free memory wanted")
+    gen = torch.Generator(device="cuda").manual_seed(8)
+    wrap = 2 ** 30 // 513                           # the row in which block 2^30 lies
+    at = torch.tensor([0, 1, 2, 1234567, wrap - 1, wrap, wrap + 1, rows - 2, rows - 1], device="cuda")
+    few = torch.randn(len(at), cols, generator=gen, device="cuda").to(torch.bfloat16)
+
+    def only_there(t):
+        """Zero but in the rows `at`, which are left zero too."""
+        t[at] = 0
+        return not any(bool(t[a:a + 2 ** 17].any()) for a in range(0, rows, 2 ** 17))
+    x, out = (torch.zeros(rows, cols, dtype=torch.bfloat16, device="cuda") for _ in range(2))
+    x[at] = few
+    codes, scales = ah.adahop_ckpt8_empty(rows, cols)
+    codes.fill_(0x55), scales.fill_(0x55)
+    small.say("most blocks: pack", rows, cols)
+    ah.adahop_ckpt8_pack(x, out=(codes, scales))
+    want = ah.adahop_ckpt8_pack(few)
+    assert torch.equal(codes[at], want[0]) and torch.equal(scales[at], want[1])
+    assert only_there(codes) and only_there(scales)
+    codes[at], scales[at] = want
+    out.fill_(7.0)
+    small.say("most blocks: unpack")
+    ah.adahop_ckpt8_unpack((codes, scales), out=out)
+    few = ah.adahop_ckpt8_unpack(want)
+    assert torch.equal(out[at], few) and only_there(out)
+    del codes, scales
+    x[at] = few
+    out.fill_(7.0)
+    small.say("most blocks: gated activation")
+    ah.adahop_swiglu(x, x, a=out)
+    assert torch.equal(out[at], ah.adahop_swiglu(few, few)["a"]) and only_there(out)
+    out[at] = few
+    want = ah.adahop_swiglu_backward(few, few, few)
+    small.say("most blocks: gated activation, backward")
+    ah.adahop_swiglu_backward(x, x, out, d_g=x, d_u=out)       # in the place of g and of a's gradient
+    assert torch.equal(x[at], want["d_g"]) and torch.equal(out[at], want["d_u"]) and only_there(x) and only_there(out)
+    del x, out
+    torch.cuda.empty_cache()
