@@ -451,7 +451,8 @@ def adahop_select_strategy(pattern_a, pattern_b, level=1):
 
 # ---- training operators around the products ------------------------------------------------------------------------------
 # Tensors are 2-D on the GPU, bfloat16 or float32, with unit column stride and any row stride; weights are vectors.  An 8-bit
-# checkpoint is a pair (codes, scales) of uint8 tensors [rows, cols] and [rows, ceil(cols / 32)].
+# checkpoint is a pair (codes, scales) of uint8 tensors [rows, cols] and [rows, ceil(cols / 32)].  stream: a torch.cuda.Stream, whose memory the
+# outputs and workspaces that are not given then come from; or a bare handle, with which they all have to be given unless it is the current stream's.
 
 _training_calls = None
 
@@ -472,19 +473,6 @@ def _training():
     return _training_calls
 
 
-def _handle(stream):
-    return None if stream is None else _stream(stream)
-
-
-def _own_workspace(stream, need, device):
-    """Scratch for a call on a stream of its own, None on the current one (the call makes its own there)."""
-    if stream is None or not need:
-        return None
-    workspace = _u8((need,), device)
-    _hold(stream, workspace)
-    return workspace
-
-
 def adahop_ckpt8_empty(rows, cols, device="cuda"):
     """Room for the 8-bit checkpoint of a [rows, cols] activation."""
     return _u8((rows, (cols + 15) // 16 * 16), device)[:, :cols], _u8((rows, (cols + 31) // 32), device)
@@ -492,7 +480,7 @@ def adahop_ckpt8_empty(rows, cols, device="cuda"):
 
 def adahop_ckpt8_pack(x, out=None, stream=None):
     """The 8-bit checkpoint (codes, scales) of x."""
-    status, out = _training().pack(x, out, _handle(stream))
+    status, out = _training().pack(x, out, stream)
     _check(status, "adahop_ckpt8_pack")
     return out
 
@@ -501,14 +489,14 @@ def adahop_ckpt8_unpack(x8, col_scale=None, out=None, dtype=torch.bfloat16, stre
     """What a checkpoint stands for, times col_scale (a vector) if given, as `dtype` (bfloat16 or float32)."""
     if dtype is not torch.bfloat16 and dtype is not torch.float32:
         raise TypeError(f"dtype: bfloat16 or float32 wanted, not {dtype}")
-    status, out = _training().unpack(x8, col_scale, out, dtype is torch.float32, _handle(stream))
+    status, out = _training().unpack(x8, col_scale, out, dtype is torch.float32, stream)
     _check(status, "adahop_ckpt8_unpack")
     return out
 
 
 def adahop_swiglu(g, u, a=None, ckpt_g=None, ckpt_u=None, keep8=False, stream=None):
     """a = silu(g) * u (bfloat16 unless a is given).  keep8: g's and u's 8-bit checkpoints too.  Returns dict(a, ckpt_g, ckpt_u)."""
-    status, out = _training().swiglu(g, u, a, ckpt_g, ckpt_u, keep8, _handle(stream))
+    status, out = _training().swiglu(g, u, a, ckpt_g, ckpt_u, keep8, stream)
     _check(status, "adahop_swiglu")
     return out
 
@@ -517,7 +505,7 @@ def adahop_swiglu_backward(g, u, d_a, d_g=None, d_u=None, a=None, stream=None):
     """Gradients of adahop_swiglu's inputs.  g, u: tensors, or their 8-bit checkpoints.  a: where silu(g) * u is written again, a
     tensor or room for an 8-bit checkpoint; None: it is not.  d_g and d_u are by default the halves of one new bfloat16 tensor, the output
     gradient of a product that computed [g | u].  Returns dict(d_g, d_u, a)."""
-    status, out = _training().swiglu_backward(g, u, d_a, d_g, d_u, a, _handle(stream))
+    status, out = _training().swiglu_backward(g, u, d_a, d_g, d_u, a, stream)
     _check(status, "adahop_swiglu_backward")
     return out
 
@@ -534,7 +522,7 @@ def adahop_block_norm(x=None, y=None, w_post=None, w_pre=None, gate=None, gate_r
     if keep is not None and keep != "stats" and keep != "ckpt8":
         raise ValueError(f"keep: None, 'stats' or 'ckpt8', not {keep!r}")
     status, out = _training().block_norm(x, y, w_post, w_pre, gate, gate_rows, residual_scale, branch_scale, eps, post_norm, pre_norm, s, h, rstd_post,
-                                         rstd_pre, ckpt_y, ckpt_s, keep == "stats", keep == "ckpt8", _handle(stream))
+                                         rstd_pre, ckpt_y, ckpt_s, keep == "stats", keep == "ckpt8", stream)
     _check(status, "adahop_block_norm")
     return out
 
@@ -545,13 +533,8 @@ def adahop_block_norm_backward(d_s, d_h, s, y, rstd_pre, rstd_post, w_post=None,
     """Gradients of adahop_block_norm's inputs from those of s and h (either may be None).  s, y: the tensors, or their
     8-bit checkpoints ckpt_s, ckpt_y; y None: there was no block output.  Gradients of weights (float32) and of the gate are computed for those that
     are given; the others' places are None.  d_x may be d_s, d_y may be d_h.  Returns dict(d_x, d_y, d_w_post, d_w_pre, d_gate)."""
-    if workspace is None and stream is not None:
-        some = d_h if d_s is None else d_s
-        rows = some.shape[0]
-        every = 0 if gate is None else max(rows, 1) if gate.dim() == 1 else int(gate_rows)
-        workspace = _own_workspace(stream, int(lib().adahop_block_norm_backward_workspace_bytes(rows, some.shape[1], every)), some.device)
     status, out = _training().block_norm_backward(d_s, d_h, s, y, rstd_pre, rstd_post, w_post, w_pre, gate, gate_rows, residual_scale, branch_scale,
-                                                  post_norm, d_x, d_y, d_w_post, d_w_pre, d_gate, workspace, _handle(stream))
+                                                  post_norm, d_x, d_y, d_w_post, d_w_pre, d_gate, workspace, stream)
     _check(status, "adahop_block_norm_backward")
     return out
 
@@ -559,8 +542,6 @@ def adahop_block_norm_backward(d_s, d_h, s, y, rstd_pre, rstd_post, w_post=None,
 def adahop_ckpt8_wgrad(G, x8, col_scale=None, add=None, Cout=None, c_bf16=False, workspace=None, stream=None):
     """Weight gradient [d_out, d_in] of a linear layer from its output gradient G (bfloat16 [tokens, d_out]) and the 8-bit checkpoint
     of its input: G^T x, times col_scale per input feature, plus add.  float32 unless c_bf16 or Cout say otherwise; add may be Cout."""
-    if workspace is None and stream is not None:
-        workspace = _own_workspace(stream, int(lib().adahop_ckpt8_wgrad_workspace_bytes(*G.shape, x8[0].shape[1])), G.device)
-    status, out = _training().wgrad(G, x8, col_scale, add, Cout, c_bf16, workspace, _handle(stream))
+    status, out = _training().wgrad(G, x8, col_scale, add, Cout, c_bf16, workspace, stream)
     _check(status, "adahop_ckpt8_wgrad")
     return out

@@ -5,6 +5,9 @@
 
 #include <ATen/core/Tensor.h>
 #include <ATen/ops/empty.h>
+#include <c10/core/DeviceGuard.h>
+#include <c10/core/StreamGuard.h>
+#include <c10/core/impl/VirtualGuardImpl.h>
 #include <torch/csrc/Exceptions.h>
 #include <torch/csrc/autograd/python_variable.h>
 
@@ -160,15 +163,89 @@ frame_t frame_of_checkpoint(PyObject *o, const char *what)
     return frame_of(PyTuple_GET_ITEM(o, 0), what);
 }
 
-// ---- outputs that the caller has not given ----------------------------------------------------------------------------------
-PyObject *empty(at::IntArrayRef shape, at::ScalarType type, const frame_t &f) { return THPVariable_Wrap(at::empty(shape, at::TensorOptions().dtype(type).device(f.device))); }
+// ---- the stream, and outputs that the caller has not given --------------------------------------------------------------------
+PyObject *current_stream = nullptr; // a callable: the handle of torch's current stream on the current device
 
-PyObject *empty_checkpoint(const frame_t &f)
+void *handle_of(PyObject *o)
+{
+    const unsigned long long h = PyLong_AsUnsignedLongLongMask(o);
+    if (h == (unsigned long long)-1 && PyErr_Occurred()) throw python_error();
+    return reinterpret_cast<void *>((uintptr_t)h);
+}
+
+int64_t integer_attribute(PyObject *o, const char *name)
+{
+    const object_t v(PyObject_GetAttrString(o, name));
+    return integer(v.p);
+}
+
+// Where a call's work is queued: on the tensors' device, on the stream that the caller names (a torch stream or a handle) or, None, on the current one.
+//
+// What a call allocates while it names another stream than the current one comes from that stream's memory, which its earlier work may still use and its
+// later work alone gets back: an output that the caller drops at once, or a workspace, is nobody else's before the kernels are done with it.  The current stream is
+// recorded on such outputs, so that one may be read there (once it has waited for the other) and dropped.  A bare handle has no memory of its own: with one of another
+// stream all outputs and workspaces have to be the caller's.
+class queue_t {
+public:
+    queue_t(PyObject *o, const frame_t &f) : device(f.device)
+    {
+        const bool torch_stream = o != Py_None && !PyIndex_Check(o);
+        if (torch_stream && !PyObject_HasAttrString(o, "cuda_stream")) refuse(PyExc_TypeError, std::string("stream: a torch.cuda.Stream or a handle wanted, not ") + Py_TYPE(o)->tp_name);
+        if (!device.is_cuda()) return; // refused by handle(), behind what else is wrong
+        on.reset_device(device);
+        if (torch_stream) {
+            const c10::Stream s = c10::Stream::unpack3(integer_attribute(o, "stream_id"), (c10::DeviceIndex)integer_attribute(o, "device_index"), (c10::DeviceType)integer_attribute(o, "device_type"));
+            if (s.device() != device) refuse(PyExc_ValueError, "stream: one of " + device.str() + " wanted, not of " + s.device().str());
+            const c10::Stream now = c10::impl::VirtualGuardImpl(device.type()).getStream(device);
+            if (s != now) {
+                before = now;
+                as.reset_stream(s);
+            }
+        }
+        const object_t now(PyObject_CallNoArgs(current_stream));
+        at = handle_of(now.p);
+        if (o != Py_None && !torch_stream) {
+            void *const given = handle_of(o);
+            allocates = given == at;
+            at = given;
+        }
+    }
+    // The stream's, asked for when the arguments have been checked.  What the frame's tensors hold has to be where a kernel can read it.
+    void *handle() const
+    {
+        if (!device.is_cuda()) refuse(PyExc_ValueError, "tensors on a GPU wanted, not on " + device.str());
+        return at;
+    }
+    at::Tensor scratch(at::IntArrayRef shape, at::ScalarType type) const
+    {
+        if (!allocates) refuse(PyExc_ValueError, "a bare handle of another stream than the current one needs all outputs and workspaces given (or a torch.cuda.Stream)");
+        return at::empty(shape, at::TensorOptions().dtype(type).device(device));
+    }
+    at::Tensor output(at::IntArrayRef shape, at::ScalarType type) const
+    {
+        at::Tensor t = scratch(shape, type);
+        if (before) t.record_stream(*before);
+        return t;
+    }
+
+    const at::Device device;
+
+private:
+    c10::OptionalDeviceGuard on;
+    c10::OptionalStreamGuard as;
+    std::optional<c10::Stream> before; // the current one, where the call is on another
+    void *at = nullptr;
+    bool allocates = true;
+};
+
+PyObject *empty(at::IntArrayRef shape, at::ScalarType type, const queue_t &q) { return THPVariable_Wrap(q.output(shape, type)); }
+
+PyObject *empty_checkpoint(const frame_t &f, const queue_t &q)
 {
     const int64_t ld = (f.cols + 15) / 16 * 16;
-    at::Tensor codes = at::empty({f.rows, ld}, at::TensorOptions().dtype(at::kByte).device(f.device));
+    at::Tensor codes = q.output({f.rows, ld}, at::kByte);
     if (ld != f.cols) codes = codes.narrow(1, 0, f.cols);
-    const object_t c(THPVariable_Wrap(codes)), s(empty({f.rows, (f.cols + 31) / 32}, at::kByte, f));
+    const object_t c(THPVariable_Wrap(codes)), s(empty({f.rows, (f.cols + 31) / 32}, at::kByte, q));
     return PyTuple_Pack(2, c.p, s.p);
 }
 
@@ -188,37 +265,25 @@ PyObject *none()
 
 at::ScalarType type_of(PyObject *o) { return THPVariable_Unpack(o).scalar_type(); }
 
-// A workspace of so many bytes: the caller's, or a new one (released when the call returns, which is right on the current stream).
+// A workspace of so many bytes: the caller's, or a new one (released when the call returns, to its stream's later work).
 struct workspace_t {
     at::Tensor own;
     void *data = nullptr;
     size_t bytes = 0;
-    workspace_t(PyObject *o, size_t need, const frame_t &f)
+    workspace_t(PyObject *o, size_t need, const queue_t &q)
     {
         if (o == Py_None) {
             if (!need) return;
-            own = at::empty({(int64_t)need}, at::TensorOptions().dtype(at::kByte).device(f.device));
+            own = q.scratch({(int64_t)need}, at::kByte);
         } else {
             own = tensor_of(o, "workspace");
-            if (own.scalar_type() != at::kByte || own.dim() != 1 || (own.size(0) > 1 && own.stride(0) != 1) || own.device() != f.device)
-                refuse(PyExc_ValueError, "workspace: a dense uint8 vector on " + f.device.str() + " wanted");
+            if (own.scalar_type() != at::kByte || own.dim() != 1 || (own.size(0) > 1 && own.stride(0) != 1) || own.device() != q.device)
+                refuse(PyExc_ValueError, "workspace: a dense uint8 vector on " + q.device.str() + " wanted");
         }
         data = own.data_ptr();
         bytes = (size_t)own.numel();
     }
 };
-
-PyObject *current_stream = nullptr; // a callable: the handle of torch's current stream
-
-// The handle that the caller has given, or None: the current stream's, asked for when the arguments have been checked.  What the frame's tensors
-// hold has to be where a kernel can read it.
-void *stream_of(PyObject *o, const frame_t &f)
-{
-    if (!f.device.is_cuda()) refuse(PyExc_ValueError, "tensors on a GPU wanted, not on " + f.device.str());
-    if (o != Py_None) return reinterpret_cast<void *>((uintptr_t)PyLong_AsUnsignedLongLongMask(o));
-    const object_t handle(PyObject_CallNoArgs(current_stream));
-    return reinterpret_cast<void *>((uintptr_t)PyLong_AsUnsignedLongLongMask(handle.p));
-}
 
 struct names_t {
     PyObject *a, *ckpt_g, *ckpt_u, *d_g, *d_u, *s, *h, *rstd_post, *rstd_pre, *ckpt_y, *ckpt_s, *d_x, *d_y, *d_w_post, *d_w_pre, *d_gate;
@@ -252,10 +317,11 @@ PyObject *pack(PyObject *, PyObject *const *v, Py_ssize_t n)
     HANDLE_TH_ERRORS
     expect(n, 3);
     const frame_t f = frame_of(v[0], "x");
+    const queue_t q(v[2], f);
     const adahop_tensor_t x = matrix(v[0], f, "x");
-    const object_t out(given_or(v[1], [&] { return empty_checkpoint(f); }));
+    const object_t out(given_or(v[1], [&] { return empty_checkpoint(f, q); }));
     const adahop_ckpt8_t k = checkpoint(out.p, f, "out");
-    return answer(entry.pack(f.rows, f.cols, &x, &k, stream_of(v[2], f)), out.p);
+    return answer(entry.pack(f.rows, f.cols, &x, &k, q.handle()), out.p);
     END_HANDLE_TH_ERRORS
 }
 
@@ -265,11 +331,12 @@ PyObject *unpack(PyObject *, PyObject *const *v, Py_ssize_t n)
     HANDLE_TH_ERRORS
     expect(n, 5);
     const frame_t f = frame_of_checkpoint(v[0], "x8");
+    const queue_t q(v[4], f);
     const adahop_ckpt8_t x = checkpoint(v[0], f, "x8");
     const adahop_tensor_t scale = vector(v[1], f, "col_scale");
-    const object_t out(given_or(v[2], [&] { return empty({f.rows, f.cols}, truth(v[3]) ? at::kFloat : at::kBFloat16, f); }));
+    const object_t out(given_or(v[2], [&] { return empty({f.rows, f.cols}, truth(v[3]) ? at::kFloat : at::kBFloat16, q); }));
     const adahop_tensor_t o = matrix(out.p, f, "out");
-    return answer(entry.unpack(f.rows, f.cols, &x, &scale, &o, stream_of(v[4], f)), out.p);
+    return answer(entry.unpack(f.rows, f.cols, &x, &scale, &o, q.handle()), out.p);
     END_HANDLE_TH_ERRORS
 }
 
@@ -279,14 +346,15 @@ PyObject *swiglu(PyObject *, PyObject *const *v, Py_ssize_t n)
     HANDLE_TH_ERRORS
     expect(n, 7);
     const frame_t f = frame_of(v[0], "g");
+    const queue_t q(v[6], f);
     const bool keep = truth(v[5]);
     adahop_swiglu_t p = {};
     p.rows = f.rows, p.cols = f.cols;
     p.g = matrix(v[0], f, "g"), p.u = matrix(v[1], f, "u");
-    const object_t a(given_or(v[2], [&] { return empty({f.rows, f.cols}, at::kBFloat16, f); }));
-    const object_t kg(given_or(v[3], [&] { return keep ? empty_checkpoint(f) : none(); })), ku(given_or(v[4], [&] { return keep ? empty_checkpoint(f) : none(); }));
+    const object_t a(given_or(v[2], [&] { return empty({f.rows, f.cols}, at::kBFloat16, q); }));
+    const object_t kg(given_or(v[3], [&] { return keep ? empty_checkpoint(f, q) : none(); })), ku(given_or(v[4], [&] { return keep ? empty_checkpoint(f, q) : none(); }));
     p.a = matrix(a.p, f, "a"), p.ckpt_g = checkpoint(kg.p, f, "ckpt_g"), p.ckpt_u = checkpoint(ku.p, f, "ckpt_u");
-    return answer(entry.swiglu(&p, stream_of(v[6], f)), {{name.a, a.p}, {name.ckpt_g, kg.p}, {name.ckpt_u, ku.p}});
+    return answer(entry.swiglu(&p, q.handle()), {{name.a, a.p}, {name.ckpt_g, kg.p}, {name.ckpt_u, ku.p}});
     END_HANDLE_TH_ERRORS
 }
 
@@ -296,6 +364,7 @@ PyObject *swiglu_backward(PyObject *, PyObject *const *v, Py_ssize_t n)
     HANDLE_TH_ERRORS
     expect(n, 7);
     const frame_t f = frame_of(v[2], "d_a");
+    const queue_t q(v[6], f);
     adahop_swiglu_t p = {};
     p.rows = f.rows, p.cols = f.cols;
     if (is_checkpoint(v[0]))
@@ -311,11 +380,11 @@ PyObject *swiglu_backward(PyObject *, PyObject *const *v, Py_ssize_t n)
     else
         p.a = matrix(v[5], f, "a");
     at::Tensor both;
-    if (v[3] == Py_None && v[4] == Py_None) both = at::empty({f.rows, 2 * f.cols}, at::TensorOptions().dtype(at::kBFloat16).device(f.device));
-    const auto half = [&](int64_t from) { return both.defined() ? THPVariable_Wrap(both.narrow(1, from, f.cols)) : empty({f.rows, f.cols}, at::kBFloat16, f); };
+    if (v[3] == Py_None && v[4] == Py_None) both = q.output({f.rows, 2 * f.cols}, at::kBFloat16);
+    const auto half = [&](int64_t from) { return both.defined() ? THPVariable_Wrap(both.narrow(1, from, f.cols)) : empty({f.rows, f.cols}, at::kBFloat16, q); };
     const object_t dg(given_or(v[3], [&] { return half(0); })), du(given_or(v[4], [&] { return half(f.cols); }));
     p.d_a = matrix(v[2], f, "d_a"), p.d_g = matrix(dg.p, f, "d_g"), p.d_u = matrix(du.p, f, "d_u");
-    return answer(entry.swiglu_backward(&p, stream_of(v[6], f)), {{name.d_g, dg.p}, {name.d_u, du.p}, {name.a, v[5]}});
+    return answer(entry.swiglu_backward(&p, q.handle()), {{name.d_g, dg.p}, {name.d_u, du.p}, {name.a, v[5]}});
     END_HANDLE_TH_ERRORS
 }
 
@@ -342,6 +411,7 @@ PyObject *block_norm(PyObject *, PyObject *const *v, Py_ssize_t n)
     expect(n, 20);
     PyObject *const x = v[0], *const y = v[1];
     const frame_t f = frame_of(x == Py_None ? y : x, x == Py_None ? "y" : "x");
+    const queue_t q(v[19], f);
     adahop_block_norm_t p = {};
     p.rows = f.rows, p.cols = f.cols;
     p.residual_scale = number(v[6]), p.branch_scale = number(v[7]), p.eps = number(v[8]);
@@ -350,17 +420,17 @@ PyObject *block_norm(PyObject *, PyObject *const *v, Py_ssize_t n)
     p.x = matrix(x, f, "x"), p.y = matrix(y, f, "y"), p.w_post = vector(v[2], f, "w_post"), p.w_pre = vector(v[3], f, "w_pre");
     set_gate(p, v[4], v[5], f);
     const bool same = !has_y && p.residual_scale == 1.0f && (v[11] == Py_None || v[11] == x); // s = x is there already
-    const auto vec = [&](bool wanted) { return wanted ? empty({f.rows}, at::kFloat, f) : none(); };
-    const auto kept = [&](bool wanted) { return wanted ? empty_checkpoint(f) : none(); };
-    const object_t s(same ? given_or(x, none) : given_or(v[11], [&] { return empty({f.rows, f.cols}, type_of(x == Py_None ? y : x), f); }));
-    const object_t h(pre ? given_or(v[12], [&] { return empty({f.rows, f.cols}, at::kBFloat16, f); }) : none());
+    const auto vec = [&](bool wanted) { return wanted ? empty({f.rows}, at::kFloat, q) : none(); };
+    const auto kept = [&](bool wanted) { return wanted ? empty_checkpoint(f, q) : none(); };
+    const object_t s(same ? given_or(x, none) : given_or(v[11], [&] { return empty({f.rows, f.cols}, type_of(x == Py_None ? y : x), q); }));
+    const object_t h(pre ? given_or(v[12], [&] { return empty({f.rows, f.cols}, at::kBFloat16, q); }) : none());
     const object_t r_post(given_or(v[13], [&] { return vec((stats || keep) && post); })), r_pre(given_or(v[14], [&] { return vec((stats || keep) && pre); }));
     const object_t ky(given_or(v[15], [&] { return kept(keep && has_y); })), ks(given_or(v[16], [&] { return kept(keep && pre); }));
     if (!same) p.s = matrix(s.p, f, "s");
     p.h = matrix(h.p, f, "h");
     p.rstd_post = floats(r_post.p, f.rows, f, "rstd_post"), p.rstd_pre = floats(r_pre.p, f.rows, f, "rstd_pre");
     p.ckpt_y = checkpoint(ky.p, f, "ckpt_y"), p.ckpt_s = checkpoint(ks.p, f, "ckpt_s");
-    return answer(entry.norm(&p, stream_of(v[19], f)), {{name.s, s.p}, {name.h, h.p}, {name.rstd_post, r_post.p}, {name.rstd_pre, r_pre.p}, {name.ckpt_y, ky.p}, {name.ckpt_s, ks.p}});
+    return answer(entry.norm(&p, q.handle()), {{name.s, s.p}, {name.h, h.p}, {name.rstd_post, r_post.p}, {name.rstd_pre, r_pre.p}, {name.ckpt_y, ky.p}, {name.ckpt_s, ks.p}});
     END_HANDLE_TH_ERRORS
 }
 
@@ -373,6 +443,7 @@ PyObject *block_norm_backward(PyObject *, PyObject *const *v, Py_ssize_t n)
     PyObject *const d_s = v[0], *const d_h = v[1], *const s = v[2], *const y = v[3];
     const bool has_s = d_s != Py_None, has_h = d_h != Py_None, has_y = y != Py_None;
     const frame_t f = frame_of(has_s ? d_s : d_h, has_s ? "d_s" : "d_h");
+    const queue_t q(v[19], f);
     adahop_block_norm_t p = {};
     p.rows = f.rows, p.cols = f.cols;
     p.post_norm = truth(v[12]) && has_y;
@@ -389,17 +460,17 @@ PyObject *block_norm_backward(PyObject *, PyObject *const *v, Py_ssize_t n)
         p.y = matrix(y, f, "y");
     p.rstd_pre = floats(v[4], f.rows, f, "rstd_pre"), p.rstd_post = floats(v[5], f.rows, f, "rstd_post");
     p.d_s = matrix(d_s, f, "d_s"), p.d_h = matrix(d_h, f, "d_h");
-    const auto like = [&](at::ScalarType type) { return empty({f.rows, f.cols}, type, f); };
-    const auto vec = [&](bool wanted) { return wanted ? empty({f.cols}, at::kFloat, f) : none(); };
+    const auto like = [&](at::ScalarType type) { return empty({f.rows, f.cols}, type, q); };
+    const auto vec = [&](bool wanted) { return wanted ? empty({f.cols}, at::kFloat, q) : none(); };
     const object_t dx(given_or(v[13], [&] { return like(has_s ? type_of(d_s) : p.s.data ? type_of(s) : type_of(d_h)); }));
     const object_t dy(given_or(v[14], [&] { return !has_y ? none() : like(has_h ? type_of(d_h) : p.y.data ? type_of(y) : at::kBFloat16); }));
     const object_t dwpost(given_or(v[15], [&] { return vec(v[6] != Py_None); })), dwpre(given_or(v[16], [&] { return vec(v[7] != Py_None && has_h); }));
-    const object_t dgate(given_or(v[17], [&] { return v[8] == Py_None ? none() : THPVariable_Wrap(at::empty(THPVariable_Unpack(v[8]).sizes(), THPVariable_Unpack(v[8]).options())); }));
+    const object_t dgate(given_or(v[17], [&] { return v[8] == Py_None ? none() : empty(THPVariable_Unpack(v[8]).sizes(), type_of(v[8]), q); }));
     p.d_x = matrix(dx.p, f, "d_x"), p.d_y = matrix(dy.p, f, "d_y");
     p.d_w_post = floats(dwpost.p, f.cols, f, "d_w_post"), p.d_w_pre = floats(dwpre.p, f.cols, f, "d_w_pre");
     if (dgate.p != Py_None) p.d_gate = tensor_of(dgate.p, "d_gate").dim() == 1 ? vector(dgate.p, f, "d_gate") : matrix(dgate.p, f, p.gates, "d_gate");
-    const workspace_t ws(v[18], entry.norm_backward_bytes(f.rows, f.cols, p.gate.data ? p.gate_rows : 0), f);
-    return answer(entry.norm_backward(&p, ws.data, ws.bytes, stream_of(v[19], f)),
+    const workspace_t ws(v[18], entry.norm_backward_bytes(f.rows, f.cols, p.gate.data ? p.gate_rows : 0), q);
+    return answer(entry.norm_backward(&p, ws.data, ws.bytes, q.handle()),
                   {{name.d_x, dx.p}, {name.d_y, dy.p}, {name.d_w_post, dwpost.p}, {name.d_w_pre, dwpre.p}, {name.d_gate, dgate.p}});
     END_HANDLE_TH_ERRORS
 }
@@ -410,14 +481,15 @@ PyObject *wgrad(PyObject *, PyObject *const *v, Py_ssize_t n)
     HANDLE_TH_ERRORS
     expect(n, 8);
     const frame_t g = frame_of(v[0], "G"), x = {g.rows, frame_of_checkpoint(v[1], "x8").cols, g.device}, c = {g.cols, x.cols, g.device};
+    const queue_t q(v[7], g);
     adahop_tensor_t G = matrix(v[0], g, "G");
     if (g.rows <= 1) G.ld = (g.cols + 7) / 8 * 8;
     const adahop_ckpt8_t k = checkpoint(v[1], x, "x8");
     const adahop_tensor_t scale = vector(v[2], c, "col_scale"), add = matrix(v[3], c, "add");
-    const object_t out(given_or(v[4], [&] { return empty({c.rows, c.cols}, truth(v[5]) ? at::kBFloat16 : at::kFloat, c); }));
+    const object_t out(given_or(v[4], [&] { return empty({c.rows, c.cols}, truth(v[5]) ? at::kBFloat16 : at::kFloat, q); }));
     const adahop_tensor_t C = matrix(out.p, c, "Cout");
-    const workspace_t ws(v[6], entry.wgrad_bytes(g.rows, g.cols, x.cols), g);
-    return answer(entry.wgrad(g.rows, g.cols, x.cols, &G, &k, &scale, &add, &C, ws.data, ws.bytes, stream_of(v[7], g)), out.p);
+    const workspace_t ws(v[6], entry.wgrad_bytes(g.rows, g.cols, x.cols), q);
+    return answer(entry.wgrad(g.rows, g.cols, x.cols, &G, &k, &scale, &add, &C, ws.data, ws.bytes, q.handle()), out.p);
     END_HANDLE_TH_ERRORS
 }
 

@@ -222,3 +222,10 @@ def test_binding_refuses_tensors_in_host_memory():
                  lambda: ah.adahop_block_norm_backward(x, x, x, x, r, r), lambda: ah.adahop_ckpt8_wgrad(x, pair)):
         with pytest.raises(ValueError, match="on a GPU"):
             call()
+
+
+def test_binding_refuses_what_is_no_stream():
+    x = torch.zeros(4, 64, dtype=torch.bfloat16)
+    for stream in ("0", 1.5, object()):
+        with pytest.raises(TypeError, match="stream"):
+            ah.adahop_ckpt8_pack(x, stream=stream)
