@@ -450,6 +450,11 @@ int adahop_probe_mfma_rate(int random_operands, int idle_sleeps, int workgroups,
  * fp32 summation order (1 .. 8: the same bits).  Returns ADAHOP_E_INVALID_ARG for any other value. */
 int adahop_debug_force_gemm_kernel(int which);
 
+/* What adahop_ckpt8_wgrad takes for these sizes (host only), so that a test knows which of its kernels it has reached: *tile = 256 or 128 columns
+ * of G and of x per workgroup, *shares = 2 where a workgroup's waves share the tokens of a 128 tile, else 1, *slices = how many slices of the
+ * tokens are summed up by a second kernel (1: none).  Returns ADAHOP_E_INVALID_ARG for sizes that it refuses or a null pointer. */
+int adahop_debug_ckpt8_wgrad_plan(int64_t tokens, int64_t d_out, int64_t d_in, int *tile, int *shares, int *slices);
+
 #ifdef __cplusplus
 }
 #endif

@@ -25,7 +25,7 @@ EXPORTS = ["adahop_quantize_mx", "adahop_iht_quantize", "adahop_foid_topk", "ada
            "adahop_oe_gemm_bf16", "adahop_detect_pattern_workspace_bytes", "adahop_detect_pattern",
            "adahop_ckpt8_pack", "adahop_ckpt8_unpack", "adahop_swiglu", "adahop_swiglu_backward", "adahop_block_norm",
            "adahop_block_norm_backward", "adahop_block_norm_backward_workspace_bytes", "adahop_ckpt8_wgrad", "adahop_ckpt8_wgrad_workspace_bytes",
-           "adahop_select_strategy", "adahop_vote_pattern", "adahop_probe_mfma_rate", "adahop_debug_force_gemm_kernel", "adahop_prepare_device", "adahop_last_hip_error", "adahop_status_string",
+           "adahop_select_strategy", "adahop_vote_pattern", "adahop_probe_mfma_rate", "adahop_debug_force_gemm_kernel", "adahop_debug_ckpt8_wgrad_plan", "adahop_prepare_device", "adahop_last_hip_error", "adahop_status_string",
            "adahop_abi_version"]
 
 
@@ -128,6 +128,7 @@ def lib():
         L.adahop_vote_pattern.argtypes = [C.POINTER(C.c_int32), I]
         L.adahop_probe_mfma_rate.argtypes = [I, I, I, I, P, P]
         L.adahop_debug_force_gemm_kernel.argtypes = [I]
+        L.adahop_debug_ckpt8_wgrad_plan.argtypes = [I64, I64, I64] + [C.POINTER(C.c_int)] * 3
         L.adahop_status_string.restype = C.c_char_p
         L.adahop_status_string.argtypes = [I]
         for name in EXPORTS:
@@ -545,3 +546,10 @@ def adahop_ckpt8_wgrad(G, x8, col_scale=None, add=None, Cout=None, c_bf16=False,
     status, out = _training().wgrad(G, x8, col_scale, add, Cout, c_bf16, workspace, stream)
     _check(status, "adahop_ckpt8_wgrad")
     return out
+
+
+def adahop_debug_ckpt8_wgrad_plan(tokens, d_out, d_in):
+    """(tile, shares, slices) that adahop_ckpt8_wgrad takes for these sizes."""
+    out = [C.c_int() for _ in range(3)]
+    _check(lib().adahop_debug_ckpt8_wgrad_plan(tokens, d_out, d_in, *(C.byref(v) for v in out)), "adahop_debug_ckpt8_wgrad_plan")
+    return tuple(v.value for v in out)

@@ -162,6 +162,13 @@ size_t adahop_ckpt8_wgrad_workspace_bytes(int64_t tokens, int64_t d_out, int64_t
     return wgrad8_workspace_bytes(tokens, d_out, d_in);
 }
 
+int adahop_debug_ckpt8_wgrad_plan(int64_t tokens, int64_t d_out, int64_t d_in, int *tile, int *shares, int *slices)
+{
+    if (!valid_shape(tokens, d_out) || !valid_shape(tokens, d_in) || !valid_shape(d_out, d_in) || d_out < 1 || !tile || !shares || !slices) return ADAHOP_E_INVALID_ARG;
+    wgrad8_plan(tokens, d_out, d_in, tile, shares, slices);
+    return ADAHOP_OK;
+}
+
 int adahop_ckpt8_wgrad(int64_t tokens, int64_t d_out, int64_t d_in, const adahop_tensor_t *G, const adahop_ckpt8_t *x, const adahop_tensor_t *col_scale,
                        const adahop_tensor_t *add, const adahop_tensor_t *C, void *workspace, size_t workspace_bytes, void *stream)
 {

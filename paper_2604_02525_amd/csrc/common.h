@@ -187,6 +187,7 @@ size_t block_norm_backward_workspace_bytes(int64_t rows, int64_t cols, int64_t g
 int launch_block_norm_backward(const adahop_block_norm_t &q, bool s32, bool y32, bool kept, void *workspace, hipStream_t st);
 int launch_block_norm_no_rows(const adahop_block_norm_t &q, hipStream_t st); // sums over nothing
 size_t wgrad8_workspace_bytes(int64_t tokens, int64_t d_out, int64_t d_in);
+void wgrad8_plan(int64_t tokens, int64_t d_out, int64_t d_in, int *tile, int *shares, int *slices);
 int launch_wgrad8(int64_t tokens, int64_t d_out, int64_t d_in, const adahop_tensor_t &G, const adahop_ckpt8_t &x, const adahop_tensor_t &col_scale,
                   const adahop_tensor_t &add, const adahop_tensor_t &C, void *workspace, hipStream_t st);
 

@@ -494,6 +494,14 @@ int configure_wgrad8()
 
 size_t wgrad8_workspace_bytes(int64_t T, int64_t N, int64_t D) { return plan_of(T, N, D).bytes; }
 
+void wgrad8_plan(int64_t T, int64_t N, int64_t D, int *tile, int *shares, int *slices)
+{
+    const plan_t p = plan_of(T, N, D);
+    *tile = p.large ? large_t::TM : small_t::TM;
+    *shares = !p.large && p.alone ? 2 : 1;
+    *slices = p.slices;
+}
+
 int launch_wgrad8(int64_t T, int64_t N, int64_t D, const adahop_tensor_t &G, const adahop_ckpt8_t &x, const adahop_tensor_t &col_scale,
                   const adahop_tensor_t &add, const adahop_tensor_t &C, void *workspace, hipStream_t st)
 {
