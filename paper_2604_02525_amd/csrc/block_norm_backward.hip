@@ -67,7 +67,7 @@ struct backward_t {
     int threads, gate_cuts; // threads per row; runs.gate_cuts()
     int64_t workgroups;
     const float2 *means; // of every row, for rows in strips
-    float *part;         // [workgroups][cols] w_pre, the same w_post, [runs.gate_parts()][cols] gate; nullptr: one workgroup, whose sums are the results
+    float *part;         // [workgroups][cols] w_pre, the same w_post, [runs.gate_parts()][cols] gate; nullptr: a single row, whose sums are the results
 };
 
 __device__ __forceinline__ void put(const adahop_tensor_t &t, int64_t at, float v)
@@ -305,14 +305,10 @@ template <bool BESIDE, bool STRIPS, bool ODD, bool KEPT, bool CUT, bool SF32, bo
     }
     if (BESIDE && waves > 1) // the barriers of their sums
         for (int64_t i = 0; i < fewer; ++i) __syncthreads();
-    // One gradient's part, as it is or the runs' sum, to fp32 row `to`; nullptr: to d_gate.
+    // One gradient's part, as it is or the runs' sum, to fp32 row `to`.
     const auto hand_over = [&](const float (&v)[8], float *to) {
         if constexpr (!BESIDE) {
-            if (left <= 0) return;
-            if (to)
-                store8<true, ODD>(to, col, left, v);
-            else
-                store8_any<ODD>(q.d_gate, col, left, v);
+            if (left > 0) store8<true, ODD>(to, col, left, v);
         } else {
             __syncthreads(); // no wave reads the one before any more
             float4 *const mine = reinterpret_cast<float4 *>(patch + 8 * threadIdx.x);
@@ -322,10 +318,7 @@ template <bool BESIDE, bool STRIPS, bool ODD, bool KEPT, bool CUT, bool SF32, bo
             for (int c = threadIdx.x; c < (int)q.cols; c += blockDim.x) {
                 float sum = patch[c];
                 for (int k = 1; k < b.runs.beside; ++k) sum += patch[8 * threads * k + c];
-                if (to)
-                    to[c] = sum;
-                else
-                    put(q.d_gate, c, sum);
+                to[c] = sum;
             }
         }
     };
@@ -339,7 +332,7 @@ template <bool BESIDE, bool STRIPS, bool ODD, bool KEPT, bool CUT, bool SF32, bo
 #pragma unroll
             for (int i = 0; i < 8; ++i) v[i] = any ? v[i] * agate[i] : 0.0f;
             if (!BESIDE || b.runs.joined)
-                hand_over(v, part ? part + 2 * one : nullptr);
+                hand_over(v, part + 2 * one); // (a single row is no part of a group)
             else if (run < b.runs.number && left > 0)
                 store8<true, ODD>(b.part + 2 * one, run * q.cols + col, left, v);
         }
@@ -437,9 +430,6 @@ template <bool KEPT> void launch_means(const adahop_block_norm_t &q, float2 *mea
         y32 ? k_block_norm_means<KEPT, false, true><<<n, ROW_THREADS, 0, st>>>(q, means) : k_block_norm_means<KEPT, false, false><<<n, ROW_THREADS, 0, st>>>(q, means);
 }
 
-// What it sums up is all there is.
-bool one_workgroup(const runs_t &r) { return r.workgroups() == 1 && r.joined; }
-
 size_t means_bytes(int64_t rows, int64_t cols) { return strips_of(cols) > 1 ? align_up((size_t)rows * sizeof(float2), 256) : 0; }
 
 } // namespace
@@ -448,7 +438,7 @@ size_t block_norm_backward_workspace_bytes(int64_t rows, int64_t cols, int64_t g
 {
     if (rows == 0) return 0;
     const runs_t r = runs_of(rows, cols, gate_rows);
-    return means_bytes(rows, cols) + (one_workgroup(r) ? 0 : (size_t)(2 * r.workgroups() + r.gate_parts()) * cols * sizeof(float));
+    return means_bytes(rows, cols) + (rows == 1 ? 0 : (size_t)(2 * r.workgroups() + r.gate_parts()) * cols * sizeof(float));
 }
 
 int launch_block_norm_no_rows(const adahop_block_norm_t &q, hipStream_t st) { return zero_gates_from(q, 0, st); }
@@ -457,7 +447,7 @@ int launch_block_norm_backward(const adahop_block_norm_t &q, bool s32, bool y32,
 {
     const runs_t r = runs_of(q.rows, q.cols, q.gate.data ? q.gate_rows : 0);
     float2 *const means = strips_of(q.cols) > 1 ? static_cast<float2 *>(workspace) : nullptr;
-    float *const part = one_workgroup(r) ? nullptr : reinterpret_cast<float *>(static_cast<uint8_t *>(workspace) + means_bytes(q.rows, q.cols));
+    float *const part = q.rows == 1 ? nullptr : reinterpret_cast<float *>(static_cast<uint8_t *>(workspace) + means_bytes(q.rows, q.cols));
     const backward_t b = {q, r, threads_of(q.cols), r.gate_cuts(), r.workgroups(), means, part};
     if (means) {
         kept ? launch_means<true>(q, means, s32, y32, st) : launch_means<false>(q, means, s32, y32, st);
