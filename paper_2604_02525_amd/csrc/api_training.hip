@@ -113,7 +113,9 @@ int adahop_block_norm(const adahop_block_norm_t *p, void *stream)
     if ((present(p->ckpt_y) || p->post_norm || present(p->gate)) && !present(p->y)) return ADAHOP_E_INVALID_ARG;
     if (p->rstd_post && !p->post_norm) return ADAHOP_E_INVALID_ARG;
     if ((present(p->ckpt_s) || p->rstd_pre) && !present(p->h)) return ADAHOP_E_INVALID_ARG;
-    return launch_block_norm(*p, static_cast<hipStream_t>(stream));
+    adahop_block_norm_t q = *p;
+    if (!present(q.y)) q.w_post = {}; // whatever it holds: no branch, nothing of it in s
+    return launch_block_norm(q, static_cast<hipStream_t>(stream));
 }
 
 size_t adahop_block_norm_backward_workspace_bytes(int64_t rows, int64_t cols, int64_t gate_rows)
@@ -153,7 +155,9 @@ int adahop_block_norm_backward(const adahop_block_norm_t *p, void *workspace, si
         }
     const size_t need = block_norm_backward_workspace_bytes(p->rows, p->cols, present(p->gate) ? p->gate_rows : 0);
     if (need && (!workspace || !aligned(workspace, 256) || workspace_bytes < need)) return ADAHOP_E_WORKSPACE;
-    return launch_block_norm_backward(*p, s32 == 1, y32 == 1, kept, workspace, st);
+    adahop_block_norm_t q = *p;
+    if (!present(q.d_h)) q.w_pre = {}; // as above
+    return launch_block_norm_backward(q, s32 == 1, y32 == 1, kept, workspace, st);
 }
 
 size_t adahop_ckpt8_wgrad_workspace_bytes(int64_t tokens, int64_t d_out, int64_t d_in)

@@ -57,6 +57,26 @@ def test_rows_with_an_infinite_sum_of_squares(ah, cols, sign, f32):
     assert all(bool(got[n][5].isnan().all()) for n in ("rstd_post", "rstd_pre", "s", "h"))
 
 
+@pytest.mark.parametrize("cols", [96, 8192, 8200])
+def test_weights_of_absent_parts(ah, cols):
+    """The weight of a branch or of a norm that is not there takes no part, whatever it holds."""
+    rows = 5
+    gen = torch.Generator(device="cuda").manual_seed(cols)
+    x, y, d = (torch.randn(rows, cols, generator=gen, device="cuda").to(torch.bfloat16) for _ in range(3))
+    w = torch.ones(cols, device="cuda")
+    bad = w.clone()
+    bad[3], bad[cols - 1] = float("inf"), float("nan")
+    small.say("weights of absent parts", cols)
+    want, got = ah.adahop_block_norm(x, w_pre=w, residual_scale=0.5), ah.adahop_block_norm(x, w_pre=w, w_post=bad, residual_scale=0.5)
+    assert torch.equal(got["s"], want["s"]) and torch.equal(got["h"], want["h"])
+    want, got = ah.adahop_block_norm(x, y, pre_norm=False), ah.adahop_block_norm(x, y, w_pre=bad, pre_norm=False)
+    assert torch.equal(got["s"], want["s"])
+    f = ah.adahop_block_norm(x, y, keep="ckpt8")
+    back = lambda w_pre: ah.adahop_block_norm_backward(d, None, None, f["ckpt_y"], None, f["rstd_post"], w_pre=w_pre)  # noqa: E731
+    want, got = back(w), back(bad)
+    assert torch.equal(got["d_x"], want["d_x"]) and torch.equal(got["d_y"], want["d_y"]) and bool(got["d_x"].isfinite().all())
+
+
 def test_a_scale_that_is_no_number(ah):
     """E8M0's 255 is NaN: so is whatever it scales, in every reader of a checkpoint, and nothing beside it."""
     rows, cols = 40, 256
