@@ -532,8 +532,8 @@ def adahop_block_norm_backward(d_s, d_h, s, y, rstd_pre, rstd_post, w_post=None,
                                branch_scale=1.0, post_norm=True, d_x=None, d_y=None, d_w_post=None, d_w_pre=None, d_gate=None, workspace=None,
                                stream=None):
     """Gradients of adahop_block_norm's inputs from those of s and h (either may be None).  s, y: the tensors, or their
-    8-bit checkpoints ckpt_s, ckpt_y; y None: there was no block output.  Gradients of weights (float32) and of the gate are computed for those that
-    are given; the others' places are None.  d_x may be d_s, d_y may be d_h.  Returns dict(d_x, d_y, d_w_post, d_w_pre, d_gate)."""
+    8-bit checkpoints ckpt_s, ckpt_y; y None: there was no block output (w_post takes no part then).  Gradients of weights (float32) and of the gate are computed for those that
+    are given and take part; the others' places are None.  d_x may be d_s, d_y may be d_h.  Returns dict(d_x, d_y, d_w_post, d_w_pre, d_gate)."""
     status, out = _training().block_norm_backward(d_s, d_h, s, y, rstd_pre, rstd_post, w_post, w_pre, gate, gate_rows, residual_scale, branch_scale,
                                                   post_norm, d_x, d_y, d_w_post, d_w_pre, d_gate, workspace, stream)
     _check(status, "adahop_block_norm_backward")

@@ -464,7 +464,7 @@ PyObject *block_norm_backward(PyObject *, PyObject *const *v, Py_ssize_t n)
     const auto vec = [&](bool wanted) { return wanted ? empty({f.cols}, at::kFloat, q) : none(); };
     const object_t dx(given_or(v[13], [&] { return like(has_s ? type_of(d_s) : p.s.data ? type_of(s) : type_of(d_h)); }));
     const object_t dy(given_or(v[14], [&] { return !has_y ? none() : like(has_h ? type_of(d_h) : p.y.data ? type_of(y) : at::kBFloat16); }));
-    const object_t dwpost(given_or(v[15], [&] { return vec(v[6] != Py_None); })), dwpre(given_or(v[16], [&] { return vec(v[7] != Py_None && has_h); }));
+    const object_t dwpost(given_or(v[15], [&] { return vec(v[6] != Py_None && has_y); })), dwpre(given_or(v[16], [&] { return vec(v[7] != Py_None && has_h); }));
     const object_t dgate(given_or(v[17], [&] { return v[8] == Py_None ? none() : empty(THPVariable_Unpack(v[8]).sizes(), type_of(v[8]), q); }));
     p.d_x = matrix(dx.p, f, "d_x"), p.d_y = matrix(dy.p, f, "d_y");
     p.d_w_post = floats(dwpost.p, f.cols, f, "d_w_post"), p.d_w_pre = floats(dwpre.p, f.cols, f, "d_w_pre");

@@ -77,6 +77,19 @@ def test_weights_of_absent_parts(ah, cols):
     assert torch.equal(got["d_x"], want["d_x"]) and torch.equal(got["d_y"], want["d_y"]) and bool(got["d_x"].isfinite().all())
 
 
+def test_backward_without_a_branch_but_with_its_weight(ah):
+    """As the forward pass takes it: the same as without, and no gradient of it."""
+    gen = torch.Generator(device="cuda").manual_seed(3)
+    x, d = (torch.randn(5, 96, generator=gen, device="cuda").to(torch.bfloat16) for _ in range(2))
+    w = torch.randn(96, generator=gen, device="cuda")
+    f = ah.adahop_block_norm(x, w_post=w, w_pre=w, keep="stats")
+    small.say("backward without a branch")
+    back = lambda **more: ah.adahop_block_norm_backward(d, d, f["s"], None, f["rstd_pre"], f["rstd_post"], w_pre=w, **more)  # noqa: E731
+    want, got = back(), back(w_post=w)
+    assert torch.equal(got["d_x"], want["d_x"]) and torch.equal(got["d_w_pre"], want["d_w_pre"])
+    assert got["d_y"] is None and got["d_w_post"] is None
+
+
 def test_a_scale_that_is_no_number(ah):
     """E8M0's 255 is NaN: so is whatever it scales, in every reader of a checkpoint, and nothing beside it."""
     rows, cols = 40, 256
