@@ -533,7 +533,9 @@ def adahop_block_norm_backward(d_s, d_h, s, y, rstd_pre, rstd_post, w_post=None,
                                stream=None):
     """Gradients of adahop_block_norm's inputs from those of s and h (either may be None).  s, y: the tensors, or their
     8-bit checkpoints ckpt_s, ckpt_y; y None: there was no block output (w_post takes no part then).  Gradients of weights (float32) and of the gate are computed for those that
-    are given and take part; the others' places are None.  d_x may be d_s, d_y may be d_h.  Returns dict(d_x, d_y, d_w_post, d_w_pre, d_gate)."""
+    are given and take part; the others' places are None.  d_x may be d_s, d_y may be d_h.  Unless it is given, d_x is of d_s's type, without d_s of
+    s's, and without both of d_h's: an 8-bit checkpoint does not say of what type the residual stream is, so where that is float32 and s and h have no
+    gradient but d_h (the last block), give d_x.  Returns dict(d_x, d_y, d_w_post, d_w_pre, d_gate)."""
     status, out = _training().block_norm_backward(d_s, d_h, s, y, rstd_pre, rstd_post, w_post, w_pre, gate, gate_rows, residual_scale, branch_scale,
                                                   post_norm, d_x, d_y, d_w_post, d_w_pre, d_gate, workspace, stream)
     _check(status, "adahop_block_norm_backward")

@@ -90,6 +90,41 @@ def test_backward_without_a_branch_but_with_its_weight(ah):
     assert got["d_y"] is None and got["d_w_post"] is None
 
 
+def test_type_of_the_residual_streams_gradient(ah):
+    """From d_h and checkpoints alone it is of d_h's type unless d_x is given; in float32 it is what bfloat16 is the rounding of."""
+    gen = torch.Generator(device="cuda").manual_seed(4)
+    x, y = (torch.randn(9, 200, generator=gen, device="cuda") for _ in range(2))
+    d = torch.randn(9, 200, generator=gen, device="cuda").to(torch.bfloat16)
+    f = ah.adahop_block_norm(x, y.to(torch.bfloat16), keep="ckpt8")
+    assert f["s"].dtype == torch.float32
+    small.say("type of d_x")
+    back = lambda s, d_s=None, **more: ah.adahop_block_norm_backward(d_s, d, s, f["ckpt_y"] if isinstance(s, tuple) else y.to(torch.bfloat16),  # noqa: E731
+                                                                     f["rstd_pre"], f["rstd_post"], **more)["d_x"]
+    rounded, whole = back(f["ckpt_s"]), back(f["ckpt_s"], d_x=torch.empty_like(x))
+    assert rounded.dtype == torch.bfloat16 and whole.dtype == torch.float32 and torch.equal(whole.to(torch.bfloat16), rounded)
+    assert not torch.equal(whole, rounded.float())
+    assert back(f["s"]).dtype == back(f["ckpt_s"], torch.zeros_like(x)).dtype == torch.float32
+
+
+@pytest.mark.parametrize("tokens,d_out,d_in", [(256, 96, 160), (96, 512, 320)])
+def test_unpacked_checkpoint_as_an_operand(ah, tokens, d_out, d_in):
+    """The weight gradient as an MXFP4 product of the unpacked checkpoint: the bits of the product of the values that the checkpoint stands for."""
+    gen = torch.Generator(device="cuda").manual_seed(tokens)
+    x = torch.randn(tokens, d_in, generator=gen, device="cuda")
+    G = torch.randn(tokens, d_out, generator=gen, device="cuda").to(torch.bfloat16)
+    x8 = ah.adahop_ckpt8_pack(x)
+    value = orc.ckpt8_unpack(*small.stored8(x8))
+    bits = torch.from_numpy(value).to(torch.bfloat16)
+    assert np.array_equal(bits.double().numpy(), value)                 # bfloat16 holds them all
+    small.say("unpacked checkpoint as an operand", tokens, d_out, d_in)
+    product = lambda v: ah.adahop_gemm(ah.Operand(G, False), ah.Operand(v, False), ah.ADAHOP_IHT, 32)["C"]  # noqa: E731
+    got, want = product(ah.adahop_ckpt8_unpack(x8)), product(bits.cuda())
+    assert torch.equal(got, want)
+    # of the same gradient as the product in bf16, to what MXFP4 leaves (an eighth and less of either operand)
+    exact = ah.adahop_ckpt8_wgrad(G, x8)
+    assert ((got - exact).norm() / exact.norm()).item() < 0.25
+
+
 def test_a_scale_that_is_no_number(ah):
     """E8M0's 255 is NaN: so is whatever it scales, in every reader of a checkpoint, and nothing beside it."""
     rows, cols = 40, 256
