@@ -1,4 +1,4 @@
-"""A stack of gated MLP blocks trained with MXFP4 products, its activations kept in 8 bits.
+"""A stack of gated MLP blocks trained with MXFP4 products (forward and input gradients), its activations kept in 8 bits.
 
     python examples/gated_mlp_stack.py --tokens 4096 --hidden 2048 --ffn 5632 --blocks 4 --steps 10
 
@@ -9,7 +9,8 @@ Each block is  h -> [g | u] = h W_gu^T -> a = silu(g) u -> y = a W_down^T,  and 
 The products of a block run as MXFP4 (adahop_gemm).  What lies between them runs in one pass over the memory each, and leaves behind what the
 backward pass takes: norm(s') and norm(y) in 8 bits, g and u in 8 bits, two numbers per row.  Of all activations only these are kept, 33/32 bytes an
 element; a is formed again from g and u by the backward pass, and the weight gradients are computed from the 8-bit
-rows.  The one checkpoint of norm(s') serves the gradient of W_gu (times w_pre, feature by feature) and the norm's own backward pass.
+rows, in bf16: nothing is rounded to 4 bits on the way into the float32 gradient. Where speed counts for more, adahop_ckpt8_unpack and an
+MXFP4 product take less than half of the time for large layers.  The one checkpoint of norm(s') serves the gradient of W_gu (times w_pre, feature by feature) and the norm's own backward pass.
 """
 import argparse
 import os

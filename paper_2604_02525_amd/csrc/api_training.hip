@@ -182,7 +182,7 @@ int adahop_ckpt8_wgrad(int64_t tokens, int64_t d_out, int64_t d_in, const adahop
     if (tokens > 0) {
         if (!present(*G) || G->f32 != 0 || !valid(*G, d_out) || G->ld % 8 != 0 || !aligned(G->data, 16)) return ADAHOP_E_INVALID_ARG;
         if (!present(*x) || !valid(*x, d_in)) return ADAHOP_E_INVALID_ARG;
-        // 64 rows are addressed by 32 bits
+        // a stage's 32 rows of G are addressed by 32 bits; the checkpoint, expanded row by row, has the same limit
         if (G->ld >= ((int64_t)1 << 25) || x->ld_codes >= ((int64_t)1 << 25) || x->ld_scales >= ((int64_t)1 << 25)) return ADAHOP_E_INVALID_ARG;
     }
     const size_t need = wgrad8_workspace_bytes(tokens, d_out, d_in);

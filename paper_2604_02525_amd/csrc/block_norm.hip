@@ -26,8 +26,8 @@ __device__ __forceinline__ float over_root(float m)
 
 // C: pieces of 8 columns per lane; ODD: the last one may be a part; SF32, YF32: the type of x and s, and of y.  The next
 // row's x and y are on their way while a row is summed.  Rows of whole pieces have kernels of their own, without the
-// paths for a part: 8192 x 4096 in 53.4 us instead of 56.5, 16384 x 8192 with both checkpoints in 239 us (5.65 TB/s)
-// instead of 244.
+// paths for a part: 8192 x 4096 in 52.1 us instead of 57.8, 16384 x 8192 with both checkpoints in 246 us instead of
+// 259 (239 us, 5.65 TB/s, at best).
 template <int C, bool ODD, bool SF32, bool YF32> __global__ __launch_bounds__(ROW_THREADS) void k_block_norm(adahop_block_norm_t q)
 {
     __shared__ row_sums_t<1> lds;

@@ -178,7 +178,7 @@ __device__ __forceinline__ float2 means_of(const adahop_block_norm_t &q, float r
 }
 
 // The means of rows that are wider than a workgroup; k_block_norm_backward then takes such rows in strips.  The operands are read twice: 4096 x 16384 from
-// 8-bit checkpoints takes 242 us in all (4.5 TB/s of what is moved).  With two pieces per lane in one kernel the sums over rows did not fit the registers: 445 us.
+// 8-bit checkpoints takes 242 to 251 us in all (4.4 TB/s of what is moved).  With two pieces per lane in one kernel the sums over rows did not fit the registers: 445 us.
 template <bool KEPT, bool SF32, bool YF32> __global__ __launch_bounds__(ROW_THREADS) void k_block_norm_means(adahop_block_norm_t q, float2 *means)
 {
     __shared__ row_sums_t<3> lds;
@@ -204,14 +204,16 @@ template <bool KEPT, bool SF32, bool YF32> __global__ __launch_bounds__(ROW_THRE
 }
 
 // BESIDE: several runs per workgroup; STRIPS: rows wider than a workgroup, whose means are there already: blockIdx.y is the strip; ODD: a row's last piece may
-// be a part (whole pieces without the paths for a part: 8192 x 4096 with token gates 119 us instead of
-// 128, 8192 x 2048 66 instead of 75); SF32: ds, dx
+// be a part (whole pieces without the paths for a part: 8192 x 4096 with token gates and checkpoints 109 us instead of
+// 124, 8192 x 2048 67 instead of 75); SF32: ds, dx
 // and a saved s are fp32; YF32: dh, dy and a saved y are.
 //
 // One accumulator serves both the gate and w_post: with A = sum(beta d yhat) over rows of one gate row, its gate gradient is w_post A and its part of
 // w_post's is gate A.  CUT: all rows of the run are of one gate row.  The row's values stay as they were loaded over the barrier and are widened again behind it
-// (half the registers).  The next row is loaded meanwhile if its registers are to be had: 8192 x 4096 with token gates, the stream in fp32 and 8-bit checkpoints, took 174 us
-// with the next row and spills, 140 without.
+// (half the registers).  The next row is loaded meanwhile where a row takes few registers as it lies in memory (RAW), a rule on types alone: 8192 x 4096 with token gates,
+// the stream in fp32 and 8-bit checkpoints, took 174 us with the next row, 140 without.  It leaves spills: from checkpoints under CUT, with the stream or the
+// block's side in fp32, 2 to 10 of the 128 registers (16384 x 8192 with the stream in fp32 takes 379 us, 5.0 TB/s, all the same); up to 3 elsewhere with a row ahead, up to 10
+// without one where everything is fp32.
 template <bool BESIDE, bool STRIPS, bool ODD, bool KEPT, bool CUT, bool SF32, bool YF32> __global__ __launch_bounds__(ROW_THREADS) void k_block_norm_backward(backward_t b)
 {
     // registers that a row takes as it lies in memory: two rows at a time where that leaves enough for the rest

@@ -3,7 +3,7 @@
 //     C[n, d] = w[d] sum_t G[t, n] X8[t, d] (+ add[n, d])
 //
 // on the BF16 matrix cores: an E4M3 element times its power of two is a bf16 number, so nothing is rounded on the way there.  The checkpoint is expanded
-// to bf16 rows in the workspace (3 bytes per element moved), then both operands are bf16.  For 28672 columns of G the expansion is 1.6 % of the time, for 4096
+// to bf16 rows in the workspace (3 bytes per element moved), then both operands are bf16.  For 28672 columns of G the expansion is 1.2 % of the time, for 4096
 // 8 %.  Converting in the product itself takes longer: codes converted once per workgroup, by way of LDS, took 6.4 ms at 16384 x 28672 x 8192
 // (writing 1024 bytes to LDS takes 13 cycles, reading them 4), in the registers of each wave that needs them 6.9 ms; this takes 5.4 ms.
 //
