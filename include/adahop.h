@@ -412,6 +412,76 @@ int adahop_ckpt8_wgrad(int64_t tokens, int64_t d_out, int64_t d_in, const adahop
                        const adahop_tensor_t *col_scale, const adahop_tensor_t *add, const adahop_tensor_t *C,
                        void *workspace, size_t workspace_bytes, void *stream);
 
+/* ---------------------------------------------------------------------------------------------
+ * What a training step does behind the last block: the loss over a vocabulary with its gradients, and
+ * the update of weights by orthogonalised momentum.  adahop_tensor_t as above.
+ *
+ * Softmax cross entropy of z[t, v] = logit_scale sum_d h[t, d] w[v, d] against one target per token,
+ * the logits never in memory as a whole:
+ *   lse[t] = log sum_v exp z[t, v],   loss[t] = lse[t] - z[t, target[t]] + z_loss lse[t]^2
+ *   dz[t, v] = d_loss[t] logit_scale ((1 + 2 z_loss lse[t]) exp(z[t, v] - lse[t]) - [v = target[t]])
+ *   d_h = dz w,   d_w = dz^T h (+ add)
+ *   forward   reads h, w, targets; writes loss and lse (float [tokens]; either may be NULL).
+ *   backward  reads these, lse and d_loss (float, element t at t * d_loss_stride, 0 for one that serves all; NULL: 1); writes
+ *             d_h and d_w (either may be absent).  add: what earlier micro-batches left; it may be d_w.
+ * h: bf16 [tokens, dim], w: bf16 [vocab, dim]; d_h [tokens, dim], d_w and add [vocab, dim] of either type.
+ * A token whose target is negative (padding, a prompt) has the loss 0 and no part in the gradients; a target of vocab
+ * or more makes the loss and the gradients NaN.  lse is that of all tokens.  A row of z with NaN or +infinity has the lse NaN.
+ * The products are of bf16 values with fp32 sums; dz is rounded to bf16 (by at most 2^-8 of each element) before the gradients'
+ * products, whose results are rounded once more if they are bf16.  No atomics: the same bits in every call.
+ * h and w are read in place where dim and their ld are multiples of 8 and their data 16-byte aligned, otherwise a copy of them in
+ * the workspace is.  workspace: adahop_linear_ce_workspace_bytes(p, backward) bytes (by the sizes, and h's and w's data and
+ * ld), 256-byte aligned, contents undefined on return; it holds the gradient of at most 2^29 logits, or of 256 words.
+ * Sizes: 0 <= tokens <= 2^21 (0: nothing is done, d_w = add or 0), 1 <= vocab, dim <= 2^21, each product of two of them below
+ * 2^35; ld of h and w below 2^22.  No output may overlap an input but d_w = add. */
+typedef struct {
+    int64_t tokens, vocab, dim;
+    adahop_tensor_t h, w;
+    const int64_t *targets;
+    float logit_scale, z_loss; /* finite */
+    float *loss, *lse;
+    const float *d_loss;       /* from here on: backward only */
+    int64_t d_loss_stride;
+    adahop_tensor_t d_h, d_w, add;
+} adahop_linear_ce_t;
+
+size_t adahop_linear_ce_workspace_bytes(const adahop_linear_ce_t *p, int backward);
+int adahop_linear_ce(const adahop_linear_ce_t *p, void *workspace, size_t workspace_bytes, void *stream);
+int adahop_linear_ce_backward(const adahop_linear_ce_t *p, void *workspace, size_t workspace_bytes, void *stream);
+
+/* Orthogonalisation by Newton-Schulz products:
+ *   X = U / (|U| + eps) (Frobenius norm),  `steps` times  X <- a X + (b A + c A^2) X  with A = X X^T,  result = scale X
+ * For rows > cols the same from the other side (A = X^T X).  1 <= steps <= 64; a, b, c, scale finite, eps >= 0 and finite.  The singular values of X
+ * have to stay below 4, as those of all usual coefficients do: X is held in fp32 and enters the products in fp16 (as two numbers where a side is at
+ * most 256), the diagonals of A and of b A + c A^2 stay in fp32.  The result is then within about 1e-3 of its norm of the
+ * same iteration in exact arithmetic.  A zero matrix gives zero (with eps = 0: NaN); infinities or NaN anywhere make the result NaN.
+ * Sizes: 1 <= rows, cols <= 2^16, rows * cols < 2^31.  workspace: adahop_newton_schulz_workspace_bytes(rows, cols) bytes, 256-byte aligned,
+ * contents undefined on return. */
+typedef struct {
+    int64_t rows, cols;
+    int steps;
+    float a, b, c, eps, scale;
+} adahop_newton_schulz_t;
+
+size_t adahop_newton_schulz_workspace_bytes(int64_t rows, int64_t cols);
+/* out: of either type, no part of g. */
+int adahop_orthogonalize(const adahop_newton_schulz_t *method, const adahop_tensor_t *g, const adahop_tensor_t *out, void *workspace,
+                         size_t workspace_bytes, void *stream);
+
+/* One update of a weight:
+ *   momentum_out = mu momentum + g,   U = g + mu momentum_out (nesterov) or momentum_out,   X as above
+ *   w_out = (1 - rate weight_decay) w - rate scale X,   w_bf16 = w_out rounded (where present)
+ * g: of either type.  momentum, momentum_out: float; momentum_out may be momentum.  w, w_out: of one type; w_out may be w.  w_bf16: bf16 or absent.
+ * All [rows, cols] of `method`.  rate, mu and weight_decay are finite. */
+typedef struct {
+    int64_t rows, cols;
+    adahop_tensor_t g, momentum, momentum_out, w, w_out, w_bf16;
+    float rate, mu, weight_decay;
+    int nesterov;
+} adahop_muon_t;
+
+int adahop_muon_update(const adahop_newton_schulz_t *method, const adahop_muon_t *p, void *workspace, size_t workspace_bytes, void *stream);
+
 /* hipError_t (as int) of the most recent failed HIP call on this thread, 0 if none. */
 int adahop_last_hip_error(void);
 const char *adahop_status_string(int status);

@@ -25,6 +25,8 @@ EXPORTS = ["adahop_quantize_mx", "adahop_iht_quantize", "adahop_foid_topk", "ada
            "adahop_oe_gemm_bf16", "adahop_detect_pattern_workspace_bytes", "adahop_detect_pattern",
            "adahop_ckpt8_pack", "adahop_ckpt8_unpack", "adahop_swiglu", "adahop_swiglu_backward", "adahop_block_norm",
            "adahop_block_norm_backward", "adahop_block_norm_backward_workspace_bytes", "adahop_ckpt8_wgrad", "adahop_ckpt8_wgrad_workspace_bytes",
+           "adahop_linear_ce", "adahop_linear_ce_backward", "adahop_linear_ce_workspace_bytes", "adahop_orthogonalize", "adahop_muon_update",
+           "adahop_newton_schulz_workspace_bytes",
            "adahop_select_strategy", "adahop_vote_pattern", "adahop_probe_mfma_rate", "adahop_debug_force_gemm_kernel", "adahop_debug_ckpt8_wgrad_plan", "adahop_prepare_device", "adahop_last_hip_error", "adahop_status_string",
            "adahop_abi_version"]
 
@@ -76,6 +78,21 @@ class adahop_block_norm_t(C.Structure):
                 + [("d_w_post", C.c_void_p), ("d_w_pre", C.c_void_p)])
 
 
+class adahop_linear_ce_t(C.Structure):
+    _fields_ = ([(n, C.c_int64) for n in ("tokens", "vocab", "dim")] + [(n, adahop_tensor_t) for n in ("h", "w")] + [("targets", C.c_void_p)]
+                + [(n, C.c_float) for n in ("logit_scale", "z_loss")] + [(n, C.c_void_p) for n in ("loss", "lse", "d_loss")]
+                + [("d_loss_stride", C.c_int64)] + [(n, adahop_tensor_t) for n in ("d_h", "d_w", "add")])
+
+
+class adahop_newton_schulz_t(C.Structure):
+    _fields_ = [("rows", C.c_int64), ("cols", C.c_int64), ("steps", C.c_int)] + [(n, C.c_float) for n in ("a", "b", "c", "eps", "scale")]
+
+
+class adahop_muon_t(C.Structure):
+    _fields_ = ([("rows", C.c_int64), ("cols", C.c_int64)] + [(n, adahop_tensor_t) for n in ("g", "momentum", "momentum_out", "w", "w_out", "w_bf16")]
+                + [(n, C.c_float) for n in ("rate", "mu", "weight_decay")] + [("nesterov", C.c_int)])
+
+
 _lib = None
 
 
@@ -124,6 +141,15 @@ def lib():
         L.adahop_ckpt8_wgrad.argtypes = [I64, I64, I64, TN, T8, TN, TN, TN, P, SZ, P]
         L.adahop_ckpt8_wgrad_workspace_bytes.argtypes = [I64, I64, I64]
         L.adahop_ckpt8_wgrad_workspace_bytes.restype = SZ
+        CE, NS = C.POINTER(adahop_linear_ce_t), C.POINTER(adahop_newton_schulz_t)
+        L.adahop_linear_ce.argtypes = [CE, P, SZ, P]
+        L.adahop_linear_ce_backward.argtypes = [CE, P, SZ, P]
+        L.adahop_linear_ce_workspace_bytes.argtypes = [CE, I]
+        L.adahop_linear_ce_workspace_bytes.restype = SZ
+        L.adahop_orthogonalize.argtypes = [NS, TN, TN, P, SZ, P]
+        L.adahop_muon_update.argtypes = [NS, C.POINTER(adahop_muon_t), P, SZ, P]
+        L.adahop_newton_schulz_workspace_bytes.argtypes = [I64, I64]
+        L.adahop_newton_schulz_workspace_bytes.restype = SZ
         L.adahop_select_strategy.argtypes = [I, I, I, C.POINTER(C.c_int)]
         L.adahop_vote_pattern.argtypes = [C.POINTER(C.c_int32), I]
         L.adahop_probe_mfma_rate.argtypes = [I, I, I, I, P, P]
@@ -555,3 +581,74 @@ def adahop_debug_ckpt8_wgrad_plan(tokens, d_out, d_in):
     out = [C.c_int() for _ in range(3)]
     _check(lib().adahop_debug_ckpt8_wgrad_plan(tokens, d_out, d_in, *(C.byref(v) for v in out)), "adahop_debug_ckpt8_wgrad_plan")
     return tuple(v.value for v in out)
+
+
+# ---- behind the last block: the loss over a vocabulary, updates of weights ---------------------------------------------------------
+# Tensors, workspaces and stream as above.
+
+_update_calls = None
+
+
+def _update():
+    """_call with the addresses of these operators' entry points; raises where _call.so is not built."""
+    global _update_calls
+    if _update_calls is None:
+        L = lib()
+        try:
+            from . import _call
+        except ImportError as e:
+            raise RuntimeError("_call.so is missing or stale: run `python -c 'import __graft_entry__ as g; g.build()'`") from e
+        _call.init_update(lambda: _stream(None), *(C.cast(getattr(L, "adahop_" + n), C.c_void_p).value for n in (
+            "linear_ce", "linear_ce_backward", "linear_ce_workspace_bytes", "orthogonalize", "muon_update", "newton_schulz_workspace_bytes")))
+        _update_calls = _call
+    return _update_calls
+
+
+def adahop_linear_ce(h, w, targets, logit_scale=1.0, z_loss=0.0, loss=None, lse=None, workspace=None, stream=None):
+    """Softmax cross entropy of z = logit_scale h w^T, a token's logits never in memory: loss = lse - z[target] + z_loss lse^2 with
+    lse = log sum exp z, both float32 per token.
+
+    h: bfloat16 [tokens, dim]; w: bfloat16 [vocab, dim]; targets: int64 [tokens], negative where a token has none (its loss is 0).  Returns dict(loss, lse)."""
+    status, out = _update().linear_ce(h, w, targets, logit_scale, z_loss, loss, lse, workspace, stream)
+    _check(status, "adahop_linear_ce")
+    return out
+
+
+def adahop_linear_ce_backward(h, w, targets, lse, d_loss=None, logit_scale=1.0, z_loss=0.0, d_h=None, d_w=None, add=None, want_h=True, want_w=True,
+                              d_w_bf16=False, workspace=None, stream=None):
+    """Gradients of adahop_linear_ce's h and w from that of its loss, the logits computed again a piece of the vocabulary at a time.
+
+    d_loss: float32 [tokens], dense or expanded from one number (None: ones).  d_h is bfloat16 unless it is given, d_w float32 unless d_w_bf16 or
+    d_w say otherwise; add: what d_w is added to, it may be d_w.  want_h, want_w: which are computed; the other's place is None.  Returns dict(d_h, d_w)."""
+    status, out = _update().linear_ce_backward(h, w, targets, lse, d_loss, logit_scale, z_loss, d_h, d_w, add, want_h, want_w, d_w_bf16, workspace, stream)
+    _check(status, "adahop_linear_ce_backward")
+    return out
+
+
+NEWTON_SCHULZ = (3.4445, -4.7750, 2.0315)
+
+
+def adahop_orthogonalize(g, out=None, dtype=torch.bfloat16, steps=5, coefficients=NEWTON_SCHULZ, eps=1e-7, scale=1.0, workspace=None, stream=None):
+    """scale X, X being g over its Frobenius norm (plus eps) after `steps` times X <- a X + (b A + c A^2) X with A = X X^T: with these coefficients g's
+    singular vectors with singular values of about 1.  `dtype`: of out where that is not given (bfloat16 or float32)."""
+    if dtype is not torch.bfloat16 and dtype is not torch.float32:
+        raise TypeError(f"dtype: bfloat16 or float32 wanted, not {dtype}")
+    status, out = _update().orthogonalize(g, out, dtype is torch.float32, steps, *coefficients, eps, scale, workspace, stream)
+    _check(status, "adahop_orthogonalize")
+    return out
+
+
+def adahop_muon_update(w, g, momentum, rate, mu=0.95, weight_decay=0.0, nesterov=True, scale=None, steps=5, coefficients=NEWTON_SCHULZ, eps=1e-7,
+                       w_out=None, momentum_out=None, w_bf16=None, workspace=None, stream=None):
+    """One update of the weight w from its gradient g: momentum = mu momentum + g, X the orthogonalised g + mu momentum (nesterov) or momentum, and
+    w = (1 - rate weight_decay) w - rate scale X.  scale: by default sqrt(max(1, rows / cols)).
+
+    w: float32 or bfloat16, momentum: float32, both in place unless w_out and momentum_out are given; w_bf16: where w's rounding to bfloat16 goes,
+    the next products' operand.  Returns dict(w, momentum, w_bf16)."""
+    if scale is None:
+        rows, cols = w.shape
+        scale = max(1.0, rows / max(cols, 1)) ** 0.5
+    status, out = _update().muon_update(w, g, momentum, rate, mu, weight_decay, nesterov, w_out, momentum_out, w_bf16, steps, *coefficients, eps, scale,
+                                        workspace, stream)
+    _check(status, "adahop_muon_update")
+    return out

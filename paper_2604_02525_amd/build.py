@@ -9,7 +9,8 @@ CSRC = os.path.join(HERE, "csrc")
 LIB = os.path.join(HERE, "libadahop.so")
 CALL = os.path.join(HERE, "_call.so")
 SOURCES = ["api.hip", "quantize.hip", "foid.hip", "gemm_mx.hip", "gemm_mx_dual.hip", "gemm_mx_small.hip", "oe_bf16.hip", "pattern.hip", "oht.hip", "probe.hip",
-           "api_training.hip", "ckpt8.hip", "block_norm.hip", "block_norm_backward.hip", "wgrad8.hip"]
+           "api_training.hip", "ckpt8.hip", "block_norm.hip", "block_norm_backward.hip", "wgrad8.hip",
+           "api_update.hip", "linear_ce.hip", "newton_schulz.hip"]
 FLAGS = ["-O3", "--offload-arch=gfx950", "-fPIC", "-std=c++17", "-ffp-contract=off", "-fno-gpu-rdc",
          "-Xclang", "-target-feature", "-Xclang", "-packed-fp32-ops", "-Wall", "-Wno-unused-command-line-argument"]
 
@@ -28,7 +29,7 @@ def call_command():
     root = os.path.dirname(torch.__file__)
     include = [f"-I{p}" for p in cpp_extension.include_paths() + [sysconfig.get_paths()["include"]]]
     return ([os.environ.get("CXX", "g++"), "-O2", "-std=c++17", "-fPIC", "-shared", "-Wall", f"-D_GLIBCXX_USE_CXX11_ABI={int(torch._C._GLIBCXX_USE_CXX11_ABI)}"]
-            + include + [os.path.join(CSRC, "call.cpp"), os.path.join(CSRC, "call_training.cpp"), "-o", CALL, "-L" + os.path.join(root, "lib"), "-ltorch_python", "-ltorch_cpu", "-lc10"])
+            + include + [os.path.join(CSRC, "call.cpp"), os.path.join(CSRC, "call_training.cpp"), os.path.join(CSRC, "call_update.cpp"), "-o", CALL, "-L" + os.path.join(root, "lib"), "-ltorch_python", "-ltorch_cpu", "-lc10"])
 
 
 def build(verbose: bool = False) -> str:

@@ -170,6 +170,7 @@ PyModuleDef module = {PyModuleDef_HEAD_INIT, "_call", nullptr, -1, methods, null
 } // namespace
 
 int add_training_calls(PyObject *module); // call_training.cpp
+int add_update_calls(PyObject *module);   // call_update.cpp
 
 PyMODINIT_FUNC PyInit__call(void)
 {
@@ -180,7 +181,7 @@ PyMODINIT_FUNC PyInit__call(void)
     for (const auto &x : names)
         if (!(*x.name = PyUnicode_InternFromString(x.text))) return nullptr;
     PyObject *const m = PyModule_Create(&module);
-    if (m && add_training_calls(m) < 0) {
+    if (m && (add_training_calls(m) < 0 || add_update_calls(m) < 0)) {
         Py_DECREF(m);
         return nullptr;
     }

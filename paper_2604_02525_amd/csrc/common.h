@@ -38,6 +38,8 @@ int configure_oht();
 int configure_foid();
 int configure_iht_quantize();
 int configure_wgrad8();
+int configure_linear_ce();
+int configure_newton_schulz();
 
 // Launchers (one per kernel family); each validates nothing and returns a status.
 // Stage-major copy of the scales for the tiled GEMM kernels [ceil(K/256)][rows][8].
@@ -190,6 +192,15 @@ size_t wgrad8_workspace_bytes(int64_t tokens, int64_t d_out, int64_t d_in);
 void wgrad8_plan(int64_t tokens, int64_t d_out, int64_t d_in, int *tile, int *shares, int *slices);
 int launch_wgrad8(int64_t tokens, int64_t d_out, int64_t d_in, const adahop_tensor_t &G, const adahop_ckpt8_t &x, const adahop_tensor_t &col_scale,
                   const adahop_tensor_t &add, const adahop_tensor_t &C, void *workspace, hipStream_t st);
+
+// The loss over a vocabulary, and updates of weights by Newton-Schulz products.
+size_t linear_ce_workspace_bytes(const adahop_linear_ce_t &q, bool backward); // by sizes, and by whether h and w are taken as they lie
+int launch_linear_ce(const adahop_linear_ce_t &q, void *workspace, hipStream_t st);
+int launch_linear_ce_backward(const adahop_linear_ce_t &q, void *workspace, hipStream_t st);
+int launch_linear_ce_no_tokens(const adahop_linear_ce_t &q, hipStream_t st); // d_w = add, or 0
+size_t newton_schulz_workspace_bytes(int64_t rows, int64_t cols);
+// out: the result; u: the update of a weight instead (g is its gradient).
+int launch_newton_schulz(const adahop_newton_schulz_t &m, const adahop_tensor_t &g, const adahop_tensor_t &out, const adahop_muon_t *u, void *workspace, hipStream_t st);
 
 // One-time set-up per device (function attributes, device properties): the only state the library keeps.
 // need(dev) is true until mark(dev) has been called for that device; devices numbered 64 and above are set

@@ -1,0 +1,416 @@
+// Softmax cross entropy over a vocabulary, from the last hidden states and the output weights, without the logits in memory:
+//
+//     z[t, v] = logit_scale sum_d h[t, d] w[v, d],   lse[t] = log sum_v exp z[t, v],   loss[t] = lse - z[t, y_t] + z_loss lse^2
+//     dz[t, v] = d_loss[t] logit_scale ((1 + 2 z_loss lse) exp(z - lse) - [v = y_t]),   d_h = dz w,   d_w = dz^T h
+//
+// Backward, the tokens that have a target are gathered first: the others take no part in either gradient, whatever they hold, and cost nothing.
+//
+// Forward: a tile of z (words of the vocabulary by tokens) stays in the matrix cores' accumulators and leaves two numbers per token, its largest logit and
+// the sum of exponentials relative to that; a second kernel joins the tiles of a token.  Backward: a piece of the vocabulary at a time, z is
+// computed again, dz of the piece goes to the workspace in bf16 and enters both gradients' products.
+//
+// The rounding of dz to bf16 (each element by at most 2^-8 of itself) is what the matrix cores take; it is of the size of the gradients' own rounding and, as
+// errors of the elements are independent, adds less than that to a sum over them.  Where all tokens have one d_loss (that of a mean), it and logit_scale are left out of
+// dz and multiply the products' fp32 sums: the target's element, mostly the largest of its row, is then -1 and little more, which loses next to nothing (8192 x 4096 x 32000: d_h 2.6e-3
+// of its norm off with them inside).  All sums, lse and the loss are fp32.
+#include <math.h>
+
+#include "row_sums.h"
+#include "tile16.h"
+
+namespace adahop {
+
+namespace {
+
+struct loss_t {
+    const int64_t *targets;
+    int64_t T, V;
+    float logit_scale, z_loss;
+};
+
+// ---- forward --------------------------------------------------------------------------------------------------------------------
+struct stats_t {
+    loss_t p;
+    float2 *part; // [T][tiles of the vocabulary]: largest logit, sum of exponentials relative to it
+    float *at;    // [T]: the target's logit
+};
+
+template <int MASK> __device__ __forceinline__ float across(float v) { return __shfl_xor(v, MASK); }
+
+// A: w (rows of a tile: words), B: h (columns: tokens).  A lane has one token per 16 columns and a quarter of the tile's words of its wave: most of a token's
+// maximum and sum are formed in its registers.
+template <class K> __global__ __launch_bounds__(K::THREADS, 2) void k_ce_stats(product_t q, stats_t e)
+{
+    extern __shared__ __attribute__((aligned(1024))) uint8_t smem[];
+    int64_t n0, d0;
+    place_of<K, false>(q, n0, d0);
+    v4f acc[K::MT][K::NT];
+    multiply<K, false, ALONG, ALONG, false>(q, n0, d0, 0, q.K, smem, acc);
+    wait_for_copies<0>();
+    __syncthreads();
+    float2 *const of_wave = reinterpret_cast<float2 *>(smem); // [WN][TN]
+    const int lane = threadIdx.x & 63, w = threadIdx.x >> 6, wn = w / K::WD, wd = w % K::WD;
+    const int first = (int)(e.p.V - n0 < K::TM ? e.p.V - n0 : K::TM) - wn * K::MT * 16 - 4 * (lane >> 4); // words of this lane's from its first on, below its rows' count
+#pragma unroll
+    for (int n = 0; n < K::NT; ++n) {
+        const int64_t t = d0 + (wd * K::NT + n) * 16 + (lane & 15);
+        const int64_t y = t < q.B.outer ? e.p.targets[t] - n0 - wn * K::MT * 16 - 4 * (lane >> 4) : -1;
+        const int mine = y >= 0 && y < K::MT * 16 ? (int)y : -1; // the target as a row of this lane's, if it is one
+        float top = -INFINITY, sum = 0.0f, at = 0.0f;
+        bool is = false;
+#pragma unroll
+        for (int m = 0; m < K::MT; ++m)
+#pragma unroll
+            for (int i = 0; i < 4; ++i) {
+                const float z = acc[m][n][i] * e.p.logit_scale;
+                acc[m][n][i] = m * 16 + i < first ? z : -INFINITY;
+                top = fmaxf(top, acc[m][n][i]);
+                at = mine == m * 16 + i ? z : at;
+                is |= mine == m * 16 + i;
+            }
+        top = fmaxf(top, across<16>(top));
+        top = fmaxf(top, across<32>(top));
+        const float from = top == -INFINITY ? 0.0f : top;
+#pragma unroll
+        for (int m = 0; m < K::MT; ++m)
+#pragma unroll
+            for (int i = 0; i < 4; ++i) sum += __expf(acc[m][n][i] - from);
+        sum += across<16>(sum);
+        sum += across<32>(sum);
+        if (is) e.at[t] = at;
+        if (lane < 16) of_wave[wn * K::TN + (wd * K::NT + n) * 16 + lane] = make_float2(top, sum);
+    }
+    __syncthreads();
+    for (int i = threadIdx.x; i < K::TN; i += K::THREADS) {
+        if (d0 + i >= q.B.outer) break;
+        float2 s = of_wave[i];
+#pragma unroll
+        for (int k = 1; k < K::WN; ++k) {
+            const float2 o = of_wave[k * K::TN + i];
+            const float top = fmaxf(s.x, o.x), from = top == -INFINITY ? 0.0f : top;
+            s = make_float2(top, s.y * __expf(s.x - from) + o.y * __expf(o.x - from));
+        }
+        e.part[(d0 + i) * q.nt + n0 / K::TM] = s;
+    }
+}
+
+// One wave per token: its tiles' numbers joined, the loss.
+__global__ __launch_bounds__(256) void k_ce_join(loss_t p, const float2 *part, const float *at, int tiles, float *loss, float *lse)
+{
+    const int64_t t = (int64_t)blockIdx.x * 4 + (threadIdx.x >> 6);
+    const int lane = threadIdx.x & 63;
+    if (t >= p.T) return;
+    float top = -INFINITY, sum = 0.0f;
+    for (int i = lane; i < tiles; i += 64) {
+        const float2 s = part[t * tiles + i];
+        const float to = fmaxf(top, s.x), from = to == -INFINITY ? 0.0f : to;
+        sum = sum * __expf(top - from) + s.y * __expf(s.x - from);
+        top = to;
+    }
+    float most = top;
+#pragma unroll
+    for (int k = 1; k < 64; k *= 2) most = fmaxf(most, __shfl_xor(most, k));
+    const float from = most == -INFINITY ? 0.0f : most;
+    sum = sum64(sum * __expf(top - from));
+    if (lane) return;
+    const float l = from + logf(sum);
+    const int64_t y = p.targets[t];
+    if (lse) lse[t] = l;
+    if (loss) loss[t] = y < 0 ? 0.0f : y < p.V ? l - at[t] + p.z_loss * l * l : NAN;
+}
+
+// ---- backward -------------------------------------------------------------------------------------------------------------------
+// dz of a piece of the vocabulary from its logits (rows: tokens, columns: words from v0 on), rounded to bf16; zeros from the piece's end to the row's.
+struct dlogits_t {
+    static constexpr bool COUNTED = true;
+    loss_t p;
+    const int32_t *token; // of each row
+    const float *lse, *d_loss;
+    int64_t d_loss_stride, v0, words, ld;
+    float factor; // in dz: logit_scale, or 1 where it comes later
+    uint16_t *dz;
+    struct more_t {
+        float lse, gain; // gain: what exp(z - lse) - [v = y] is multiplied by
+        int64_t y;
+    };
+    __device__ __forceinline__ more_t get(int64_t r, int64_t, int) const
+    {
+        const int64_t t = token[r], y = p.targets[t];
+        const float g = (d_loss ? d_loss[t * d_loss_stride] : 1.0f) * factor;
+        return {lse[t], y < p.V ? g : NAN, y};
+    }
+    __device__ __forceinline__ float4 apply(int64_t r, int64_t c, int have, float4 v, const more_t &m) const
+    {
+        const float z[4] = {v.x, v.y, v.z, v.w}, s = 1.0f + 2.0f * p.z_loss * m.lse;
+        const int64_t hit = m.y - v0 - c;
+        float d[4];
+#pragma unroll
+        for (int i = 0; i < 4; ++i) {
+            d[i] = (s * __expf(z[i] * p.logit_scale - m.lse) - (hit == i ? 1.0f : 0.0f)) * m.gain;
+            if (i >= have) d[i] = 0.0f;
+        }
+        uint16_t *const to = dz + r * ld + c; // 8-byte aligned
+        *reinterpret_cast<u32x2 *>(to) = u32x2{bf16_pair(d[0], d[1]), bf16_pair(d[2], d[3])};
+        if (c + 4 >= words && c + 4 < ld) *reinterpret_cast<u32x2 *>(to + 4) = u32x2{0, 0}; // rows are whole pieces of eight
+        return v;
+    }
+};
+
+// An operand of rows that a copy to LDS cannot take as they are, laid out anew: rows of whole pieces of eight, zeros behind their end.
+__global__ __launch_bounds__(256) void k_lay_out(adahop_tensor_t x, int64_t rows, int64_t cols, uint16_t *out, int64_t ld)
+{
+    const int64_t pieces = ld / 8, all = rows * pieces;
+    for (int64_t i = (int64_t)blockIdx.x * 256 + threadIdx.x; i < all; i += (int64_t)gridDim.x * 256) {
+        const int64_t r = i / pieces, c = (i - r * pieces) * 8;
+        const raw8<false> v = load8<false>(x.data, r * x.ld + c, (int)(cols - c < 8 ? cols - c : 8));
+        *reinterpret_cast<u32x4 *>(out + r * ld + c) = v.w[0];
+    }
+}
+
+// Which tokens have a target, in their order, and how many: one workgroup, 8192 tokens at a time.
+__global__ __launch_bounds__(1024) void k_ce_tokens(const int64_t *targets, int64_t T, int32_t *token, int32_t *count)
+{
+    constexpr int EACH = 8;
+    __shared__ int of_wave[16];
+    const int lane = threadIdx.x & 63, w = threadIdx.x >> 6;
+    int before = 0; // found so far
+    for (int64_t from = 0; from < T; from += 1024 * EACH) {
+        const int64_t t = from + threadIdx.x * EACH;
+        uint32_t has = 0;
+#pragma unroll
+        for (int i = 0; i < EACH; ++i) has |= (uint32_t)(t + i < T && targets[t + i] >= 0) << i;
+        const int mine = __popc(has);
+        int sum = mine; // of this lane and those before it
+#pragma unroll
+        for (int k = 1; k < 64; k *= 2) {
+            const int o = __shfl_up(sum, k);
+            sum += lane >= k ? o : 0;
+        }
+        if (lane == 63) of_wave[w] = sum;
+        __syncthreads();
+        int at = before + sum - mine, all = 0;
+#pragma unroll
+        for (int i = 0; i < 16; ++i) {
+            at += i < w ? of_wave[i] : 0;
+            all += of_wave[i];
+        }
+#pragma unroll
+        for (int i = 0; i < EACH; ++i)
+            if (has >> i & 1) token[at++] = (int32_t)(t + i);
+        before += all;
+        __syncthreads();
+    }
+    if (threadIdx.x == 0) *count = before;
+}
+
+// h's rows of these tokens, one after the other.  A workgroup has a row; those past the last token's have nothing to do.
+__global__ __launch_bounds__(256) void k_gather(adahop_tensor_t x, int64_t cols, const int32_t *token, const int32_t *count, uint16_t *out, int64_t ld)
+{
+    const int64_t r = blockIdx.x;
+    if (r >= *count) return;
+    const int64_t from = (int64_t)token[r] * x.ld;
+    for (int64_t c = threadIdx.x * 8; c < ld; c += 256 * 8) {
+        const raw8<false> v = load8<false>(x.data, from + c, (int)(cols - c < 8 ? cols - c : 8));
+        *reinterpret_cast<u32x4 *>(out + r * ld + c) = v.w[0];
+    }
+}
+
+// d_h of the tokens without a target.
+__global__ __launch_bounds__(256) void k_ce_zeros(const int64_t *targets, int64_t cols, adahop_tensor_t out)
+{
+    const int64_t t = blockIdx.x;
+    if (targets[t] >= 0) return;
+    const float zero[8] = {};
+    for (int64_t c = threadIdx.x * 8; c < cols; c += 256 * 8) store8_any(out, t * out.ld + c, (int)(cols - c < 8 ? cols - c : 8), zero);
+}
+
+// ---- host -----------------------------------------------------------------------------------------------------------------------
+constexpr int64_t PIECE_BYTES = (int64_t)1 << 30; // of dz in the workspace, at most (one word's column however long)
+
+bool copies_as_it_is(const adahop_tensor_t &x, int64_t cols) { return aligned(x.data, 16) && x.ld % 8 == 0 && cols % 8 == 0; }
+
+struct forward_plan_t {
+    int64_t tiles;
+    bool large;
+    size_t part, at, h, w, total;
+};
+
+struct backward_plan_t {
+    int64_t words, pieces, ld; // of a piece of the vocabulary
+    size_t dz, sum_h, part, count, token, h, w, total;
+};
+
+bool large_tiles(int64_t T, int64_t V) { return ceil_div(T, 256) * ceil_div(V, 256) >= 256; }
+
+// lay_h, lay_w: the operand is laid out anew
+forward_plan_t forward_plan(int64_t T, int64_t V, int64_t D, bool lay_h, bool lay_w)
+{
+    forward_plan_t p;
+    p.large = large_tiles(T, V);
+    p.tiles = ceil_div(V, p.large ? tile256_t::TM : tile128_t::TM);
+    const size_t ld = align_up(D, 8) * 2;
+    p.part = 0;
+    p.at = align_up((size_t)T * p.tiles * sizeof(float2), 256);
+    p.h = align_up(p.at + T * sizeof(float), 256);
+    p.w = align_up(p.h + (lay_h ? T * ld : 0), 256);
+    p.total = align_up(p.w + (lay_w ? V * ld : 0), 256);
+    return p;
+}
+
+size_t most(size_t a, size_t b) { return a > b ? a : b; }
+
+backward_plan_t backward_plan(int64_t T, int64_t V, int64_t D, bool lay_w)
+{
+    backward_plan_t p;
+    const int64_t fit = PIECE_BYTES / 2 / T / 256 * 256, each = fit < 256 ? 256 : fit;
+    p.pieces = ceil_div(V, each);
+    p.words = p.pieces == 1 ? V : align_up(ceil_div(V, p.pieces), 256);
+    p.pieces = ceil_div(V, p.words);
+    p.ld = align_up(p.words, 8);
+    const size_t ld = align_up(D, 8) * 2;
+    const int64_t rest = V - (p.pieces - 1) * p.words;
+    size_t part = 0;
+    for (const int64_t words : {p.words, rest}) part = most(part, most(plan16(T, D, words, false).part_bytes, plan16(words, D, T, false).part_bytes));
+    p.dz = 0;
+    p.sum_h = align_up((size_t)T * p.ld * 2, 256);
+    p.part = align_up(p.sum_h + (p.pieces > 1 ? (size_t)T * D * sizeof(float) : 0), 256);
+    p.count = align_up(p.part + part, 256);
+    p.token = p.count + 256;
+    p.h = align_up(p.token + T * sizeof(int32_t), 256);
+    p.w = align_up(p.h + T * ld, 256);
+    p.total = align_up(p.w + (lay_w ? V * ld : 0), 256);
+    return p;
+}
+
+device_once_t g_once;
+
+template <class K> int launch_stats(product_t &q, const stats_t &e, hipStream_t st)
+{
+    q.nt = (uint32_t)ceil_div(q.A.outer, K::TM), q.dt = (uint32_t)ceil_div(q.B.outer, K::TN);
+    k_ce_stats<K><<<q.nt * q.dt, K::THREADS, K::LDS, st>>>(q, e);
+    return check_launch();
+}
+
+// h or w as the products take it: itself, or a copy at `to`.
+int lay_out(const adahop_tensor_t &x, int64_t rows, int64_t cols, bool anew, void *to, side_t *out, hipStream_t st)
+{
+    if (!anew) {
+        *out = {static_cast<const uint16_t *>(x.data), x.ld, rows};
+        return ADAHOP_OK;
+    }
+    const int64_t ld = align_up(cols, 8), blocks = ceil_div(rows * (ld / 8), 256);
+    *out = {static_cast<const uint16_t *>(to), ld, rows};
+    k_lay_out<<<(unsigned)(blocks < 16384 ? blocks : 16384), 256, 0, st>>>(x, rows, cols, static_cast<uint16_t *>(to), ld);
+    return check_launch();
+}
+
+} // namespace
+
+int configure_linear_ce()
+{
+    int dev = 0;
+    int rc = check_hip(hipGetDevice(&dev));
+    if (rc != ADAHOP_OK || !g_once.need(dev)) return rc;
+    rc = check_hip(hipFuncSetAttribute(reinterpret_cast<const void *>(&k_ce_stats<tile256_t>), hipFuncAttributeMaxDynamicSharedMemorySize, tile256_t::LDS));
+    if (rc == ADAHOP_OK) rc = check_hip(hipFuncSetAttribute(reinterpret_cast<const void *>(&k_ce_stats<tile128_t>), hipFuncAttributeMaxDynamicSharedMemorySize, tile128_t::LDS));
+    if (rc == ADAHOP_OK) rc = configure_both16<false, ALONG, ALONG, false, false, dlogits_t>();
+    if (rc == ADAHOP_OK) rc = configure_both16<false, DOWN, DOWN, false, false, grad_t>();
+    if (rc == ADAHOP_OK) rc = configure_both16<false, ALONG, DOWN, false, false, grad_t>();
+    if (rc == ADAHOP_OK) g_once.mark(dev);
+    return rc;
+}
+
+size_t linear_ce_workspace_bytes(const adahop_linear_ce_t &q, bool backward)
+{
+    const bool lay_h = !copies_as_it_is(q.h, q.dim), lay_w = !copies_as_it_is(q.w, q.dim);
+    return backward ? backward_plan(q.tokens, q.vocab, q.dim, lay_w).total : forward_plan(q.tokens, q.vocab, q.dim, lay_h, lay_w).total;
+}
+
+int launch_linear_ce(const adahop_linear_ce_t &c, void *workspace, hipStream_t st)
+{
+    int rc = configure_linear_ce();
+    if (rc != ADAHOP_OK) return rc;
+    const bool lay_h = !copies_as_it_is(c.h, c.dim), lay_w = !copies_as_it_is(c.w, c.dim);
+    const forward_plan_t p = forward_plan(c.tokens, c.vocab, c.dim, lay_h, lay_w);
+    char *const ws = static_cast<char *>(workspace);
+    product_t q = {};
+    if ((rc = lay_out(c.w, c.vocab, c.dim, lay_w, ws + p.w, &q.A, st)) != ADAHOP_OK) return rc;
+    if ((rc = lay_out(c.h, c.tokens, c.dim, lay_h, ws + p.h, &q.B, st)) != ADAHOP_OK) return rc;
+    q.K = align_up(c.dim, 8);
+    const stats_t e = {{c.targets, c.tokens, c.vocab, c.logit_scale, c.z_loss}, reinterpret_cast<float2 *>(ws + p.part), reinterpret_cast<float *>(ws + p.at)};
+    rc = p.large ? launch_stats<tile256_t>(q, e, st) : launch_stats<tile128_t>(q, e, st);
+    if (rc != ADAHOP_OK) return rc;
+    k_ce_join<<<(unsigned)ceil_div(c.tokens, 4), 256, 0, st>>>(e.p, e.part, e.at, (int)p.tiles, c.loss, c.lse);
+    return check_launch();
+}
+
+int launch_linear_ce_backward(const adahop_linear_ce_t &c, void *workspace, hipStream_t st)
+{
+    int rc = configure_linear_ce();
+    if (rc != ADAHOP_OK) return rc;
+    const bool lay_w = !copies_as_it_is(c.w, c.dim);
+    const int64_t T = c.tokens, V = c.vocab, D = c.dim, ldh = align_up(D, 8);
+    const backward_plan_t p = backward_plan(T, V, D, lay_w);
+    char *const ws = static_cast<char *>(workspace);
+    int32_t *const count = reinterpret_cast<int32_t *>(ws + p.count), *const token = reinterpret_cast<int32_t *>(ws + p.token);
+    uint16_t *const dz = reinterpret_cast<uint16_t *>(ws + p.dz), *const h = reinterpret_cast<uint16_t *>(ws + p.h);
+    side_t w;
+    if ((rc = lay_out(c.w, V, D, lay_w, ws + p.w, &w, st)) != ADAHOP_OK) return rc;
+    k_ce_tokens<<<1, 1024, 0, st>>>(c.targets, T, token, count);
+    if ((rc = check_launch()) != ADAHOP_OK) return rc;
+    k_gather<<<(unsigned)T, 256, 0, st>>>(c.h, D, token, count, h, ldh);
+    if ((rc = check_launch()) != ADAHOP_OK) return rc;
+    if (c.d_h.data) {
+        k_ce_zeros<<<(unsigned)T, 256, 0, st>>>(c.targets, D, c.d_h);
+        if ((rc = check_launch()) != ADAHOP_OK) return rc;
+    }
+    const adahop_tensor_t none = {}, sum_h = {ws + p.sum_h, D, 1};
+    const bool one = !c.d_loss || c.d_loss_stride == 0; // for all tokens
+    const float factor = one ? c.logit_scale : 1.0f;
+    const float *const by = one ? c.d_loss : nullptr;
+    for (int64_t i = 0; i < p.pieces; ++i) {
+        const int64_t v0 = i * p.words, words = V - v0 < p.words ? V - v0 : p.words, ld = align_up(words, 8);
+        const side_t piece = {w.data + v0 * w.ld, w.ld, words};
+        product_t q = {};
+        q.A = {h, ldh, T}, q.B = piece, q.K = ldh;
+        q.rows_of = count;
+        const dlogits_t e = {{c.targets, T, V, c.logit_scale, c.z_loss}, token, c.lse, one ? nullptr : c.d_loss, c.d_loss_stride, v0, words, ld, one ? 1.0f : c.logit_scale, dz};
+        plan16_t plan = plan16(T, words, q.K, false);
+        if (plan.slices > 1) plan.large = false, plan.slices = 1, plan.slice = align_up(q.K, 64);
+        if ((rc = launch_product16<false, ALONG, ALONG, false, false>(plan, q, e, nullptr, st)) != ADAHOP_OK) return rc;
+        if (c.d_w.data) {
+            const int64_t size = c.d_w.f32 ? 4 : 2, size_add = c.add.f32 ? 4 : 2;
+            q.A = {dz, ld, words}, q.B = {h, ldh, D}, q.K = T;
+            q.rows_of = nullptr, q.K_of = count;
+            const grad_t g = {{static_cast<char *>(c.d_w.data) + v0 * c.d_w.ld * size, c.d_w.ld, c.d_w.f32},
+                              c.add.data ? adahop_tensor_t{static_cast<char *>(c.add.data) + v0 * c.add.ld * size_add, c.add.ld, c.add.f32} : none, nullptr, factor, by};
+            if ((rc = launch_product16<false, DOWN, DOWN, false, false>(plan16(words, D, T, false), q, g, ws + p.part, st)) != ADAHOP_OK) return rc;
+        }
+        if (c.d_h.data) {
+            const bool end = i + 1 == p.pieces;
+            q.A = {dz, ld, T}, q.B = {piece.data, piece.ld, D}, q.K = words;
+            q.rows_of = count, q.K_of = nullptr;
+            const grad_t g = {end ? c.d_h : sum_h, i ? sum_h : none, end ? token : nullptr, factor, by};
+            if ((rc = launch_product16<false, ALONG, DOWN, false, false>(plan16(T, D, words, false), q, g, ws + p.part, st)) != ADAHOP_OK) return rc;
+        }
+    }
+    return ADAHOP_OK;
+}
+
+// d_w = add, or 0, where there are no tokens.
+__global__ __launch_bounds__(256) void k_ce_no_tokens(adahop_tensor_t to, adahop_tensor_t add, int64_t rows, int64_t cols)
+{
+    const int64_t c = ((int64_t)blockIdx.y * 64 + (threadIdx.x & 63)) * 4, r = (int64_t)blockIdx.x * 4 + (threadIdx.x >> 6);
+    if (c >= cols || r >= rows) return;
+    const int have = (int)(cols - c < 4 ? cols - c : 4);
+    const float one[4] = {1.0f, 1.0f, 1.0f, 1.0f};
+    put4(to, r, c, have, one, make_float4(0.0f, 0.0f, 0.0f, 0.0f), get4(add, r, c, have));
+}
+
+int launch_linear_ce_no_tokens(const adahop_linear_ce_t &c, hipStream_t st)
+{
+    k_ce_no_tokens<<<dim3((unsigned)ceil_div(c.vocab, 4), (unsigned)ceil_div(c.dim, 256)), 256, 0, st>>>(c.d_w, c.add, c.vocab, c.dim);
+    return check_launch();
+}
+
+} // namespace adahop

@@ -1,0 +1,466 @@
+// Orthogonalisation of a matrix by Newton-Schulz products, and the update of a weight by it:
+//
+//     X = U / (|U| + eps),   repeat `steps` times:  A = X X^T,  X <- a X + (b A + c A^2) X,   out = scale X
+//
+// (for a matrix of more rows than columns A = X^T X, from the other side).  U is the matrix given, or for an update of a weight its gradient with momentum:
+// m' = mu m + g, U = g + mu m' (nesterov) or m', w' = (1 - rate decay) w - rate scale X.
+//
+// The singular values of X pass through a x + b x^3 + c x^5 in every step, and with them what rounding adds: directions that are weak at first grow by a factor of a.
+// Plain 16-bit iterates lose them (bf16: 1 to 15 % of the result).  What this does instead, each product still being one pass of 16-bit operands:
+//   * X is carried in fp32; only what enters the products is rounded, to fp16 (times a power of two), so that a X is exact.
+//   * The diagonals of A and of b A + c A^2 are apart, in fp32: they are by far the largest elements, their rounding would be the largest error.  With A = D + O:
+//     the polynomial is b (D + O) + c (D^2 + D O + O D + O^2), of which the matrix cores form O^2, and its diagonal joins a in what multiplies the carried X.
+//   * Where the smaller side is at most 256, X enters as the sum of two fp16 numbers: errors there average over fewer elements, and the products cost little.
+// The result is then 2e-4 to 1e-3 of its norm off the same iteration in 64 bits (bf16's own rounding: 1.7e-3).
+//
+// A and A^2 are symmetric: only tiles on and below the diagonal are computed, the mirror image is stored with them.
+#include <math.h>
+
+#include "tile16.h"
+
+namespace adahop {
+
+namespace {
+
+constexpr int SX = 12, SO = 12, SB = 10; // X, O and the polynomial's off-diagonal part are held times 2^S in fp16: below 16, 16 and 64
+constexpr int PARTS = 1024;              // workgroups of the sum of squares, at most
+constexpr int SPLIT_SIDE = 256;
+
+constexpr float pow2(int e) { return e >= 0 ? (float)((uint64_t)1 << e) : 1.0f / (float)((uint64_t)1 << -e); }
+
+__device__ __forceinline__ uint32_t f16_pair(float a, float b) // round to nearest even
+{
+    typedef _Float16 v2h __attribute__((ext_vector_type(2)));
+    const v2h p = {(_Float16)a, (_Float16)b};
+    return __builtin_bit_cast(uint32_t, p);
+}
+__device__ __forceinline__ u32x2 f16_four(const float (&v)[4]) { return u32x2{f16_pair(v[0], v[1]), f16_pair(v[2], v[3])}; }
+__device__ __forceinline__ void f16_values(u32x2 w, float (&v)[4])
+{
+    typedef _Float16 v4h __attribute__((ext_vector_type(4)));
+    const v4h h = __builtin_bit_cast(v4h, w);
+#pragma unroll
+    for (int i = 0; i < 4; ++i) v[i] = (float)h[i];
+}
+__device__ __forceinline__ void store_eight(uint16_t *to, const float (&v)[8])
+{
+    *reinterpret_cast<u32x4 *>(to) = u32x4{f16_pair(v[0], v[1]), f16_pair(v[2], v[3]), f16_pair(v[4], v[5]), f16_pair(v[6], v[7])};
+}
+
+// ---- before the products ----------------------------------------------------------------------------------------------------------
+struct source_t {
+    adahop_tensor_t g, m, m_out; // m, m_out: absent without momentum
+    float mu;
+    int nesterov;
+    int64_t rows, cols;
+};
+
+// n <= 8 elements of U from (r, c) on, zeros behind them; with momentum from what it has become.
+__device__ __forceinline__ void u_at(const source_t &s, const adahop_tensor_t &m, int64_t r, int64_t c, int n, bool advance, float (&u)[8])
+{
+    load8_any(s.g, r * s.g.ld + c, n, u);
+    if (!m.data) return;
+    float v[8];
+    load8_any(m, r * m.ld + c, n, v);
+#pragma unroll
+    for (int i = 0; i < 8; ++i) {
+        if (advance) v[i] = s.mu * v[i] + u[i];
+        u[i] = s.nesterov ? u[i] + s.mu * v[i] : v[i];
+    }
+    if (advance) store8_any(s.m_out, r * s.m_out.ld + c, n, v);
+}
+
+// The momentum's step, and sums of U's squares, in 64 bits: no element is too large or too small for them.
+__global__ __launch_bounds__(256) void k_squares(source_t s, double *part)
+{
+    __shared__ double of_wave[4];
+    const int64_t pieces = (s.cols + 7) / 8, all = s.rows * pieces;
+    double sum = 0.0;
+    for (int64_t i = (int64_t)blockIdx.x * 256 + threadIdx.x; i < all; i += (int64_t)gridDim.x * 256) {
+        const int64_t r = i / pieces, c = (i - r * pieces) * 8;
+        float u[8];
+        u_at(s, s.m, r, c, (int)(s.cols - c < 8 ? s.cols - c : 8), true, u);
+#pragma unroll
+        for (int k = 0; k < 8; ++k) sum += (double)u[k] * u[k];
+    }
+#pragma unroll
+    for (int k = 1; k < 64; k *= 2) sum += __shfl_xor(sum, k);
+    if ((threadIdx.x & 63) == 0) of_wave[threadIdx.x >> 6] = sum;
+    __syncthreads();
+    if (threadIdx.x == 0) part[blockIdx.x] = of_wave[0] + of_wave[1] + of_wave[2] + of_wave[3];
+}
+
+// Where the iterates are held: [rows_pad][ld], both multiples of 32, zeros outside the matrix.
+struct iterate_t {
+    float *x;
+    uint16_t *h; // fp16 of x 2^SX; split: what that leaves, in the same scale, `low` elements further on
+    int64_t ld, low; // low = 0: not split
+};
+
+__device__ __forceinline__ void put_half(const iterate_t &t, int64_t at, const float (&v)[4])
+{
+    float s[4], back[4];
+#pragma unroll
+    for (int i = 0; i < 4; ++i) s[i] = v[i] * pow2(SX);
+    const u32x2 h = f16_four(s);
+    *reinterpret_cast<u32x2 *>(t.h + at) = h;
+    if (!t.low) return;
+    f16_values(h, back);
+#pragma unroll
+    for (int i = 0; i < 4; ++i) s[i] -= back[i];
+    *reinterpret_cast<u32x2 *>(t.h + t.low + at) = f16_four(s);
+}
+
+// The first iterate: U over its norm.
+__global__ __launch_bounds__(256) void k_first(source_t s, const double *part, int parts, float eps, iterate_t to, int64_t rows_pad)
+{
+    __shared__ double of_wave[4];
+    double sum = 0.0;
+    for (int i = threadIdx.x; i < parts; i += 256) sum += part[i];
+#pragma unroll
+    for (int k = 1; k < 64; k *= 2) sum += __shfl_xor(sum, k);
+    if ((threadIdx.x & 63) == 0) of_wave[threadIdx.x >> 6] = sum;
+    __syncthreads();
+    const double inverse = 1.0 / (sqrt(of_wave[0] + of_wave[1] + of_wave[2] + of_wave[3]) + eps);
+    const int64_t pieces = to.ld / 8, all = rows_pad * pieces;
+    for (int64_t i = (int64_t)blockIdx.x * 256 + threadIdx.x; i < all; i += (int64_t)gridDim.x * 256) {
+        const int64_t r = i / pieces, c = (i - r * pieces) * 8;
+        const int n = r < s.rows ? (int)(s.cols - c < 8 ? s.cols - c : 8) : 0;
+        float u[8] = {};
+        if (n > 0) u_at(s, s.m_out, r, c, n, false, u);
+        float lo[4], hi[4];
+#pragma unroll
+        for (int k = 0; k < 4; ++k) {
+            lo[k] = k < n ? (float)(u[k] * inverse) : 0.0f;
+            hi[k] = k + 4 < n ? (float)(u[k + 4] * inverse) : 0.0f;
+        }
+        const int64_t at = r * to.ld + c;
+        *reinterpret_cast<float4 *>(to.x + at) = make_float4(lo[0], lo[1], lo[2], lo[3]);
+        *reinterpret_cast<float4 *>(to.x + at + 4) = make_float4(hi[0], hi[1], hi[2], hi[3]);
+        put_half(to, at, lo);
+        put_half(to, at + 4, hi);
+    }
+}
+
+// ---- what becomes of the products ---------------------------------------------------------------------------------------------------
+// X X^T: its diagonal, and the rest in fp16.
+struct gram_t {
+    static constexpr bool COUNTED = false;
+    typedef nothing_t more_t;
+    uint16_t *O;
+    float *D;
+    int64_t ld;
+    __device__ __forceinline__ more_t get(int64_t, int64_t, int) const { return {}; }
+    __device__ __forceinline__ float4 apply(int64_t r, int64_t c, int, float4 v, more_t) const
+    {
+        float o[4] = {v.x, v.y, v.z, v.w};
+#pragma unroll
+        for (int i = 0; i < 4; ++i) {
+            if (r == c + i) {
+                D[r] = o[i] * pow2(-2 * SX);
+                o[i] = 0.0f;
+            }
+            o[i] *= pow2(SO - 2 * SX);
+        }
+        *reinterpret_cast<u32x2 *>(O + r * ld + c) = f16_four(o);
+        return make_float4(o[0], o[1], o[2], o[3]);
+    }
+    __device__ __forceinline__ void put_turned(int64_t c, int64_t r, const float (&v)[8]) const { store_eight(O + c * ld + r, v); }
+};
+
+// O O: the polynomial's off-diagonal part in fp16, its diagonal (with a) in fp32.
+struct poly_t {
+    static constexpr bool COUNTED = false;
+    const uint16_t *O;
+    const float *D;
+    uint16_t *P;
+    float *diagonal;
+    int64_t ld;
+    float a, b, c;
+    struct more_t {
+        u32x2 o;
+        float4 dc;
+        float dr;
+    };
+    __device__ __forceinline__ more_t get(int64_t r, int64_t col, int) const
+    {
+        return {*reinterpret_cast<const u32x2 *>(O + r * ld + col), *reinterpret_cast<const float4 *>(D + col), D[r]};
+    }
+    __device__ __forceinline__ float4 apply(int64_t r, int64_t col, int, float4 v, const more_t &m) const
+    {
+        const float sq[4] = {v.x, v.y, v.z, v.w}, dc[4] = {m.dc.x, m.dc.y, m.dc.z, m.dc.w};
+        float o[4], p[4];
+        f16_values(m.o, o);
+#pragma unroll
+        for (int i = 0; i < 4; ++i) {
+            const float s = sq[i] * pow2(-2 * SO);
+            o[i] *= pow2(-SO);
+            p[i] = (b * o[i] + c * ((m.dr + dc[i]) * o[i] + s)) * pow2(SB);
+            if (r == col + i) {
+                diagonal[r] = a + (b * m.dr + c * (m.dr * m.dr + s));
+                p[i] = 0.0f;
+            }
+        }
+        *reinterpret_cast<u32x2 *>(P + r * ld + col) = f16_four(p);
+        return make_float4(p[0], p[1], p[2], p[3]);
+    }
+    __device__ __forceinline__ void put_turned(int64_t col, int64_t r, const float (&v)[8]) const { store_eight(P + col * ld + r, v); }
+};
+
+// The next iterate's elements from the product's and the carried ones.  BY_ROW: the diagonal goes by rows (A = X X^T), else by columns.
+template <bool BY_ROW> struct carried_t {
+    const float *x, *diagonal;
+    int64_t ld;
+    struct more_t {
+        float4 x, d;
+    };
+    __device__ __forceinline__ more_t get(int64_t r, int64_t c) const
+    {
+        more_t m;
+        m.x = *reinterpret_cast<const float4 *>(x + r * ld + c);
+        if constexpr (BY_ROW) {
+            const float d = diagonal[r];
+            m.d = make_float4(d, d, d, d);
+        } else {
+            m.d = *reinterpret_cast<const float4 *>(diagonal + c);
+        }
+        return m;
+    }
+    static __device__ __forceinline__ void next(float4 v, const more_t &m, float (&n)[4])
+    {
+        const float k = pow2(-SB - SX);
+        n[0] = m.d.x * m.x.x + v.x * k;
+        n[1] = m.d.y * m.x.y + v.y * k;
+        n[2] = m.d.z * m.x.z + v.z * k;
+        n[3] = m.d.w * m.x.w + v.w * k;
+    }
+};
+
+template <bool BY_ROW> struct step_t { // the next iterate; x in place
+    static constexpr bool COUNTED = false;
+    typedef typename carried_t<BY_ROW>::more_t more_t;
+    carried_t<BY_ROW> from;
+    iterate_t to;
+    __device__ __forceinline__ more_t get(int64_t r, int64_t c, int) const { return from.get(r, c); }
+    __device__ __forceinline__ float4 apply(int64_t r, int64_t c, int, float4 v, const more_t &m) const
+    {
+        float n[4];
+        from.next(v, m, n);
+        const int64_t at = r * to.ld + c;
+        *reinterpret_cast<float4 *>(to.x + at) = make_float4(n[0], n[1], n[2], n[3]);
+        put_half(to, at, n);
+        return v;
+    }
+};
+
+template <bool BY_ROW> struct result_t { // the last one, as the result
+    static constexpr bool COUNTED = false;
+    typedef typename carried_t<BY_ROW>::more_t more_t;
+    carried_t<BY_ROW> from;
+    adahop_tensor_t out;
+    int64_t rows, cols;
+    float scale;
+    __device__ __forceinline__ more_t get(int64_t r, int64_t c, int) const { return from.get(r, c); }
+    __device__ __forceinline__ float4 apply(int64_t r, int64_t c, int, float4 v, const more_t &m) const
+    {
+        if (r >= rows || c >= cols) return v;
+        float n[4];
+        from.next(v, m, n);
+        const float s[4] = {scale, scale, scale, scale};
+        put4(out, r, c, (int)(cols - c < 4 ? cols - c : 4), s, make_float4(n[0], n[1], n[2], n[3]), make_float4(0.0f, 0.0f, 0.0f, 0.0f));
+        return v;
+    }
+};
+
+template <bool BY_ROW> struct update_t { // the last one, as a step of the weight
+    static constexpr bool COUNTED = false;
+    carried_t<BY_ROW> from;
+    adahop_tensor_t w, out, copy; // copy: bf16, or absent
+    int64_t rows, cols;
+    float keep, rate;
+    struct more_t {
+        typename carried_t<BY_ROW>::more_t x;
+        float4 w;
+    };
+    __device__ __forceinline__ more_t get(int64_t r, int64_t c, int) const
+    {
+        more_t m;
+        m.x = from.get(r, c);
+        m.w = r < rows && c < cols ? get4(w, r, c, (int)(cols - c < 4 ? cols - c : 4)) : make_float4(0.0f, 0.0f, 0.0f, 0.0f);
+        return m;
+    }
+    __device__ __forceinline__ float4 apply(int64_t r, int64_t c, int, float4 v, const more_t &m) const
+    {
+        if (r >= rows || c >= cols) return v;
+        const int have = (int)(cols - c < 4 ? cols - c : 4);
+        float n[4];
+        from.next(v, m.x, n);
+        const float one[4] = {1.0f, 1.0f, 1.0f, 1.0f};
+        const float4 to = make_float4(keep * m.w.x - rate * n[0], keep * m.w.y - rate * n[1], keep * m.w.z - rate * n[2], keep * m.w.w - rate * n[3]),
+                     zero = make_float4(0.0f, 0.0f, 0.0f, 0.0f);
+        put4(out, r, c, have, one, to, zero);
+        if (copy.data) put4(copy, r, c, have, one, to, zero);
+        return v;
+    }
+};
+
+// ---- host ----------------------------------------------------------------------------------------------------------------------------
+struct ns_plan_t {
+    bool wide, split;
+    int64_t rows, cols, side, length; // padded: the matrix's, the smaller one and the larger
+    plan16_t gram, poly, step;
+    size_t sums, D, diagonal, O, P, x, h[2], part, total;
+};
+
+ns_plan_t ns_plan(int64_t rows, int64_t cols)
+{
+    ns_plan_t p;
+    p.wide = rows <= cols;
+    p.rows = align_up(rows, 32), p.cols = align_up(cols, 32);
+    p.side = p.wide ? p.rows : p.cols, p.length = p.wide ? p.cols : p.rows;
+    p.split = (p.wide ? rows : cols) <= SPLIT_SIDE;
+    p.gram = plan16(p.side, p.side, p.length * (p.split ? 3 : 1), true);
+    p.poly = plan16(p.side, p.side, p.side, true);
+    p.step = plan16(p.rows, p.cols, p.side * (p.split ? 2 : 1), false);
+    size_t part = p.gram.part_bytes;
+    for (const plan16_t *q : {&p.poly, &p.step})
+        if (q->part_bytes > part) part = q->part_bytes;
+    size_t at = 0;
+    const auto take = [&](size_t bytes) {
+        const size_t here = at;
+        at = align_up(at + bytes, 256);
+        return here;
+    };
+    const size_t all = (size_t)p.rows * p.cols, square = (size_t)p.side * p.side;
+    p.sums = take(PARTS * sizeof(double));
+    p.D = take(p.side * sizeof(float));
+    p.diagonal = take(p.side * sizeof(float));
+    p.O = take(square * 2);
+    p.P = take(square * 2);
+    p.x = take(all * sizeof(float));
+    for (size_t &h : p.h) h = take(all * 2 * (p.split ? 2 : 1));
+    p.part = take(part);
+    p.total = at;
+    return p;
+}
+
+device_once_t g_once;
+
+template <bool SEG> int configure_some()
+{
+    int rc = configure_both16<true, ALONG, ALONG, SEG, true, gram_t>();
+    if (rc == ADAHOP_OK) rc = configure_both16<true, DOWN, DOWN, SEG, true, gram_t>();
+    if (rc == ADAHOP_OK) rc = configure_both16<true, ALONG, DOWN, SEG, false, step_t<true>>();
+    if (rc == ADAHOP_OK) rc = configure_both16<true, ALONG, ALONG, SEG, false, step_t<false>>();
+    if (rc == ADAHOP_OK) rc = configure_both16<true, ALONG, DOWN, SEG, false, result_t<true>>();
+    if (rc == ADAHOP_OK) rc = configure_both16<true, ALONG, ALONG, SEG, false, result_t<false>>();
+    if (rc == ADAHOP_OK) rc = configure_both16<true, ALONG, DOWN, SEG, false, update_t<true>>();
+    if (rc == ADAHOP_OK) rc = configure_both16<true, ALONG, ALONG, SEG, false, update_t<false>>();
+    return rc;
+}
+
+// The products of one call.
+struct ns_call_t {
+    ns_plan_t p;
+    char *ws;
+    hipStream_t st;
+    iterate_t at(int which) const
+    {
+        return {reinterpret_cast<float *>(ws + p.x), reinterpret_cast<uint16_t *>(ws + p.h[which]), p.cols, p.split ? p.rows * p.cols : 0};
+    }
+    float *D() const { return reinterpret_cast<float *>(ws + p.D); }
+    float *diagonal() const { return reinterpret_cast<float *>(ws + p.diagonal); }
+    uint16_t *O() const { return reinterpret_cast<uint16_t *>(ws + p.O); }
+    uint16_t *P() const { return reinterpret_cast<uint16_t *>(ws + p.P); }
+
+    template <bool SEG> int gram(int which) const
+    {
+        const iterate_t x = at(which);
+        product_t q = {};
+        q.A = q.B = {x.h, x.ld, p.side};
+        q.K = p.length;
+        q.seg = {3, {0, 0, x.low}, {0, x.low, 0}}; // high high + high low + low high
+        const gram_t e = {O(), D(), p.side};
+        return p.wide ? launch_product16<true, ALONG, ALONG, SEG, true>(p.gram, q, e, ws + p.part, st) : launch_product16<true, DOWN, DOWN, SEG, true>(p.gram, q, e, ws + p.part, st);
+    }
+    int poly(const float (&k)[3]) const
+    {
+        product_t q = {};
+        q.A = q.B = {O(), p.side, p.side};
+        q.K = p.side;
+        const poly_t e = {O(), D(), P(), diagonal(), p.side, k[0], k[1], k[2]};
+        return launch_product16<true, ALONG, ALONG, false, true>(p.poly, q, e, ws + p.part, st);
+    }
+    // P X (wide), X P: with P symmetric, its rows serve as its columns
+    template <bool SEG, bool WIDE, class E> int step(int which, const E &e) const
+    {
+        const iterate_t x = at(which);
+        product_t q = {};
+        q.K = p.side;
+        if constexpr (WIDE) {
+            q.A = {P(), p.side, p.rows}, q.B = {x.h, x.ld, p.cols};
+            q.seg = {2, {0, 0, 0}, {0, x.low, 0}};
+            return launch_product16<true, ALONG, DOWN, SEG, false>(p.step, q, e, ws + p.part, st);
+        } else {
+            q.A = {x.h, x.ld, p.rows}, q.B = {P(), p.side, p.cols};
+            q.seg = {2, {0, x.low, 0}, {0, 0, 0}};
+            return launch_product16<true, ALONG, ALONG, SEG, false>(p.step, q, e, ws + p.part, st);
+        }
+    }
+};
+
+template <bool SEG, bool WIDE> int iterate(const ns_call_t &c, const adahop_newton_schulz_t &m, const adahop_tensor_t &out, const adahop_muon_t *u)
+{
+    const float k[3] = {m.a, m.b, m.c};
+    for (int i = 0; i < m.steps; ++i) {
+        int rc = c.gram<SEG>(i & 1);
+        if (rc == ADAHOP_OK) rc = c.poly(k);
+        if (rc != ADAHOP_OK) return rc;
+        const carried_t<WIDE> from = {c.at(0).x, c.diagonal(), c.p.cols};
+        if (i + 1 < m.steps)
+            rc = c.step<SEG, WIDE>(i & 1, step_t<WIDE>{from, c.at((i & 1) ^ 1)});
+        else if (u)
+            rc = c.step<SEG, WIDE>(i & 1, update_t<WIDE>{from, u->w, u->w_out, u->w_bf16, u->rows, u->cols, 1.0f - u->rate * u->weight_decay, u->rate * m.scale});
+        else
+            rc = c.step<SEG, WIDE>(i & 1, result_t<WIDE>{from, out, m.rows, m.cols, m.scale});
+        if (rc != ADAHOP_OK) return rc;
+    }
+    return ADAHOP_OK;
+}
+
+} // namespace
+
+int configure_newton_schulz()
+{
+    int dev = 0;
+    int rc = check_hip(hipGetDevice(&dev));
+    if (rc != ADAHOP_OK || !g_once.need(dev)) return rc;
+    rc = configure_some<false>();
+    if (rc == ADAHOP_OK) rc = configure_some<true>();
+    if (rc == ADAHOP_OK) rc = configure_both16<true, ALONG, ALONG, false, true, poly_t>();
+    if (rc == ADAHOP_OK) g_once.mark(dev);
+    return rc;
+}
+
+size_t newton_schulz_workspace_bytes(int64_t rows, int64_t cols) { return ns_plan(rows, cols).total; }
+
+int launch_newton_schulz(const adahop_newton_schulz_t &m, const adahop_tensor_t &g, const adahop_tensor_t &out, const adahop_muon_t *u, void *workspace, hipStream_t st)
+{
+    int rc = configure_newton_schulz();
+    if (rc != ADAHOP_OK) return rc;
+    const ns_call_t c = {ns_plan(m.rows, m.cols), static_cast<char *>(workspace), st};
+    source_t s = {g, {}, {}, 0.0f, 0, m.rows, m.cols};
+    if (u) s.m = u->momentum, s.m_out = u->momentum_out, s.mu = u->mu, s.nesterov = u->nesterov;
+    double *const sums = reinterpret_cast<double *>(c.ws + c.p.sums);
+    const int64_t pieces = ceil_div(m.rows * ceil_div(m.cols, 8), 256);
+    const int parts = (int)(pieces < PARTS ? pieces : PARTS);
+    k_squares<<<parts, 256, 0, st>>>(s, sums);
+    if ((rc = check_launch()) != ADAHOP_OK) return rc;
+    const int64_t blocks = ceil_div(c.p.rows * (c.p.cols / 8), 256);
+    k_first<<<(unsigned)(blocks < 4096 ? blocks : 4096), 256, 0, st>>>(s, sums, parts, m.eps, c.at(0), c.p.rows);
+    if ((rc = check_launch()) != ADAHOP_OK) return rc;
+    if (c.p.split) return c.p.wide ? iterate<true, true>(c, m, out, u) : iterate<true, false>(c, m, out, u);
+    return c.p.wide ? iterate<false, true>(c, m, out, u) : iterate<false, false>(c, m, out, u);
+}
+
+} // namespace adahop
