@@ -43,7 +43,7 @@ template <class K> __global__ __launch_bounds__(K::THREADS, 2) void k_ce_stats(p
 {
     extern __shared__ __attribute__((aligned(1024))) uint8_t smem[];
     int64_t n0, d0;
-    place_of<K, false>(q, n0, d0);
+    place_of<K, false>(q.nt, q.dt, run_of_xcd(blockIdx.x, q.nt * q.dt), n0, d0);
     v4f acc[K::MT][K::NT];
     multiply<K, false, ALONG, ALONG, false>(q, n0, d0, 0, q.K, smem, acc);
     wait_for_copies<0>();
@@ -123,24 +123,28 @@ __global__ __launch_bounds__(256) void k_ce_join(loss_t p, const float2 *part, c
 // dz of a piece of the vocabulary from its logits (rows: tokens, columns: words from v0 on), rounded to bf16; zeros from the piece's end to the row's.
 struct dlogits_t {
     static constexpr bool COUNTED = true;
+    static constexpr int AHEAD = 2;
     loss_t p;
     const int32_t *token; // of each row
     const float *lse, *d_loss;
     int64_t d_loss_stride, v0, words, ld;
     float factor; // in dz: logit_scale, or 1 where it comes later
     uint16_t *dz;
+    typedef nothing_t column_t;
+    __device__ __forceinline__ column_t column(int64_t, int) const { return {}; }
     struct more_t {
         float lse, gain; // gain: what exp(z - lse) - [v = y] is multiplied by
         int64_t y;
     };
-    __device__ __forceinline__ more_t get(int64_t r, int64_t, int) const
+    __device__ __forceinline__ more_t get(const spot_t &at, int) const
     {
-        const int64_t t = token[r], y = p.targets[t];
+        const int64_t t = token[at.row()], y = p.targets[t];
         const float g = (d_loss ? d_loss[t * d_loss_stride] : 1.0f) * factor;
         return {lse[t], y < p.V ? g : NAN, y};
     }
-    __device__ __forceinline__ float4 apply(int64_t r, int64_t c, int have, float4 v, const more_t &m) const
+    __device__ __forceinline__ float4 apply(const spot_t &at, int have, float4 v, column_t, const more_t &m) const
     {
+        const int64_t c = at.col();
         const float z[4] = {v.x, v.y, v.z, v.w}, s = 1.0f + 2.0f * p.z_loss * m.lse;
         const int64_t hit = m.y - v0 - c;
         float d[4];
@@ -149,7 +153,7 @@ struct dlogits_t {
             d[i] = (s * __expf(z[i] * p.logit_scale - m.lse) - (hit == i ? 1.0f : 0.0f)) * m.gain;
             if (i >= have) d[i] = 0.0f;
         }
-        uint16_t *const to = dz + r * ld + c; // 8-byte aligned
+        uint16_t *const to = at.in(dz, ld); // 8-byte aligned
         *reinterpret_cast<u32x2 *>(to) = u32x2{bf16_pair(d[0], d[1]), bf16_pair(d[2], d[3])};
         if (c + 4 >= words && c + 4 < ld) *reinterpret_cast<u32x2 *>(to + 4) = u32x2{0, 0}; // rows are whole pieces of eight
         return v;
@@ -313,9 +317,9 @@ int configure_linear_ce()
     if (rc != ADAHOP_OK || !g_once.need(dev)) return rc;
     rc = check_hip(hipFuncSetAttribute(reinterpret_cast<const void *>(&k_ce_stats<tile256_t>), hipFuncAttributeMaxDynamicSharedMemorySize, tile256_t::LDS));
     if (rc == ADAHOP_OK) rc = check_hip(hipFuncSetAttribute(reinterpret_cast<const void *>(&k_ce_stats<tile128_t>), hipFuncAttributeMaxDynamicSharedMemorySize, tile128_t::LDS));
-    if (rc == ADAHOP_OK) rc = configure_both16<false, ALONG, ALONG, false, false, dlogits_t>();
-    if (rc == ADAHOP_OK) rc = configure_both16<false, DOWN, DOWN, false, false, grad_t>();
-    if (rc == ADAHOP_OK) rc = configure_both16<false, ALONG, DOWN, false, false, grad_t>();
+    if (rc == ADAHOP_OK) rc = configure_all16<false, ALONG, ALONG, false, false, dlogits_t>();
+    if (rc == ADAHOP_OK) rc = configure_all16<false, DOWN, DOWN, false, false, grad_t>();
+    if (rc == ADAHOP_OK) rc = configure_all16<false, ALONG, DOWN, false, false, grad_t>();
     if (rc == ADAHOP_OK) g_once.mark(dev);
     return rc;
 }
@@ -375,9 +379,7 @@ int launch_linear_ce_backward(const adahop_linear_ce_t &c, void *workspace, hipS
         q.A = {h, ldh, T}, q.B = piece, q.K = ldh;
         q.rows_of = count;
         const dlogits_t e = {{c.targets, T, V, c.logit_scale, c.z_loss}, token, c.lse, one ? nullptr : c.d_loss, c.d_loss_stride, v0, words, ld, one ? 1.0f : c.logit_scale, dz};
-        plan16_t plan = plan16(T, words, q.K, false);
-        if (plan.slices > 1) plan.large = false, plan.slices = 1, plan.slice = align_up(q.K, 64);
-        if ((rc = launch_product16<false, ALONG, ALONG, false, false>(plan, q, e, nullptr, st)) != ADAHOP_OK) return rc;
+        if ((rc = launch_product16<false, ALONG, ALONG, false, false>(plan16(T, words, q.K, false, 1), q, e, nullptr, st)) != ADAHOP_OK) return rc;
         if (c.d_w.data) {
             const int64_t size = c.d_w.f32 ? 4 : 2, size_add = c.add.f32 ? 4 : 2;
             q.A = {dz, ld, words}, q.B = {h, ldh, D}, q.K = T;

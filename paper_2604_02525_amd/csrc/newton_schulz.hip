@@ -97,18 +97,18 @@ struct iterate_t {
     int64_t ld, low; // low = 0: not split
 };
 
-__device__ __forceinline__ void put_half(const iterate_t &t, int64_t at, const float (&v)[4])
+__device__ __forceinline__ void put_half(uint16_t *high, uint16_t *low, bool split, const float (&v)[4])
 {
     float s[4], back[4];
 #pragma unroll
     for (int i = 0; i < 4; ++i) s[i] = v[i] * pow2(SX);
     const u32x2 h = f16_four(s);
-    *reinterpret_cast<u32x2 *>(t.h + at) = h;
-    if (!t.low) return;
+    *reinterpret_cast<u32x2 *>(high) = h;
+    if (!split) return;
     f16_values(h, back);
 #pragma unroll
     for (int i = 0; i < 4; ++i) s[i] -= back[i];
-    *reinterpret_cast<u32x2 *>(t.h + t.low + at) = f16_four(s);
+    *reinterpret_cast<u32x2 *>(low) = f16_four(s);
 }
 
 // The first iterate: U over its norm.
@@ -137,8 +137,8 @@ __global__ __launch_bounds__(256) void k_first(source_t s, const double *part, i
         const int64_t at = r * to.ld + c;
         *reinterpret_cast<float4 *>(to.x + at) = make_float4(lo[0], lo[1], lo[2], lo[3]);
         *reinterpret_cast<float4 *>(to.x + at + 4) = make_float4(hi[0], hi[1], hi[2], hi[3]);
-        put_half(to, at, lo);
-        put_half(to, at + 4, hi);
+        put_half(to.h + at, to.h + to.low + at, to.low != 0, lo);
+        put_half(to.h + at + 4, to.h + to.low + at + 4, to.low != 0, hi);
     }
 }
 
@@ -146,13 +146,16 @@ __global__ __launch_bounds__(256) void k_first(source_t s, const double *part, i
 // X X^T: its diagonal, and the rest in fp16.
 struct gram_t {
     static constexpr bool COUNTED = false;
-    typedef nothing_t more_t;
+    static constexpr int AHEAD = 2;
+    typedef nothing_t column_t, more_t;
     uint16_t *O;
     float *D;
     int64_t ld;
-    __device__ __forceinline__ more_t get(int64_t, int64_t, int) const { return {}; }
-    __device__ __forceinline__ float4 apply(int64_t r, int64_t c, int, float4 v, more_t) const
+    __device__ __forceinline__ column_t column(int64_t, int) const { return {}; }
+    __device__ __forceinline__ more_t get(const spot_t &, int) const { return {}; }
+    __device__ __forceinline__ float4 apply(const spot_t &s, int, float4 v, column_t, more_t) const
     {
+        const int64_t r = s.row(), c = s.col();
         float o[4] = {v.x, v.y, v.z, v.w};
 #pragma unroll
         for (int i = 0; i < 4; ++i) {
@@ -162,7 +165,7 @@ struct gram_t {
             }
             o[i] *= pow2(SO - 2 * SX);
         }
-        *reinterpret_cast<u32x2 *>(O + r * ld + c) = f16_four(o);
+        *reinterpret_cast<u32x2 *>(s.in(O, ld)) = f16_four(o);
         return make_float4(o[0], o[1], o[2], o[3]);
     }
     __device__ __forceinline__ void put_turned(int64_t c, int64_t r, const float (&v)[8]) const { store_eight(O + c * ld + r, v); }
@@ -171,24 +174,24 @@ struct gram_t {
 // O O: the polynomial's off-diagonal part in fp16, its diagonal (with a) in fp32.
 struct poly_t {
     static constexpr bool COUNTED = false;
+    static constexpr int AHEAD = 3;
     const uint16_t *O;
     const float *D;
     uint16_t *P;
     float *diagonal;
     int64_t ld;
     float a, b, c;
+    typedef float4 column_t;
     struct more_t {
         u32x2 o;
-        float4 dc;
         float dr;
     };
-    __device__ __forceinline__ more_t get(int64_t r, int64_t col, int) const
+    __device__ __forceinline__ column_t column(int64_t col, int) const { return *reinterpret_cast<const float4 *>(D + col); }
+    __device__ __forceinline__ more_t get(const spot_t &s, int) const { return {*reinterpret_cast<const u32x2 *>(s.in(O, ld)), D[s.row()]}; }
+    __device__ __forceinline__ float4 apply(const spot_t &at, int, float4 v, const column_t &d, const more_t &m) const
     {
-        return {*reinterpret_cast<const u32x2 *>(O + r * ld + col), *reinterpret_cast<const float4 *>(D + col), D[r]};
-    }
-    __device__ __forceinline__ float4 apply(int64_t r, int64_t col, int, float4 v, const more_t &m) const
-    {
-        const float sq[4] = {v.x, v.y, v.z, v.w}, dc[4] = {m.dc.x, m.dc.y, m.dc.z, m.dc.w};
+        const int64_t r = at.row(), col = at.col();
+        const float sq[4] = {v.x, v.y, v.z, v.w}, dc[4] = {d.x, d.y, d.z, d.w};
         float o[4], p[4];
         f16_values(m.o, o);
 #pragma unroll
@@ -201,71 +204,82 @@ struct poly_t {
                 p[i] = 0.0f;
             }
         }
-        *reinterpret_cast<u32x2 *>(P + r * ld + col) = f16_four(p);
+        *reinterpret_cast<u32x2 *>(at.in(P, ld)) = f16_four(p);
         return make_float4(p[0], p[1], p[2], p[3]);
     }
     __device__ __forceinline__ void put_turned(int64_t col, int64_t r, const float (&v)[8]) const { store_eight(P + col * ld + r, v); }
 };
 
 // The next iterate's elements from the product's and the carried ones.  BY_ROW: the diagonal goes by rows (A = X X^T), else by columns.
-template <bool BY_ROW> struct carried_t {
+template <bool BY_ROW> struct carried_t;
+
+template <> struct carried_t<true> {
+    typedef nothing_t column_t;
+    struct more_t {
+        float4 x;
+        float d;
+    };
     const float *x, *diagonal;
     int64_t ld;
-    struct more_t {
-        float4 x, d;
-    };
-    __device__ __forceinline__ more_t get(int64_t r, int64_t c) const
-    {
-        more_t m;
-        m.x = *reinterpret_cast<const float4 *>(x + r * ld + c);
-        if constexpr (BY_ROW) {
-            const float d = diagonal[r];
-            m.d = make_float4(d, d, d, d);
-        } else {
-            m.d = *reinterpret_cast<const float4 *>(diagonal + c);
-        }
-        return m;
-    }
-    static __device__ __forceinline__ void next(float4 v, const more_t &m, float (&n)[4])
+    __device__ __forceinline__ column_t column(int64_t, int) const { return {}; }
+    __device__ __forceinline__ more_t get(const spot_t &s) const { return {*reinterpret_cast<const float4 *>(s.in(x, ld)), diagonal[s.row()]}; }
+    static __device__ __forceinline__ void next(float4 v, column_t, const more_t &m, float (&n)[4])
     {
         const float k = pow2(-SB - SX);
-        n[0] = m.d.x * m.x.x + v.x * k;
-        n[1] = m.d.y * m.x.y + v.y * k;
-        n[2] = m.d.z * m.x.z + v.z * k;
-        n[3] = m.d.w * m.x.w + v.w * k;
+        n[0] = m.d * m.x.x + v.x * k, n[1] = m.d * m.x.y + v.y * k, n[2] = m.d * m.x.z + v.z * k, n[3] = m.d * m.x.w + v.w * k;
+    }
+};
+
+template <> struct carried_t<false> {
+    typedef float4 column_t, more_t;
+    const float *x, *diagonal;
+    int64_t ld;
+    __device__ __forceinline__ column_t column(int64_t c, int) const { return *reinterpret_cast<const float4 *>(diagonal + c); }
+    __device__ __forceinline__ more_t get(const spot_t &s) const { return *reinterpret_cast<const float4 *>(s.in(x, ld)); }
+    static __device__ __forceinline__ void next(float4 v, const column_t &d, const more_t &x, float (&n)[4])
+    {
+        const float k = pow2(-SB - SX);
+        n[0] = d.x * x.x + v.x * k, n[1] = d.y * x.y + v.y * k, n[2] = d.z * x.z + v.z * k, n[3] = d.w * x.w + v.w * k;
     }
 };
 
 template <bool BY_ROW> struct step_t { // the next iterate; x in place
     static constexpr bool COUNTED = false;
+    static constexpr int AHEAD = BY_ROW ? 2 : 3;
+    typedef typename carried_t<BY_ROW>::column_t column_t;
     typedef typename carried_t<BY_ROW>::more_t more_t;
     carried_t<BY_ROW> from;
     iterate_t to;
-    __device__ __forceinline__ more_t get(int64_t r, int64_t c, int) const { return from.get(r, c); }
-    __device__ __forceinline__ float4 apply(int64_t r, int64_t c, int, float4 v, const more_t &m) const
+    __device__ __forceinline__ column_t column(int64_t c, int have) const { return from.column(c, have); }
+    __device__ __forceinline__ more_t get(const spot_t &s, int) const { return from.get(s); }
+    __device__ __forceinline__ float4 apply(const spot_t &s, int, float4 v, const column_t &d, const more_t &m) const
     {
         float n[4];
-        from.next(v, m, n);
-        const int64_t at = r * to.ld + c;
-        *reinterpret_cast<float4 *>(to.x + at) = make_float4(n[0], n[1], n[2], n[3]);
-        put_half(to, at, n);
+        from.next(v, d, m, n);
+        *reinterpret_cast<float4 *>(s.in(to.x, to.ld)) = make_float4(n[0], n[1], n[2], n[3]);
+        uint16_t *const h = s.in(to.h, to.ld);
+        put_half(h, h + to.low, to.low != 0, n);
         return v;
     }
 };
 
 template <bool BY_ROW> struct result_t { // the last one, as the result
     static constexpr bool COUNTED = false;
+    static constexpr int AHEAD = BY_ROW ? 2 : 3;
+    typedef typename carried_t<BY_ROW>::column_t column_t;
     typedef typename carried_t<BY_ROW>::more_t more_t;
     carried_t<BY_ROW> from;
     adahop_tensor_t out;
     int64_t rows, cols;
     float scale;
-    __device__ __forceinline__ more_t get(int64_t r, int64_t c, int) const { return from.get(r, c); }
-    __device__ __forceinline__ float4 apply(int64_t r, int64_t c, int, float4 v, const more_t &m) const
+    __device__ __forceinline__ column_t column(int64_t c, int have) const { return from.column(c, have); }
+    __device__ __forceinline__ more_t get(const spot_t &s, int) const { return from.get(s); }
+    __device__ __forceinline__ float4 apply(const spot_t &at, int, float4 v, const column_t &d, const more_t &m) const
     {
+        const int64_t r = at.row(), c = at.col();
         if (r >= rows || c >= cols) return v;
         float n[4];
-        from.next(v, m, n);
+        from.next(v, d, m, n);
         const float s[4] = {scale, scale, scale, scale};
         put4(out, r, c, (int)(cols - c < 4 ? cols - c : 4), s, make_float4(n[0], n[1], n[2], n[3]), make_float4(0.0f, 0.0f, 0.0f, 0.0f));
         return v;
@@ -274,6 +288,8 @@ template <bool BY_ROW> struct result_t { // the last one, as the result
 
 template <bool BY_ROW> struct update_t { // the last one, as a step of the weight
     static constexpr bool COUNTED = false;
+    static constexpr int AHEAD = 2;
+    typedef typename carried_t<BY_ROW>::column_t column_t;
     carried_t<BY_ROW> from;
     adahop_tensor_t w, out, copy; // copy: bf16, or absent
     int64_t rows, cols;
@@ -282,19 +298,22 @@ template <bool BY_ROW> struct update_t { // the last one, as a step of the weigh
         typename carried_t<BY_ROW>::more_t x;
         float4 w;
     };
-    __device__ __forceinline__ more_t get(int64_t r, int64_t c, int) const
+    __device__ __forceinline__ column_t column(int64_t c, int have) const { return from.column(c, have); }
+    __device__ __forceinline__ more_t get(const spot_t &s, int) const
     {
+        const int64_t r = s.row(), c = s.col();
         more_t m;
-        m.x = from.get(r, c);
+        m.x = from.get(s);
         m.w = r < rows && c < cols ? get4(w, r, c, (int)(cols - c < 4 ? cols - c : 4)) : make_float4(0.0f, 0.0f, 0.0f, 0.0f);
         return m;
     }
-    __device__ __forceinline__ float4 apply(int64_t r, int64_t c, int, float4 v, const more_t &m) const
+    __device__ __forceinline__ float4 apply(const spot_t &at, int, float4 v, const column_t &d, const more_t &m) const
     {
+        const int64_t r = at.row(), c = at.col();
         if (r >= rows || c >= cols) return v;
         const int have = (int)(cols - c < 4 ? cols - c : 4);
         float n[4];
-        from.next(v, m.x, n);
+        from.next(v, d, m.x, n);
         const float one[4] = {1.0f, 1.0f, 1.0f, 1.0f};
         const float4 to = make_float4(keep * m.w.x - rate * n[0], keep * m.w.y - rate * n[1], keep * m.w.z - rate * n[2], keep * m.w.w - rate * n[3]),
                      zero = make_float4(0.0f, 0.0f, 0.0f, 0.0f);
@@ -348,14 +367,14 @@ device_once_t g_once;
 
 template <bool SEG> int configure_some()
 {
-    int rc = configure_both16<true, ALONG, ALONG, SEG, true, gram_t>();
-    if (rc == ADAHOP_OK) rc = configure_both16<true, DOWN, DOWN, SEG, true, gram_t>();
-    if (rc == ADAHOP_OK) rc = configure_both16<true, ALONG, DOWN, SEG, false, step_t<true>>();
-    if (rc == ADAHOP_OK) rc = configure_both16<true, ALONG, ALONG, SEG, false, step_t<false>>();
-    if (rc == ADAHOP_OK) rc = configure_both16<true, ALONG, DOWN, SEG, false, result_t<true>>();
-    if (rc == ADAHOP_OK) rc = configure_both16<true, ALONG, ALONG, SEG, false, result_t<false>>();
-    if (rc == ADAHOP_OK) rc = configure_both16<true, ALONG, DOWN, SEG, false, update_t<true>>();
-    if (rc == ADAHOP_OK) rc = configure_both16<true, ALONG, ALONG, SEG, false, update_t<false>>();
+    int rc = configure_all16<true, ALONG, ALONG, SEG, true, gram_t>();
+    if (rc == ADAHOP_OK) rc = configure_all16<true, DOWN, DOWN, SEG, true, gram_t>();
+    if (rc == ADAHOP_OK) rc = configure_all16<true, ALONG, DOWN, SEG, false, step_t<true>>();
+    if (rc == ADAHOP_OK) rc = configure_all16<true, ALONG, ALONG, SEG, false, step_t<false>>();
+    if (rc == ADAHOP_OK) rc = configure_all16<true, ALONG, DOWN, SEG, false, result_t<true>>();
+    if (rc == ADAHOP_OK) rc = configure_all16<true, ALONG, ALONG, SEG, false, result_t<false>>();
+    if (rc == ADAHOP_OK) rc = configure_all16<true, ALONG, DOWN, SEG, false, update_t<true>>();
+    if (rc == ADAHOP_OK) rc = configure_all16<true, ALONG, ALONG, SEG, false, update_t<false>>();
     return rc;
 }
 
@@ -437,7 +456,7 @@ int configure_newton_schulz()
     if (rc != ADAHOP_OK || !g_once.need(dev)) return rc;
     rc = configure_some<false>();
     if (rc == ADAHOP_OK) rc = configure_some<true>();
-    if (rc == ADAHOP_OK) rc = configure_both16<true, ALONG, ALONG, false, true, poly_t>();
+    if (rc == ADAHOP_OK) rc = configure_all16<true, ALONG, ALONG, false, true, poly_t>();
     if (rc == ADAHOP_OK) g_once.mark(dev);
     return rc;
 }

@@ -36,9 +36,12 @@ struct segments_t {
 struct product_t {
     side_t A, B;
     int64_t K;       // a multiple of 8 where an operand is ALONG; of 32 with several segments
-    int64_t slice;   // of all segments' K per slice: a multiple of 64
-    float *part;     // [slices][A.outer][B.outer], or nullptr: one slice, finished by the kernel itself
     uint32_t nt, dt; // tiles along A's outer index and B's
+    // The first `whole` tiles are a workgroup's each.  Of the others a workgroup has one of `slices` slices of the contraction (`slice` elements of all segments' K, a
+    // multiple of 64), whose sums go to part, [tile][slice][TM][TN]; with one slice they are whole too.
+    uint32_t whole, slices;
+    int64_t slice;
+    float *part;
     segments_t seg;
     const int32_t *rows_of, *K_of; // (or nullptr) how many of A's outer indices and of the contraction's elements there are, where only the device knows
 };
@@ -48,38 +51,43 @@ template <int MT_, int NT_, int WN_, int WD_, int RING_> struct shape_t {
     static constexpr int MT = MT_, NT = NT_, WN = WN_, WD = WD_, RING = RING_;
     static constexpr int WAVES = WN * WD, THREADS = 64 * WAVES, TM = 16 * WN * MT, TN = 16 * WD * NT, RA = 2 * TM, RB = 2 * TN; // bytes of a row of a DOWN stage
     static constexpr uint32_t A = STAGE * RA, B = STAGE * RB, SLOT = A + B, LDS = RING * SLOT;
-    static constexpr int COPIES_A = A / 1024 / WAVES, COPIES_B = B / 1024 / WAVES, ISSUED = COPIES_A + COPIES_B; // per wave and stage
-    static_assert(COPIES_A * WAVES * 1024 == A && COPIES_B * WAVES * 1024 == B, "whole copies");
-    // DOWN: by what the pieces of 32 bytes of a row are exchanged, so that the eight rows of a transposing read of half a wave lie in different banks
-    static __device__ __forceinline__ uint32_t turn_of(uint32_t row, uint32_t bytes) { return bytes >= 256 ? (row & 3) | (row >> 1 & 4) : (row >> 1 & 1) | (row >> 2 & 2); }
+    static constexpr int COPIES = A / 1024 / (WAVES / 2); // per wave and stage: half of the waves copy A, the others B
+    static_assert(TM == TN && COPIES * (WAVES / 2) * 1024 == A, "whole copies");
+    // DOWN: by what the pieces of 32 bytes of a row are exchanged, so that the eight rows of a transposing read of half a wave (four consecutive ones and those 8 further on)
+    // lie in different banks.  Rows of a multiple of 256 bytes begin at the same bank: by bits 0, 1 and 3 of the row.  Rows of 128 or 384: two of them lie apart, by bits 1 and 3.
+    static __device__ __forceinline__ uint32_t turn_of(uint32_t row, uint32_t bytes) { return bytes % 256 ? (row >> 1 & 1) | (row >> 2 & 2) : (row & 3) | (row >> 1 & 4); }
+    // What lane l of copy number `copy` of a stage reads: its row, and the byte in it
     static __device__ __forceinline__ uint32_t row_of(uint32_t copy, uint32_t l, uint32_t bytes) { return (copy * 1024 + l * 16) / bytes; }
-    static __device__ __forceinline__ uint32_t byte_of(uint32_t row, uint32_t l, uint32_t bytes)
+    static __device__ __forceinline__ uint32_t byte_of(uint32_t row, uint32_t l, uint32_t copy, uint32_t bytes)
     {
-        const uint32_t chunk = l % (bytes / 16);
+        const uint32_t chunk = (copy * 1024 + l * 16 - row * bytes) / 16;
         return ((chunk >> 1) ^ turn_of(row, bytes)) * 32 + (chunk & 1) * 16;
     }
 };
 
 typedef shape_t<8, 4, 2, 4, 4> tile256_t;
+typedef shape_t<6, 3, 2, 4, 4> tile192_t;
 typedef shape_t<4, 4, 2, 2, 4> tile128_t;
 
-// One operand's copies: the resource that a stage is read from, where it goes on, and what this lane reads of it.
-template <class K, lies_t LIES, bool SEG, int OUTER, int COPIES> struct copies_t {
+// A wave's copies, all of one operand: the resource that a stage is read from, where it goes on, and what this lane reads of it.
+template <class K, bool SEG> struct copies_t {
+    static constexpr int OUTER = K::TM;
     static constexpr uint32_t BYTES = 2 * OUTER;
     rsrc_t from;
-    uint32_t off[COPIES];
+    uint32_t off[K::COPIES];
     uint32_t full, last, step, beyond; // extents of a whole stage and of one at the contraction's end; beyond: what puts this lane's piece out of bounds there
     int64_t hop[SEG ? 2 : 1];          // from the last stage of a segment to the first of the next
 
-    __device__ __forceinline__ copies_t(const side_t &s, int64_t K_, int64_t at, int64_t begin, uint32_t odd, uint32_t w, uint32_t lane, const int64_t (&starts)[3], int segment)
+    // w: which of the waves that copy this operand
+    __device__ __forceinline__ void set(lies_t lies, const side_t &s, int64_t K_, int64_t at, int64_t begin, uint32_t odd, uint32_t w, uint32_t lane, const int64_t (&starts)[3], int segment)
     {
         const uint32_t pitch = (uint32_t)(s.ld * 2);
         const int64_t most = s.outer - at, first = SEG ? starts[segment] : 0;
-        if constexpr (LIES == DOWN) {
+        if (lies == DOWN) {
 #pragma unroll
-            for (int i = 0; i < COPIES; ++i) {
-                const uint32_t row = K::row_of(w * COPIES + i, lane, BYTES);
-                off[i] = row * pitch + K::byte_of(row, lane, BYTES);
+            for (int i = 0; i < K::COPIES; ++i) {
+                const uint32_t row = K::row_of(w * K::COPIES + i, lane, BYTES);
+                off[i] = row * pitch + K::byte_of(row, lane, w * K::COPIES + i, BYTES);
             }
             const uint32_t wide = (uint32_t)(most * 2 < BYTES ? most * 2 : BYTES); // bytes of a row, in whole words below
             full = ((STAGE - 1) * pitch + wide + 3) & ~3u;
@@ -90,7 +98,7 @@ template <class K, lies_t LIES, bool SEG, int OUTER, int COPIES> struct copies_t
         } else {
             const uint32_t piece = (lane & 3) ^ (lane >> 4 & 3); // rows of four lanes: the row's bits 2 and 3 are the lane's 4 and 5
 #pragma unroll
-            for (int i = 0; i < COPIES; ++i) off[i] = ((w * COPIES + i) * 16 + (lane >> 2)) * pitch + piece * 16;
+            for (int i = 0; i < K::COPIES; ++i) off[i] = ((w * K::COPIES + i) * 16 + (lane >> 2)) * pitch + piece * 16;
             const uint32_t rows = (uint32_t)(most < OUTER ? most : OUTER);
             full = (rows - 1) * pitch + 2 * STAGE;
             last = odd ? (rows - 1) * pitch + (odd + 7) / 8 * 16 : 0;
@@ -102,6 +110,17 @@ template <class K, lies_t LIES, bool SEG, int OUTER, int COPIES> struct copies_t
             const int64_t run = (K_ / STAGE - 1) * (int64_t)step; // bytes from a segment's first stage to its last
 #pragma unroll
             for (int i = 0; i < 2; ++i) hop[i] = (starts[i + 1] - starts[i]) * 2 - run;
+        }
+    }
+    // Into scalar registers, which the copies take the resource from: it is the same in all lanes, but the compiler may have come to it another way.
+    __device__ __forceinline__ void settle()
+    {
+        const auto one = [](uint32_t v) { return (uint32_t)__builtin_amdgcn_readfirstlane(v); };
+        from.x = one(from.x), from.y = one(from.y), from.z = one(from.z), from.w = one(from.w);
+        full = one(full), last = one(last), step = one(step);
+        if constexpr (SEG) {
+#pragma unroll
+            for (int i = 0; i < 2; ++i) hop[i] = (int64_t)((uint64_t)one((uint32_t)((uint64_t)hop[i] >> 32)) << 32 | one((uint32_t)hop[i]));
         }
     }
     __device__ __forceinline__ void forward(int64_t bytes)
@@ -130,40 +149,41 @@ __device__ __forceinline__ void multiply(const product_t &q, int64_t n0, int64_t
     constexpr int MT = K::MT, NT = K::NT, RING = K::RING;
     const int tid = threadIdx.x, lane = tid & 63, w = __builtin_amdgcn_readfirstlane(tid >> 6), wn = w / K::WD, wd = w % K::WD;
     const uint32_t base = __builtin_amdgcn_readfirstlane(lds_address(smem));
-    int32_t left = (int32_t)(end - begin), ahead = left; // elements from the stage at hand, and from the one that is copied next, on
+    int32_t left = __builtin_amdgcn_readfirstlane((int32_t)(end - begin)), ahead = left; // elements from the stage at hand, and from the one that is copied next, on
     int segment = 0;
     uint32_t in = 0, run = 0;
     if constexpr (SEG) {
         run = (uint32_t)(q.K / STAGE);
-        segment = (int)(begin / q.K);
+        segment = __builtin_amdgcn_readfirstlane((int)(begin / q.K));
         begin -= segment * q.K;
-        in = (uint32_t)(begin / STAGE);
+        in = __builtin_amdgcn_readfirstlane((uint32_t)(begin / STAGE));
     }
     const uint32_t odd = SEG ? 0u : (uint32_t)left % STAGE;
-    copies_t<K, LA, SEG, K::TM, K::COPIES_A> a(q.A, q.K, n0, begin, odd, w, lane, q.seg.a, segment);
-    copies_t<K, LB, SEG, K::TN, K::COPIES_B> b(q.B, q.K, d0, begin, odd, w, lane, q.seg.b, segment);
+    copies_t<K, SEG> mine;
+    const bool of_b = w >= K::WAVES / 2;
+    if (of_b)
+        mine.set(LB, q.B, q.K, d0, begin, odd, w - K::WAVES / 2, lane, q.seg.b, segment);
+    else
+        mine.set(LA, q.A, q.K, n0, begin, odd, w, lane, q.seg.a, segment);
+    mine.settle();
     uint32_t to = base, at = base; // slots: copied to next, read next
     const auto after = [&](uint32_t slot) { return slot == base + (RING - 1) * K::SLOT ? base : slot + K::SLOT; };
-    uint32_t cut_a = 0, cut_b = 0;
-    // The resources of the stage that is copied next: a whole one, the contraction's end, or nothing.  Without a branch: it would end the block that the
+    uint32_t cut = 0;
+    // The resource of the stage that is copied next: a whole one, the contraction's end, or nothing.  Without a branch: it would end the block that the
     // instructions around are scheduled in.
     const auto trim = [&] {
-        a.from.z = ahead >= STAGE ? a.full : ahead > 0 ? a.last : 0;
-        b.from.z = ahead >= STAGE ? b.full : ahead > 0 ? b.last : 0;
-        if constexpr (LA == ALONG) cut_a = ahead >= STAGE ? 0 : a.beyond;
-        if constexpr (LB == ALONG) cut_b = ahead >= STAGE ? 0 : b.beyond;
+        mine.from.z = ahead >= STAGE ? mine.full : ahead > 0 ? mine.last : 0;
+        if constexpr (LA == ALONG || LB == ALONG) cut = ahead >= STAGE ? 0 : mine.beyond;
     };
-    const uint32_t own_a = w * K::COPIES_A * 1024, own_b = w * K::COPIES_B * 1024;
+    const uint32_t own = w * K::COPIES * 1024; // B's copies follow A's
     const auto copied = [&] {
         if constexpr (SEG) {
             const bool cross = ++in == run;
-            a.forward(cross ? (segment ? a.hop[1] : a.hop[0]) : (int64_t)a.step);
-            b.forward(cross ? (segment ? b.hop[1] : b.hop[0]) : (int64_t)b.step);
+            mine.forward(cross ? (segment ? mine.hop[1] : mine.hop[0]) : (int64_t)mine.step);
             in = cross ? 0 : in;
             segment += cross;
         } else {
-            a.forward(a.step);
-            b.forward(b.step);
+            mine.forward(mine.step);
         }
         ahead -= STAGE;
         to = after(to);
@@ -171,10 +191,7 @@ __device__ __forceinline__ void multiply(const product_t &q, int64_t n0, int64_t
     };
     const auto copy = [&](auto number) {
         constexpr int i = decltype(number)::value;
-        if constexpr (i < K::COPIES_A)
-            dma16_bounded<i * 1024>(a.from, LA == ALONG ? a.off[i] | cut_a : a.off[i], to + own_a);
-        else
-            dma16_bounded<K::A + (i - K::COPIES_A) * 1024>(b.from, LB == ALONG ? b.off[i - K::COPIES_A] | cut_b : b.off[i - K::COPIES_A], to + own_b);
+        dma16_bounded<i * 1024>(mine.from, LA == ALONG || LB == ALONG ? mine.off[i] | cut : mine.off[i], __builtin_amdgcn_readfirstlane(to + own));
     };
 
     // What this lane reads: the matrix instruction wants the eight elements from 8 (lane / 16) on of row or column lane % 16.  DOWN: four lanes of a group of 16
@@ -221,15 +238,15 @@ __device__ __forceinline__ void multiply(const product_t &q, int64_t n0, int64_t
     };
     constexpr int PLACES = MT * NT, BARRIER = NT - 1; // a stage's matrix instructions are places, with what is issued beside each
     constexpr int READS_B = PB * NT, EACH = (READS_B + (MT - 1) * (NT - 2) - 1) / ((MT - 1) * (NT - 2)); // reads of B beside one of the places for them
-    static_assert(NT > 2 && K::ISSUED <= PLACES - NT, "what goes beside the matrix instructions fits");
+    static_assert(NT > 2 && K::COPIES <= PLACES - NT, "what goes beside the matrix instructions fits");
 
     trim();
 #pragma unroll 1
     for (int i = 0; i < RING - 1; ++i) {
-        static_for<0, K::ISSUED>(copy);
+        static_for<0, K::COPIES>(copy);
         copied();
     }
-    wait_for_copies<(RING - 2) * K::ISSUED>();
+    wait_for_copies<(RING - 2) * K::COPIES>();
     // Everything that the compiler counts with the reads of LDS is done before these, and these are issued in the order of the loop's: its waits in
     // the loop go by what may be outstanding on either way into it.
     __builtin_amdgcn_s_waitcnt(0xc07f); // lgkmcnt(0)
@@ -252,7 +269,7 @@ __device__ __forceinline__ void multiply(const product_t &q, int64_t n0, int64_t
             acc[m][n] = mfma16<F16>(va, vb, acc[m][n]);
             if constexpr (m == 0 && n < 2) read_a(MT - 1, n); // of this stage
             if constexpr (place == BARRIER) {
-                asm volatile("s_waitcnt vmcnt(%0)\n\ts_barrier" ::"n"((RING - 3) * K::ISSUED) : "memory"); // the next stage is there
+                asm volatile("s_waitcnt vmcnt(%0)\n\ts_barrier" ::"n"((RING - 3) * K::COPIES) : "memory"); // the next stage is there
                 at = after(at);
             }
             if constexpr (m > 0) {
@@ -262,7 +279,7 @@ __device__ __forceinline__ void multiply(const product_t &q, int64_t n0, int64_t
                 else
                     static_for<first, first + EACH < READS_B ? first + EACH : READS_B>([&](auto i) { read_b(set ^ 1, decltype(i)::value / PB, decltype(i)::value % PB); });
             }
-            if constexpr (place >= PLACES - K::ISSUED) copy(std::integral_constant<int, place - (PLACES - K::ISSUED)>{});
+            if constexpr (place >= PLACES - K::COPIES) copy(std::integral_constant<int, place - (PLACES - K::COPIES)>{});
             ADAHOP_PIN();
         });
         copied();
@@ -274,66 +291,113 @@ __device__ __forceinline__ void multiply(const product_t &q, int64_t n0, int64_t
     }
 }
 
-// Which tile a workgroup takes.  Workgroups go round the eight XCDs; each takes a run of tiles, which it walks in columns of four tiles: what runs on it at a time
-// shares few tiles of either operand.  SYMMETRIC: only tiles on and below the diagonal, row by row.
-template <class K, bool SYMMETRIC> __device__ __forceinline__ void place_of(const product_t &q, int64_t &n0, int64_t &d0)
+// Where tile t is.  A run of tiles goes by columns of four: what an XCD works on at a time shares few tiles of either operand.  SYMMETRIC: only
+// tiles on and below the diagonal.
+template <class K, bool SYMMETRIC> __device__ __forceinline__ void place_of(uint32_t nt, uint32_t dt, uint32_t t, int64_t &n0, int64_t &d0)
 {
-    const uint32_t tiles = SYMMETRIC ? q.nt * (q.nt + 1) / 2 : q.nt * q.dt, id = blockIdx.x, per = tiles / 8, rest = tiles % 8, xcd = id % 8;
-    const uint32_t t = xcd * per + (xcd < rest ? xcd : rest) + id / 8;
-    if constexpr (SYMMETRIC) {
-        uint32_t i = (uint32_t)((sqrtf(8.0f * t + 1.0f) - 1.0f) * 0.5f);
-        while (i * (i + 1) / 2 > t) --i; // the root is to within one
-        while ((i + 1) * (i + 2) / 2 <= t) ++i;
-        n0 = (int64_t)i * K::TM, d0 = (int64_t)(t - i * (i + 1) / 2) * K::TN;
+    if constexpr (SYMMETRIC) { // groups of four rows: 16 g + 10 tiles in group g, its columns up to 4 g + 1 whole
+        uint32_t g = (uint32_t)((sqrtf(8.0f * t + 1.0f) - 1.0f) * 0.125f);
+        while (g && 8 * g * g + 2 * g > t) --g; // the root is to within one
+        while (8 * (g + 1) * (g + 1) + 2 * (g + 1) <= t) ++g;
+        const uint32_t in = t - (8 * g * g + 2 * g), high = nt - 4 * g < 4 ? nt - 4 * g : 4, even = high * (4 * g + 1);
+        uint32_t i = in % high, j = in / high;
+        if (in >= even) { // the last columns' ends: high - 1 tiles, high - 2, ...
+            uint32_t left = in - even, down = 1;
+            for (; left >= high - down; ++down) left -= high - down;
+            i = down + left, j = 4 * g + down;
+        }
+        n0 = (int64_t)(4 * g + i) * K::TM, d0 = (int64_t)j * K::TN;
     } else {
-        const uint32_t group = t / (4 * q.dt), in = t - group * 4 * q.dt, high = q.nt - 4 * group < 4 ? q.nt - 4 * group : 4;
+        const uint32_t group = t / (4 * dt), in = t - group * 4 * dt, high = nt - 4 * group < 4 ? nt - 4 * group : 4;
         n0 = (int64_t)(4 * group + in % high) * K::TM, d0 = (int64_t)(in / high) * K::TN;
     }
 }
 
+// Workgroups go round the eight XCDs; each takes a run of `tiles` tiles.
+__device__ __forceinline__ uint32_t run_of_xcd(uint32_t id, uint32_t tiles)
+{
+    const uint32_t per = tiles / 8, rest = tiles % 8, xcd = id % 8;
+    return xcd * per + (xcd < rest ? xcd : rest) + id / 8;
+}
+
 // What becomes of the sums is a finish E:
 //   COUNTED                        whether rows_of and K_of are looked at
-//   E::more_t                      what it reads for four elements
-//   more_t get(r, c, have)         that, ahead of its use
-//   float4 apply(r, c, have, v, m) finishes C[r, c .. c + have) and stores it; returns the values for put_turned
+//   E::column_t, column(c, have)   what it reads for four columns, once for all their rows
+//   E::more_t, get(spot, have)     what it reads for four elements, ahead of its use (AHEAD - 1 blocks of 32 rows)
+//   float4 apply(spot, have, v, column, more) finishes and stores the first `have` of them; returns the values for put_turned
 //   put_turned(c, r, v)            SYMMETRIC: stores eight of them, C[r .. r + 8, c], as row c
 struct nothing_t {};
 
-struct store_part_t { // a slice's sums as they are
-    typedef nothing_t more_t;
-    float *to;
-    int64_t ld;
-    __device__ __forceinline__ more_t get(int64_t, int64_t, int) const { return {}; }
-    __device__ __forceinline__ float4 apply(int64_t r, int64_t c, int have, float4 v, more_t) const
+// Where a lane's four elements are: a row and a column for the whole wave, and the lane's from there on.
+struct spot_t {
+    int64_t r0, c0;
+    uint32_t r, c;
+    __device__ __forceinline__ int64_t row() const { return r0 + r; }
+    __device__ __forceinline__ int64_t col() const { return c0 + c; }
+    // its element of an array of rows of ld < 2^26 elements: a wave's address in scalar registers, 32 bits of the lane's own
+    template <class T> __device__ __forceinline__ T *in(T *base, int64_t ld) const
     {
-        const float one[4] = {1.0f, 1.0f, 1.0f, 1.0f};
-        put4({to, ld, 1}, r, c, have, one, v, make_float4(0.0f, 0.0f, 0.0f, 0.0f));
+        typedef typename std::conditional<std::is_const<T>::value, const char, char>::type byte_t;
+        return reinterpret_cast<T *>(reinterpret_cast<byte_t *>(base + r0 * ld + c0) + (uint32_t)((r * (uint32_t)ld + c) * sizeof(T)));
+    }
+};
+
+struct store_part_t { // a slice's sums as they are
+    static constexpr int AHEAD = 2;
+    typedef nothing_t column_t, more_t;
+    float *to; // of the tile at (n0, d0)
+    int64_t n0, d0, ld;
+    __device__ __forceinline__ column_t column(int64_t, int) const { return {}; }
+    __device__ __forceinline__ more_t get(const spot_t &, int) const { return {}; }
+    __device__ __forceinline__ float4 apply(const spot_t &s, int, float4 v, column_t, more_t) const
+    {
+        *reinterpret_cast<float4 *>(spot_t{s.r0 - n0, s.c0 - d0, s.r, s.c}.in(to, ld)) = v;
         return v;
     }
 };
 
+// The mirror image of a wave's patch of 32 rows of 16 NT columns at (r0, c0): four lanes have the 32 rows of a column.
+template <int NT, class E> __device__ __forceinline__ void put_mirror(const product_t &q, int64_t r0, int64_t c0, const float *patch, const E &e)
+{
+    constexpr int PITCH = 16 * NT + 4;
+    const int lane = threadIdx.x & 63, down = 8 * (lane & 3);
+#pragma unroll
+    for (int i = 0; i < NT; ++i) {
+        const int col = 16 * i + (lane >> 2);
+        float v[8];
+#pragma unroll
+        for (int j = 0; j < 8; ++j) v[j] = patch[(down + j) * PITCH + col];
+        if (c0 + col < q.B.outer && r0 + down < q.A.outer) e.put_turned(c0 + col, r0 + down, v);
+    }
+}
+
 // C's rows go by way of a wave's own patch of LDS, 32 at a time, so that a lane has four consecutive columns of a row: 16-byte stores of whole rows.  In
-// the accumulators a lane has column lane % 16 of a tile, rows 4 (lane / 16) + i.  What the finish reads is read 32 rows ahead: no load
-// passes a store that it might depend on.
+// the accumulators a lane has column lane % 16 of a tile, rows 4 (lane / 16) + i.  What the finish reads is read 64 rows ahead: no load passes a store that it might
+// depend on, and one block of rows ahead does not cover the memory's latency.
 template <class K, bool SYMMETRIC, class E>
 __device__ __forceinline__ void finish_tile(const product_t &q, int64_t n0, int64_t d0, uint8_t *smem, const v4f (&acc)[K::MT][K::NT], const E &e)
 {
-    constexpr int MT = K::MT, NT = K::NT, PITCH = 16 * NT + 4, LANES = 4 * NT, STEPS = LANES / 2;
+    constexpr int MT = K::MT, NT = K::NT, PITCH = 16 * NT + 4, LANES = 4 * NT, ROWS = 64 / LANES, STEPS = (32 + ROWS - 1) / ROWS, AHEAD = E::AHEAD; // lanes of a row, rows at a time
     static_assert(K::WAVES * 32 * PITCH * sizeof(float) <= K::LDS, "the waves' patches fit");
     const int lane = threadIdx.x & 63, w = __builtin_amdgcn_readfirstlane(threadIdx.x >> 6), wn = w / K::WD, wd = w % K::WD;
     const int c4 = lane % LANES * 4, r0 = lane / LANES;
-    const int64_t c = d0 + wd * NT * 16 + c4;
+    const int64_t c0 = d0 + wd * NT * 16, c = c0 + c4, first = n0 + wn * MT * 16;
     const int have = (int)(q.B.outer - c < 4 ? q.B.outer - c : 4);
-    const auto row_at = [&](int m, int i) { return n0 + (wn * MT + m) * 16 + r0 + i * (64 / LANES); };
+    // whether step i of the rows from 16 m on is one of this lane's
+    const auto is = [&](int m, int i) { return have > 0 && r0 < q.A.outer - first - m * 16 - i * ROWS && (32 % ROWS == 0 || (r0 < ROWS && r0 + i * ROWS < 32)); };
+    const auto spot = [&](int m, int i) { return spot_t{first + m * 16 + i * ROWS, c0, (uint32_t)r0, (uint32_t)c4}; };
     float *const patch = reinterpret_cast<float *>(smem) + w * 32 * PITCH;
-    typename E::more_t more[2][STEPS];
+    typename E::column_t column;
+    if (have > 0) column = e.column(c, have);
+    typename E::more_t more[AHEAD][STEPS];
     const auto get = [&](int m) {
 #pragma unroll
         for (int i = 0; i < STEPS; ++i)
-            if (have > 0 && row_at(m, i) < q.A.outer) more[m / 2 & 1][i] = e.get(row_at(m, i), c, have);
+            if (is(m, i)) more[m / 2 % AHEAD][i] = e.get(spot(m, i), have);
     };
-    get(0);
-    wait_for_copies<0>();
+    wait_for_copies<0>(); // those of zeros behind the last stage
+#pragma unroll
+    for (int m = 0; m < 2 * (AHEAD - 1) && m < MT; m += 2) get(m);
     asm volatile("s_barrier" ::: "memory"); // no wave reads or copies any more
 #pragma unroll
     for (int m = 0; m < MT; m += 2) {
@@ -343,27 +407,19 @@ __device__ __forceinline__ void finish_tile(const product_t &q, int64_t n0, int6
 #pragma unroll
             for (int i = 0; i < 8; ++i) patch[(16 * (i >> 2) + 4 * (lane >> 4) + (i & 3)) * PITCH + 16 * n + (lane & 15)] = acc[m + (i >> 2)][n][i & 3];
         lds_between_lanes();
-        if (m + 2 < MT) get(m + 2);
+        if (m + 2 * (AHEAD - 1) < MT) get(m + 2 * (AHEAD - 1));
 #pragma unroll
         for (int i = 0; i < STEPS; ++i) {
-            float4 *const v = reinterpret_cast<float4 *>(patch + (r0 + i * (64 / LANES)) * PITCH + c4);
-            if (have > 0 && row_at(m, i) < q.A.outer) {
-                const float4 done = e.apply(row_at(m, i), c, have, *v, more[m / 2 & 1][i]);
+            float4 *const v = reinterpret_cast<float4 *>(patch + (r0 + i * ROWS) * PITCH + c4);
+            if (is(m, i)) {
+                const float4 done = e.apply(spot(m, i), have, *v, column, more[m / 2 % AHEAD][i]);
                 if constexpr (SYMMETRIC) *v = done;
             }
         }
         if constexpr (SYMMETRIC) {
-            if (n0 != d0) { // the tile's mirror image: four lanes have 32 rows of a column
+            if (n0 != d0) {
                 lds_between_lanes();
-                const int64_t r = n0 + (wn * MT + m) * 16 + 8 * (lane & 3);
-#pragma unroll
-                for (int i = 0; i < NT; ++i) {
-                    const int col = 16 * i + (lane >> 2);
-                    float v[8];
-#pragma unroll
-                    for (int j = 0; j < 8; ++j) v[j] = patch[(8 * (lane & 3) + j) * PITCH + col];
-                    if (d0 + wd * NT * 16 + col < q.B.outer && r < q.A.outer) e.put_turned(d0 + wd * NT * 16 + col, r, v);
-                }
+                put_mirror<NT>(q, first + m * 16, c0, patch, e);
             }
         }
     }
@@ -373,68 +429,90 @@ __device__ __forceinline__ void finish_tile(const product_t &q, int64_t n0, int6
 template <class K, bool F16, lies_t LA, lies_t LB, bool SEG, bool SYMMETRIC, class E> __global__ __launch_bounds__(K::THREADS, 2) void k_product16(product_t q, E e)
 {
     extern __shared__ __attribute__((aligned(1024))) uint8_t smem[];
-    int64_t n0, d0;
-    place_of<K, SYMMETRIC>(q, n0, d0);
-    float *const part = q.part + (int64_t)blockIdx.y * q.A.outer * q.B.outer;
-    int64_t all = SEG ? q.K * q.seg.count : q.K;
+    int64_t n0, d0, begin = 0, all = SEG ? q.K * q.seg.count : q.K, end = all;
+    const uint32_t past = blockIdx.x - q.whole;
+    const bool sliced = blockIdx.x >= q.whole && q.slices > 1;
+    place_of<K, SYMMETRIC>(q.nt, q.dt, blockIdx.x < q.whole ? run_of_xcd(blockIdx.x, q.whole) : q.whole + past / q.slices, n0, d0);
     if constexpr (E::COUNTED) {
-        if (q.K_of) all = __builtin_amdgcn_readfirstlane(*q.K_of);
+        if (q.K_of) end = all = __builtin_amdgcn_readfirstlane(*q.K_of);
         if (q.rows_of) {
             q.A.outer = __builtin_amdgcn_readfirstlane(*q.rows_of);
             if (n0 >= q.A.outer) return;
         }
     }
-    const int64_t begin = (int64_t)blockIdx.y * q.slice, till = begin + q.slice < all ? begin + q.slice : all, end = till < begin ? begin : till;
+    if (sliced) {
+        begin = past % q.slices * q.slice;
+        end = begin + q.slice < all ? begin + q.slice : all < begin ? begin : all;
+    }
     v4f acc[K::MT][K::NT];
     multiply<K, F16, LA, LB, SEG>(q, n0, d0, begin, end, smem, acc);
-    if (q.part)
-        finish_tile<K, false>(q, n0, d0, smem, acc, store_part_t{part, q.B.outer});
+    if (sliced)
+        finish_tile<K, false>(q, n0, d0, smem, acc, store_part_t{q.part + (int64_t)past * K::TM * K::TN, n0, d0, K::TN});
     else
         finish_tile<K, SYMMETRIC>(q, n0, d0, smem, acc, e);
 }
 
-// The sums of the slices, in their order, finished.  A lane has four columns.  SYMMETRIC: `tile` is the tiles' edge; above the diagonal of tiles the sums are those of the
-// mirror image.
-template <bool SYMMETRIC, class E>
-__global__ __launch_bounds__(256) void k_join16(const float *part, int slices, int64_t rows, int64_t cols, int tile, const int32_t *rows_of, E e)
+// The sums of the slices of the tiles that have some, in their order, finished: a wave has 32 rows of 32 columns of a tile.
+template <class K, bool SYMMETRIC, class E> __global__ __launch_bounds__(64) void k_join16(product_t q, E e)
 {
-    const int64_t c = ((int64_t)blockIdx.y * 64 + (threadIdx.x & 63)) * 4, r = (int64_t)blockIdx.x * 4 + (threadIdx.x >> 6);
-    if (c >= cols || r >= (rows_of ? *rows_of : rows)) return;
-    const int have = (int)(cols - c < 4 ? cols - c : 4);
-    const typename E::more_t more = e.get(r, c, have);
-    float v[4] = {};
-    const bool turned = SYMMETRIC && r / tile < c / tile;
-    const float *p = turned ? part + c * cols + r : part + r * cols + c;
-    const int64_t across = turned ? cols : 1;
-    if (have == 4 && !turned) {
-#pragma unroll 4
-        for (int s = 0; s < slices; ++s, p += rows * cols) {
-            const u32x4 a = *reinterpret_cast<const u32x4_e4 *>(p);
-#pragma unroll
-            for (int i = 0; i < 4; ++i) v[i] += __uint_as_float(a[i]);
-        }
-    } else {
-        for (int s = 0; s < slices; ++s, p += rows * cols)
-#pragma unroll
-            for (int i = 0; i < 4; ++i)
-                if (i < have) v[i] += p[i * across];
+    constexpr int PITCH = 36, ACROSS = K::TN / 32, PATCHES = K::TM / 32 * ACROSS, STEPS = 4;
+    __shared__ float patch[SYMMETRIC ? 32 * PITCH : 1];
+    const uint32_t tail = blockIdx.x / PATCHES, in = blockIdx.x % PATCHES;
+    const int lane = threadIdx.x, c4 = (lane & 7) * 4, r0 = lane >> 3;
+    int64_t n0, d0;
+    place_of<K, SYMMETRIC>(q.nt, q.dt, q.whole + tail, n0, d0);
+    if constexpr (E::COUNTED) {
+        if (q.rows_of) q.A.outer = *q.rows_of;
     }
-    e.apply(r, c, have, make_float4(v[0], v[1], v[2], v[3]), more);
+    const int64_t first = n0 + in / ACROSS * 32, c0 = d0 + in % ACROSS * 32, r = first + r0, c = c0 + c4;
+    const auto spot = [&](int i) { return spot_t{first + 8 * i, c0, (uint32_t)r0, (uint32_t)c4}; };
+    const int have = (int)(q.B.outer - c < 4 ? q.B.outer - c : 4);
+    const float *p = q.part + (int64_t)tail * q.slices * K::TM * K::TN + (r - n0) * K::TN + (c - d0); // of every element of a tile, whether C has it or not
+    typename E::column_t column;
+    typename E::more_t more[STEPS];
+    if (have > 0) column = e.column(c, have);
+    float4 sum[STEPS];
+#pragma unroll
+    for (int i = 0; i < STEPS; ++i) {
+        sum[i] = make_float4(0.0f, 0.0f, 0.0f, 0.0f);
+        if (have > 0 && r + 8 * i < q.A.outer) more[i] = e.get(spot(i), have);
+    }
+#pragma unroll 8
+    for (uint32_t s = 0; s < q.slices; ++s, p += K::TM * K::TN)
+#pragma unroll
+        for (int i = 0; i < STEPS; ++i) {
+            const float4 v = *reinterpret_cast<const float4 *>(p + i * 8 * K::TN);
+            sum[i] = make_float4(sum[i].x + v.x, sum[i].y + v.y, sum[i].z + v.z, sum[i].w + v.w);
+        }
+#pragma unroll
+    for (int i = 0; i < STEPS; ++i)
+        if (have > 0 && r + 8 * i < q.A.outer) {
+            const float4 done = e.apply(spot(i), have, sum[i], column, more[i]);
+            if constexpr (SYMMETRIC) *reinterpret_cast<float4 *>(patch + (r0 + 8 * i) * PITCH + c4) = done;
+        }
+    if constexpr (SYMMETRIC) {
+        if (n0 == d0) return;
+        lds_between_lanes();
+        put_mirror<2>(q, first, c0, patch, e);
+    }
 }
 
 // to = factor v + add, of bf16 or float.  place (or nullptr): which of `to`'s rows row r is.  by (or nullptr): a number on the device that the factor is multiplied by.
 struct grad_t {
     static constexpr bool COUNTED = true;
+    static constexpr int AHEAD = 2;
+    typedef nothing_t column_t;
     typedef float4 more_t;
     adahop_tensor_t to, add;
     const int32_t *place;
     float factor;
     const float *by;
-    __device__ __forceinline__ more_t get(int64_t r, int64_t c, int have) const { return get4(add, r, c, have); }
-    __device__ __forceinline__ float4 apply(int64_t r, int64_t c, int have, float4 v, more_t more) const
+    __device__ __forceinline__ column_t column(int64_t, int) const { return {}; }
+    __device__ __forceinline__ more_t get(const spot_t &s, int have) const { return get4(add, s.row(), s.col(), have); }
+    __device__ __forceinline__ float4 apply(const spot_t &s, int have, float4 v, column_t, more_t more) const
     {
         const float f = by ? factor * *by : factor, scale[4] = {f, f, f, f};
-        put4(to, place ? place[r] : r, c, have, scale, v, more);
+        put4(to, place ? place[s.row()] : s.row(), s.col(), have, scale, v, more);
         return v;
     }
 };
@@ -442,38 +520,40 @@ struct grad_t {
 // ---- host ----------------------------------------------------------------------------------------------------------------------
 // Tiles and slices of a product by its expected time.
 struct plan16_t {
-    bool large;
-    int slices;
+    int edge;
+    uint32_t tiles, whole, slices; // of the tiles behind the whole ones
     int64_t slice;
     size_t part_bytes;
 };
 
-// As measured for the weight gradient from a checkpoint (plan_of in wgrad8.hip), in microseconds on 256 compute units: a stage of a round of workgroups 0.7 with the large
-// tiles, one workgroup per compute unit; with the small ones 0.5 where there are two per compute unit, 0.3 where there is one; a round's beginning and end 4 and 2.5.
-inline plan16_t plan16(int64_t rows, int64_t cols, int64_t K, bool symmetric)
+// In microseconds, on 256 compute units: a stage of a round of workgroups takes 0.74 with tiles of 256, 0.43 of 192, one workgroup per compute unit; of 128 0.6 where there are two
+// per compute unit, 0.3 where there is one; a round's beginning and end 12, 10 and 6.  Whole rounds of tiles are computed whole.  What is left is cut into slices if they,
+// their sums' way to memory and back and one launch more take less time than another round.  `slices_at_most` = 1: never.
+inline plan16_t plan16(int64_t rows, int64_t cols, int64_t K, bool symmetric, int64_t slices_at_most = 64)
 {
-    const auto count = [&](int64_t t) { return symmetric ? ceil_div(rows, t) * (ceil_div(rows, t) + 1) / 2 : ceil_div(rows, t) * ceil_div(cols, t); };
-    const int64_t stages = ceil_div(K, STAGE), large = count(256), small = count(128);
-    plan16_t p = {};
-    double best = 0.0;
-    for (int64_t slices = 1; slices <= 64 && (slices == 1 || stages / slices >= 8); ++slices) {
-        const int64_t each = ceil_div(ceil_div(stages, slices), 2) * 2; // stages per slice; the kernel takes them in pairs
-        const int64_t number = ceil_div(stages, each);
-        const double join = number > 1 ? 6.0 + (double)number * rows * cols * 8 / 5e6 : 0.0;
-        const int64_t rounds = small * number / 512, over = small * number % 512;
-        const double in_large = ceil_div(large * number, 256) * (4.0 + 0.7 * each) + join;
-        const double in_small = (rounds + (over > 0)) * 2.5 + (rounds * 0.5 + (over > 256 ? 0.5 : over > 0 ? 0.3 : 0.0)) * each + join;
-        const double t = in_large < in_small ? in_large : in_small;
-        if (p.slices == 0 || t < best) {
-            best = t;
-            p.large = in_large < in_small;
-            p.slices = (int)number;
-            p.slice = each * STAGE;
+    plan16_t best = {};
+    double best_time = 0.0;
+    const int64_t stages = ceil_div(ceil_div(K, STAGE), 2) * 2; // the kernel takes them in pairs
+    for (const int edge : {256, 192, 128}) {
+        const int64_t room = edge > 128 ? 256 : 512, down = ceil_div(rows, edge), across = ceil_div(cols, edge);
+        const int64_t tiles = symmetric ? down * (down + 1) / 2 : down * across, rest = tiles % room;
+        const double each = edge == 256 ? 0.74 : edge == 192 ? 0.43 : 0.6, ends = edge == 256 ? 12.0 : edge == 192 ? 10.0 : 6.0, whole = (double)(tiles / room) * (ends + each * (double)stages);
+        const auto a_round = [&](int64_t workgroups, int64_t of) { return ends + (workgroups <= 256 && edge == 128 ? 0.3 : each) * (double)of; };
+        plan16_t p = {edge, (uint32_t)tiles, (uint32_t)tiles, 1, 0, 0};
+        double time = whole + (rest ? a_round(rest, stages) : 0.0);
+        for (int64_t s = 2; rest && s <= slices_at_most && stages / s >= 4; ++s) {
+            const int64_t of = ceil_div(ceil_div(stages, s), 2) * 2, number = ceil_div(stages, of);
+            const double t = whole + (double)(rest * number / room) * (ends + each * (double)of) + (rest * number % room ? a_round(rest * number % room, of) : 0.0) + 8.0 +
+                             (double)(rest * number * edge * edge) * 8 / 5e6;
+            if (t < time) {
+                time = t;
+                p.whole = (uint32_t)(tiles - rest), p.slices = (uint32_t)number, p.slice = of * STAGE;
+                p.part_bytes = (size_t)rest * number * edge * edge * sizeof(float);
+            }
         }
-        if (join > best) break;
+        if (edge == 256 || time < best_time) best = p, best_time = time;
     }
-    p.part_bytes = p.slices > 1 ? (size_t)p.slices * rows * cols * sizeof(float) : 0;
-    return p;
+    return best;
 }
 
 template <class K, bool F16, lies_t LA, lies_t LB, bool SEG, bool SYMMETRIC, class E> inline int configure_product16()
@@ -481,10 +561,14 @@ template <class K, bool F16, lies_t LA, lies_t LB, bool SEG, bool SYMMETRIC, cla
     return check_hip(hipFuncSetAttribute(reinterpret_cast<const void *>(&k_product16<K, F16, LA, LB, SEG, SYMMETRIC, E>), hipFuncAttributeMaxDynamicSharedMemorySize, K::LDS));
 }
 
-template <class K, bool F16, lies_t LA, lies_t LB, bool SEG, bool SYMMETRIC, class E> inline int launch_tiles16(product_t &q, int slices, const E &e, hipStream_t st)
+template <class K, bool F16, lies_t LA, lies_t LB, bool SEG, bool SYMMETRIC, class E> inline int launch_tiles16(product_t &q, const plan16_t &plan, const E &e, hipStream_t st)
 {
+    const uint32_t rest = plan.tiles - plan.whole;
     q.nt = (uint32_t)ceil_div(q.A.outer, K::TM), q.dt = (uint32_t)ceil_div(q.B.outer, K::TN);
-    k_product16<K, F16, LA, LB, SEG, SYMMETRIC, E><<<dim3(SYMMETRIC ? q.nt * (q.nt + 1) / 2 : q.nt * q.dt, slices), K::THREADS, K::LDS, st>>>(q, e);
+    k_product16<K, F16, LA, LB, SEG, SYMMETRIC, E><<<plan.whole + rest * plan.slices, K::THREADS, K::LDS, st>>>(q, e);
+    const int rc = check_launch();
+    if (rc != ADAHOP_OK || !rest) return rc;
+    k_join16<K, SYMMETRIC, E><<<rest * (K::TM / 32) * (K::TN / 32), 64, 0, st>>>(q, e);
     return check_launch();
 }
 
@@ -492,19 +576,16 @@ template <class K, bool F16, lies_t LA, lies_t LB, bool SEG, bool SYMMETRIC, cla
 template <bool F16, lies_t LA, lies_t LB, bool SEG, bool SYMMETRIC, class E>
 inline int launch_product16(const plan16_t &plan, product_t q, const E &e, void *part, hipStream_t st)
 {
-    q.slice = plan.slice;
-    q.part = plan.slices > 1 ? static_cast<float *>(part) : nullptr;
-    const int rc = plan.large ? launch_tiles16<tile256_t, F16, LA, LB, SEG, SYMMETRIC>(q, plan.slices, e, st)
-                              : launch_tiles16<tile128_t, F16, LA, LB, SEG, SYMMETRIC>(q, plan.slices, e, st);
-    if (rc != ADAHOP_OK || !q.part) return rc;
-    k_join16<SYMMETRIC, E><<<dim3((unsigned)ceil_div(q.A.outer, 4), (unsigned)ceil_div(q.B.outer, 256)), 256, 0, st>>>(q.part, plan.slices, q.A.outer, q.B.outer,
-                                                                                                                 plan.large ? 256 : 128, q.rows_of, e);
-    return check_launch();
+    q.whole = plan.whole, q.slices = plan.slices, q.slice = plan.slice;
+    q.part = static_cast<float *>(part);
+    return plan.edge == 256 ? launch_tiles16<tile256_t, F16, LA, LB, SEG, SYMMETRIC>(q, plan, e, st)
+           : plan.edge == 192 ? launch_tiles16<tile192_t, F16, LA, LB, SEG, SYMMETRIC>(q, plan, e, st) : launch_tiles16<tile128_t, F16, LA, LB, SEG, SYMMETRIC>(q, plan, e, st);
 }
 
-template <bool F16, lies_t LA, lies_t LB, bool SEG, bool SYMMETRIC, class E> inline int configure_both16()
+template <bool F16, lies_t LA, lies_t LB, bool SEG, bool SYMMETRIC, class E> inline int configure_all16()
 {
-    const int rc = configure_product16<tile256_t, F16, LA, LB, SEG, SYMMETRIC, E>();
+    int rc = configure_product16<tile256_t, F16, LA, LB, SEG, SYMMETRIC, E>();
+    if (rc == ADAHOP_OK) rc = configure_product16<tile192_t, F16, LA, LB, SEG, SYMMETRIC, E>();
     return rc == ADAHOP_OK ? configure_product16<tile128_t, F16, LA, LB, SEG, SYMMETRIC, E>() : rc;
 }
 
