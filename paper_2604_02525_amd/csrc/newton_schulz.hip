@@ -90,7 +90,7 @@ __global__ __launch_bounds__(256) void k_squares(source_t s, double *part)
     if (threadIdx.x == 0) part[blockIdx.x] = of_wave[0] + of_wave[1] + of_wave[2] + of_wave[3];
 }
 
-// Where the iterates are held: [rows_pad][ld], both multiples of 32, zeros outside the matrix.
+// Where the iterates are held: [rows_pad][ld], both multiples of 64, zeros outside the matrix.
 struct iterate_t {
     float *x;
     uint16_t *h; // fp16 of x 2^SX; split: what that leaves, in the same scale, `low` elements further on
@@ -112,7 +112,7 @@ __device__ __forceinline__ void put_half(uint16_t *high, uint16_t *low, bool spl
 }
 
 // The first iterate: U over its norm.
-__global__ __launch_bounds__(256) void k_first(source_t s, const double *part, int parts, float eps, iterate_t to, int64_t rows_pad)
+__global__ __launch_bounds__(256) void k_first(source_t s, const double *part, int parts, float eps, iterate_t to, int64_t rows_pad, int64_t cols_pad)
 {
     __shared__ double of_wave[4];
     double sum = 0.0;
@@ -122,7 +122,7 @@ __global__ __launch_bounds__(256) void k_first(source_t s, const double *part, i
     if ((threadIdx.x & 63) == 0) of_wave[threadIdx.x >> 6] = sum;
     __syncthreads();
     const double inverse = 1.0 / (sqrt(of_wave[0] + of_wave[1] + of_wave[2] + of_wave[3]) + eps);
-    const int64_t pieces = to.ld / 8, all = rows_pad * pieces;
+    const int64_t pieces = cols_pad / 8, all = rows_pad * pieces;
     for (int64_t i = (int64_t)blockIdx.x * 256 + threadIdx.x; i < all; i += (int64_t)gridDim.x * 256) {
         const int64_t r = i / pieces, c = (i - r * pieces) * 8;
         const int n = r < s.rows ? (int)(s.cols - c < 8 ? s.cols - c : 8) : 0;
@@ -327,17 +327,22 @@ template <bool BY_ROW> struct update_t { // the last one, as a step of the weigh
 struct ns_plan_t {
     bool wide, split;
     int64_t rows, cols, side, length; // padded: the matrix's, the smaller one and the larger
+    int64_t ld, ld_side;              // of the iterate's rows, of the square matrices'
     plan16_t gram, poly, step;
     size_t sums, D, diagonal, O, P, x, h[2], part, total;
 };
+
+// Rows of a multiple of 8 KB of 16-bit elements are held a line further apart: a slab's pieces of all rows would lie in few of the caches' channels.
+int64_t row_pitch(int64_t elements) { return elements % 4096 ? elements : elements + 64; }
 
 ns_plan_t ns_plan(int64_t rows, int64_t cols)
 {
     ns_plan_t p;
     p.wide = rows <= cols;
-    p.rows = align_up(rows, 32), p.cols = align_up(cols, 32);
+    p.rows = align_up(rows, SLAB), p.cols = align_up(cols, SLAB);
     p.side = p.wide ? p.rows : p.cols, p.length = p.wide ? p.cols : p.rows;
     p.split = (p.wide ? rows : cols) <= SPLIT_SIDE;
+    p.ld = row_pitch(p.cols), p.ld_side = row_pitch(p.side);
     p.gram = plan16(p.side, p.side, p.length * (p.split ? 3 : 1), true);
     p.poly = plan16(p.side, p.side, p.side, true);
     p.step = plan16(p.rows, p.cols, p.side * (p.split ? 2 : 1), false);
@@ -350,7 +355,7 @@ ns_plan_t ns_plan(int64_t rows, int64_t cols)
         at = align_up(at + bytes, 256);
         return here;
     };
-    const size_t all = (size_t)p.rows * p.cols, square = (size_t)p.side * p.side;
+    const size_t all = (size_t)p.rows * p.ld, square = (size_t)p.side * p.ld_side;
     p.sums = take(PARTS * sizeof(double));
     p.D = take(p.side * sizeof(float));
     p.diagonal = take(p.side * sizeof(float));
@@ -385,7 +390,7 @@ struct ns_call_t {
     hipStream_t st;
     iterate_t at(int which) const
     {
-        return {reinterpret_cast<float *>(ws + p.x), reinterpret_cast<uint16_t *>(ws + p.h[which]), p.cols, p.split ? p.rows * p.cols : 0};
+        return {reinterpret_cast<float *>(ws + p.x), reinterpret_cast<uint16_t *>(ws + p.h[which]), p.ld, p.split ? p.rows * p.ld : 0};
     }
     float *D() const { return reinterpret_cast<float *>(ws + p.D); }
     float *diagonal() const { return reinterpret_cast<float *>(ws + p.diagonal); }
@@ -399,15 +404,15 @@ struct ns_call_t {
         q.A = q.B = {x.h, x.ld, p.side};
         q.K = p.length;
         q.seg = {3, {0, 0, x.low}, {0, x.low, 0}}; // high high + high low + low high
-        const gram_t e = {O(), D(), p.side};
+        const gram_t e = {O(), D(), p.ld_side};
         return p.wide ? launch_product16<true, ALONG, ALONG, SEG, true>(p.gram, q, e, ws + p.part, st) : launch_product16<true, DOWN, DOWN, SEG, true>(p.gram, q, e, ws + p.part, st);
     }
     int poly(const float (&k)[3]) const
     {
         product_t q = {};
-        q.A = q.B = {O(), p.side, p.side};
+        q.A = q.B = {O(), p.ld_side, p.side};
         q.K = p.side;
-        const poly_t e = {O(), D(), P(), diagonal(), p.side, k[0], k[1], k[2]};
+        const poly_t e = {O(), D(), P(), diagonal(), p.ld_side, k[0], k[1], k[2]};
         return launch_product16<true, ALONG, ALONG, false, true>(p.poly, q, e, ws + p.part, st);
     }
     // P X (wide), X P: with P symmetric, its rows serve as its columns
@@ -417,11 +422,11 @@ struct ns_call_t {
         product_t q = {};
         q.K = p.side;
         if constexpr (WIDE) {
-            q.A = {P(), p.side, p.rows}, q.B = {x.h, x.ld, p.cols};
+            q.A = {P(), p.ld_side, p.rows}, q.B = {x.h, x.ld, p.cols};
             q.seg = {2, {0, 0, 0}, {0, x.low, 0}};
             return launch_product16<true, ALONG, DOWN, SEG, false>(p.step, q, e, ws + p.part, st);
         } else {
-            q.A = {x.h, x.ld, p.rows}, q.B = {P(), p.side, p.cols};
+            q.A = {x.h, x.ld, p.rows}, q.B = {P(), p.ld_side, p.cols};
             q.seg = {2, {0, x.low, 0}, {0, 0, 0}};
             return launch_product16<true, ALONG, ALONG, SEG, false>(p.step, q, e, ws + p.part, st);
         }
@@ -435,7 +440,7 @@ template <bool SEG, bool WIDE> int iterate(const ns_call_t &c, const adahop_newt
         int rc = c.gram<SEG>(i & 1);
         if (rc == ADAHOP_OK) rc = c.poly(k);
         if (rc != ADAHOP_OK) return rc;
-        const carried_t<WIDE> from = {c.at(0).x, c.diagonal(), c.p.cols};
+        const carried_t<WIDE> from = {c.at(0).x, c.diagonal(), c.p.ld};
         if (i + 1 < m.steps)
             rc = c.step<SEG, WIDE>(i & 1, step_t<WIDE>{from, c.at((i & 1) ^ 1)});
         else if (u)
@@ -476,7 +481,7 @@ int launch_newton_schulz(const adahop_newton_schulz_t &m, const adahop_tensor_t 
     k_squares<<<parts, 256, 0, st>>>(s, sums);
     if ((rc = check_launch()) != ADAHOP_OK) return rc;
     const int64_t blocks = ceil_div(c.p.rows * (c.p.cols / 8), 256);
-    k_first<<<(unsigned)(blocks < 4096 ? blocks : 4096), 256, 0, st>>>(s, sums, parts, m.eps, c.at(0), c.p.rows);
+    k_first<<<(unsigned)(blocks < 4096 ? blocks : 4096), 256, 0, st>>>(s, sums, parts, m.eps, c.at(0), c.p.rows, c.p.cols);
     if ((rc = check_launch()) != ADAHOP_OK) return rc;
     if (c.p.split) return c.p.wide ? iterate<true, true>(c, m, out, u) : iterate<true, false>(c, m, out, u);
     return c.p.wide ? iterate<false, true>(c, m, out, u) : iterate<false, false>(c, m, out, u);

@@ -5,12 +5,15 @@
 // Either operand may hold the contraction along its rows (ALONG, [outer][K]) or down its columns (DOWN, [K][outer]), so that no operand is ever transposed
 // in memory: a gradient of logits [tokens][vocabulary] enters one product by its rows and another by its columns.
 //
-// The scheme is that of the weight gradient from a checkpoint (wgrad8.hip): both operands go to a ring of stages in LDS by copies that pass no register, 32
-// elements of the contraction a stage; a wave's 16 x 16 x 32 instructions are fed from LDS a stage ahead; one barrier per stage.  A DOWN operand is turned by
-// the transposing reads of LDS; an ALONG one is read as it lies, 16 bytes (eight elements of a row) per lane.  What lies outside an operand reads as zero, in both.
+// The scheme is that of the weight gradient from a checkpoint (wgrad8.hip): both operands go to LDS by copies that pass no register, a wave's 16 x 16 x 32 instructions are fed
+// from LDS 32 elements of the contraction ahead.  A DOWN operand is turned by the transposing reads of LDS; an ALONG one is read as it lies, 16 bytes (eight elements
+// of a row) per lane.  What lies outside an operand reads as zero, in both.  Here LDS holds two slabs of 64 elements of the contraction rather than four of 32: an ALONG
+// operand's rows are then fetched in whole lines of 128 bytes (where both are DOWN, whose rows are long, in halves all the same, further ahead).  In halves of them the L2s' requests, not the matrix cores, set the pace: 32 compute units' took as long as their matrix instructions
+// (matrix cores busy 53 % against 79 % with both operands DOWN).
 //
-// LDS layout of a stage of an ALONG operand: 64 bytes a row, its four pieces of 16 bytes exchanged by the row's bits 2 and 3: the sixteen rows that a quarter of a wave
-// reads one piece of lie in sixteen different sixteenths of the banks.
+// LDS layout of a slab of an ALONG operand: 128 bytes a row, its eight pieces of 16 bytes exchanged by a number for the row's bits 1 to 3 (exchange_of).  A read of 16 bytes per lane serves
+// sixteen lanes at a time, not lanes in a row: any two of the sixteen are in different banks for sixteen rows with one piece, for four rows at either end with one piece and
+// the eight between them with its neighbour, and for eight rows with two neighbouring pieces.  With a number that does so for the first alone half of the reads' cycles were conflicts (counted).
 #pragma once
 #include "tile_copies.h"
 
@@ -21,6 +24,10 @@ namespace {
 typedef _Float16 v8h __attribute__((ext_vector_type(8)));
 
 enum lies_t { ALONG, DOWN };
+
+constexpr int SLAB = 64; // of the contraction: two matrix instructions'
+
+__device__ __forceinline__ uint32_t exchange_of(uint32_t q) { return (2 * q & 7) ^ (q >> 2) * 5; } // 0, 2, 4, 6, 5, 7, 1, 3
 
 struct side_t {
     const uint16_t *data; // 16-byte aligned
@@ -35,7 +42,7 @@ struct segments_t {
 
 struct product_t {
     side_t A, B;
-    int64_t K;       // a multiple of 8 where an operand is ALONG; of 32 with several segments
+    int64_t K;       // a multiple of 8 where an operand is ALONG; of 64 with several segments
     uint32_t nt, dt; // tiles along A's outer index and B's
     // The first `whole` tiles are a workgroup's each.  Of the others a workgroup has one of `slices` slices of the contraction (`slice` elements of all segments' K, a
     // multiple of 64), whose sums go to part, [tile][slice][TM][TN]; with one slice they are whole too.
@@ -46,17 +53,17 @@ struct product_t {
     const int32_t *rows_of, *K_of; // (or nullptr) how many of A's outer indices and of the contraction's elements there are, where only the device knows
 };
 
-// Tiles of C by WN x WD waves of 16 MT x 16 NT, a ring of RING stages.
-template <int MT_, int NT_, int WN_, int WD_, int RING_> struct shape_t {
-    static constexpr int MT = MT_, NT = NT_, WN = WN_, WD = WD_, RING = RING_;
-    static constexpr int WAVES = WN * WD, THREADS = 64 * WAVES, TM = 16 * WN * MT, TN = 16 * WD * NT, RA = 2 * TM, RB = 2 * TN; // bytes of a row of a DOWN stage
-    static constexpr uint32_t A = STAGE * RA, B = STAGE * RB, SLOT = A + B, LDS = RING * SLOT;
-    static constexpr int COPIES = A / 1024 / (WAVES / 2); // per wave and stage: half of the waves copy A, the others B
-    static_assert(TM == TN && COPIES * (WAVES / 2) * 1024 == A, "whole copies");
+// Tiles of C by WN x WD waves of 16 MT x 16 NT.
+template <int MT_, int NT_, int WN_, int WD_> struct shape_t {
+    static constexpr int MT = MT_, NT = NT_, WN = WN_, WD = WD_;
+    static constexpr int WAVES = WN * WD, THREADS = 64 * WAVES, TM = 16 * WN * MT, TN = 16 * WD * NT, RA = 2 * TM, RB = 2 * TN; // bytes of a row of a DOWN slab
+    static constexpr uint32_t A = SLAB * RA, B = SLAB * RB, SLOT = A + B, LDS = 2 * SLOT;
+    static constexpr int COPIES = A / 1024 / (WAVES / 2); // per wave and slab: half of the waves copy A, the others B
+    static_assert(TM == TN && COPIES * (WAVES / 2) * 1024 == A && COPIES % 2 == 0, "whole copies");
     // DOWN: by what the pieces of 32 bytes of a row are exchanged, so that the eight rows of a transposing read of half a wave (four consecutive ones and those 8 further on)
     // lie in different banks.  Rows of a multiple of 256 bytes begin at the same bank: by bits 0, 1 and 3 of the row.  Rows of 128 or 384: two of them lie apart, by bits 1 and 3.
     static __device__ __forceinline__ uint32_t turn_of(uint32_t row, uint32_t bytes) { return bytes % 256 ? (row >> 1 & 1) | (row >> 2 & 2) : (row & 3) | (row >> 1 & 4); }
-    // What lane l of copy number `copy` of a stage reads: its row, and the byte in it
+    // What lane l of copy number `copy` of a slab reads: its row, and the byte in it
     static __device__ __forceinline__ uint32_t row_of(uint32_t copy, uint32_t l, uint32_t bytes) { return (copy * 1024 + l * 16) / bytes; }
     static __device__ __forceinline__ uint32_t byte_of(uint32_t row, uint32_t l, uint32_t copy, uint32_t bytes)
     {
@@ -65,18 +72,19 @@ template <int MT_, int NT_, int WN_, int WD_, int RING_> struct shape_t {
     }
 };
 
-typedef shape_t<8, 4, 2, 4, 4> tile256_t;
-typedef shape_t<6, 3, 2, 4, 4> tile192_t;
-typedef shape_t<4, 4, 2, 2, 4> tile128_t;
+typedef shape_t<8, 4, 2, 4> tile256_t;
+typedef shape_t<6, 3, 2, 4> tile192_t;
+typedef shape_t<4, 4, 2, 2> tile128_t;
 
-// A wave's copies, all of one operand: the resource that a stage is read from, where it goes on, and what this lane reads of it.
-template <class K, bool SEG> struct copies_t {
-    static constexpr int OUTER = K::TM;
+// A wave's copies, all of one operand: the resource that a slab is read from, where it goes on, and what this lane reads of it.
+// UNIT: elements of the contraction that are copied at a time, a slab or half of one.
+template <class K, bool SEG, int UNIT> struct copies_t {
+    static constexpr int OUTER = K::TM, COPIES = K::COPIES * UNIT / SLAB;
     static constexpr uint32_t BYTES = 2 * OUTER;
     rsrc_t from;
-    uint32_t off[K::COPIES];
-    uint32_t full, last, step, beyond; // extents of a whole stage and of one at the contraction's end; beyond: what puts this lane's piece out of bounds there
-    int64_t hop[SEG ? 2 : 1];          // from the last stage of a segment to the first of the next
+    uint32_t off[COPIES];
+    uint32_t full, last, step, beyond[2]; // extents of a whole unit and of one at the contraction's end; beyond: what puts this lane's piece of copies of either parity out of bounds there
+    int64_t hop[SEG ? 2 : 1];             // from the last unit of a segment to the first of the next
 
     // w: which of the waves that copy this operand
     __device__ __forceinline__ void set(lies_t lies, const side_t &s, int64_t K_, int64_t at, int64_t begin, uint32_t odd, uint32_t w, uint32_t lane, const int64_t (&starts)[3], int segment)
@@ -85,29 +93,31 @@ template <class K, bool SEG> struct copies_t {
         const int64_t most = s.outer - at, first = SEG ? starts[segment] : 0;
         if (lies == DOWN) {
 #pragma unroll
-            for (int i = 0; i < K::COPIES; ++i) {
-                const uint32_t row = K::row_of(w * K::COPIES + i, lane, BYTES);
-                off[i] = row * pitch + K::byte_of(row, lane, w * K::COPIES + i, BYTES);
+            for (int i = 0; i < COPIES; ++i) {
+                const uint32_t row = K::row_of(w * COPIES + i, lane, BYTES);
+                off[i] = row * pitch + K::byte_of(row, lane, w * COPIES + i, BYTES);
             }
             const uint32_t wide = (uint32_t)(most * 2 < BYTES ? most * 2 : BYTES); // bytes of a row, in whole words below
-            full = ((STAGE - 1) * pitch + wide + 3) & ~3u;
+            full = ((UNIT - 1) * pitch + wide + 3) & ~3u;
             last = odd ? ((odd - 1) * pitch + wide + 3) & ~3u : 0;
-            step = STAGE * pitch;
-            beyond = 0;
+            step = UNIT * pitch;
+            beyond[0] = beyond[1] = 0;
             from = resource(s.data + first + begin * s.ld + at, full);
         } else {
-            const uint32_t piece = (lane & 3) ^ (lane >> 4 & 3); // rows of four lanes: the row's bits 2 and 3 are the lane's 4 and 5
+            // eight lanes have a row: its bits 1 and 2 are the lane's 4 and 5, bit 3 is the copy's parity
+            const uint32_t piece[2] = {(lane & 7) ^ exchange_of(lane >> 4), (lane & 7) ^ exchange_of(4 + (lane >> 4))};
 #pragma unroll
-            for (int i = 0; i < K::COPIES; ++i) off[i] = ((w * K::COPIES + i) * 16 + (lane >> 2)) * pitch + piece * 16;
+            for (int i = 0; i < COPIES; ++i) off[i] = ((w * COPIES + i) * 8 + (lane >> 3)) * pitch + piece[i & 1] * 16;
             const uint32_t rows = (uint32_t)(most < OUTER ? most : OUTER);
-            full = (rows - 1) * pitch + 2 * STAGE;
+            full = (rows - 1) * pitch + 2 * SLAB;
             last = odd ? (rows - 1) * pitch + (odd + 7) / 8 * 16 : 0;
-            step = 2 * STAGE;
-            beyond = odd && piece * 8 >= odd ? 0x80000000u : 0;
+            step = 2 * SLAB;
+#pragma unroll
+            for (int i = 0; i < 2; ++i) beyond[i] = odd && piece[i] * 8 >= odd ? 0x80000000u : 0;
             from = resource(s.data + first + at * s.ld + begin, full);
         }
         if constexpr (SEG) {
-            const int64_t run = (K_ / STAGE - 1) * (int64_t)step; // bytes from a segment's first stage to its last
+            const int64_t run = (K_ / UNIT - 1) * (int64_t)step; // bytes from a segment's first unit to its last
 #pragma unroll
             for (int i = 0; i < 2; ++i) hop[i] = (starts[i + 1] - starts[i]) * 2 - run;
         }
@@ -146,36 +156,44 @@ __device__ __forceinline__ u32x4 lds_read16(uint32_t lds_addr) { return *(const 
 template <class K, bool F16, lies_t LA, lies_t LB, bool SEG>
 __device__ __forceinline__ void multiply(const product_t &q, int64_t n0, int64_t d0, int64_t begin, int64_t end, uint8_t *smem, v4f (&acc)[K::MT][K::NT])
 {
-    constexpr int MT = K::MT, NT = K::NT, RING = K::RING;
+    constexpr int MT = K::MT, NT = K::NT;
+    constexpr bool FINE = LA == DOWN && LB == DOWN; // halves of slabs are copied, three ahead
+    constexpr int UNIT = FINE ? SLAB / 2 : SLAB;
+    typedef copies_t<K, SEG, UNIT> mine_t;
+    constexpr int COPIES = mine_t::COPIES;
     const int tid = threadIdx.x, lane = tid & 63, w = __builtin_amdgcn_readfirstlane(tid >> 6), wn = w / K::WD, wd = w % K::WD;
     const uint32_t base = __builtin_amdgcn_readfirstlane(lds_address(smem));
-    int32_t left = __builtin_amdgcn_readfirstlane((int32_t)(end - begin)), ahead = left; // elements from the stage at hand, and from the one that is copied next, on
+    int32_t left = __builtin_amdgcn_readfirstlane((int32_t)(end - begin)), ahead = left; // elements from the slab at hand, and from what is copied next, on
     int segment = 0;
     uint32_t in = 0, run = 0;
     if constexpr (SEG) {
-        run = (uint32_t)(q.K / STAGE);
+        run = (uint32_t)(q.K / UNIT);
         segment = __builtin_amdgcn_readfirstlane((int)(begin / q.K));
         begin -= segment * q.K;
-        in = __builtin_amdgcn_readfirstlane((uint32_t)(begin / STAGE));
+        in = __builtin_amdgcn_readfirstlane((uint32_t)(begin / UNIT));
     }
-    const uint32_t odd = SEG ? 0u : (uint32_t)left % STAGE;
-    copies_t<K, SEG> mine;
+    const uint32_t odd = SEG ? 0u : (uint32_t)left % UNIT;
+    mine_t mine;
     const bool of_b = w >= K::WAVES / 2;
     if (of_b)
         mine.set(LB, q.B, q.K, d0, begin, odd, w - K::WAVES / 2, lane, q.seg.b, segment);
     else
         mine.set(LA, q.A, q.K, n0, begin, odd, w, lane, q.seg.a, segment);
     mine.settle();
-    uint32_t to = base, at = base; // slots: copied to next, read next
-    const auto after = [&](uint32_t slot) { return slot == base + (RING - 1) * K::SLOT ? base : slot + K::SLOT; };
-    uint32_t cut = 0;
-    // The resource of the stage that is copied next: a whole one, the contraction's end, or nothing.  Without a branch: it would end the block that the
+    const uint32_t own = of_b ? K::A + (w - K::WAVES / 2) * COPIES * 1024 : w * COPIES * 1024;
+    uint32_t to = base, at = base; // where is copied to next, the slab that is read next
+    const auto other = [&](uint32_t slot) { return slot == base ? base + K::SLOT : base; };
+    const auto after = [&](uint32_t place) { // FINE: slab, second half, the other slab, its second half
+        constexpr uint32_t HALF = SLAB / 2 * K::RA;
+        return place == base ? base + HALF : place == base + HALF ? base + K::SLOT : place == base + K::SLOT ? base + K::SLOT + HALF : base;
+    };
+    uint32_t cut[2] = {};
+    // The resource of what is copied next: a whole unit, the contraction's end, or nothing.  Without a branch: it would end the block that the
     // instructions around are scheduled in.
     const auto trim = [&] {
-        mine.from.z = ahead >= STAGE ? mine.full : ahead > 0 ? mine.last : 0;
-        if constexpr (LA == ALONG || LB == ALONG) cut = ahead >= STAGE ? 0 : mine.beyond;
+        mine.from.z = ahead >= UNIT ? mine.full : ahead > 0 ? mine.last : 0;
+        if constexpr (LA == ALONG || LB == ALONG) cut[0] = ahead >= UNIT ? 0 : mine.beyond[0], cut[1] = ahead >= UNIT ? 0 : mine.beyond[1];
     };
-    const uint32_t own = w * K::COPIES * 1024; // B's copies follow A's
     const auto copied = [&] {
         if constexpr (SEG) {
             const bool cross = ++in == run;
@@ -185,32 +203,32 @@ __device__ __forceinline__ void multiply(const product_t &q, int64_t n0, int64_t
         } else {
             mine.forward(mine.step);
         }
-        ahead -= STAGE;
-        to = after(to);
+        ahead -= UNIT;
+        to = FINE ? after(to) : other(to);
         trim();
     };
     const auto copy = [&](auto number) {
         constexpr int i = decltype(number)::value;
-        dma16_bounded<i * 1024>(mine.from, LA == ALONG || LB == ALONG ? mine.off[i] | cut : mine.off[i], __builtin_amdgcn_readfirstlane(to + own));
+        dma16_bounded<i * 1024>(mine.from, LA == ALONG || LB == ALONG ? mine.off[i] | cut[i & 1] : mine.off[i], __builtin_amdgcn_readfirstlane(to + own));
     };
 
-    // What this lane reads: the matrix instruction wants the eight elements from 8 (lane / 16) on of row or column lane % 16.  DOWN: four lanes of a group of 16
-    // supply the four pieces of a row, of four columns each, and the group receives four rows: two reads.  ALONG: one read.
+    // What this lane reads of a half slab: the matrix instruction wants the eight elements from 8 (lane / 16) on of row or column lane % 16.  DOWN: four lanes of a group of
+    // 16 supply the four pieces of a row, of four columns each, and the group receives four rows: two reads.  ALONG: one read.
     const int s16 = lane & 15, g = lane >> 4;
     constexpr int PA = LA == DOWN ? 2 : 1, PB = LB == DOWN ? 2 : 1;
-    uint32_t ra[PA == 2 ? MT : 1], rb[PB == 2 ? NT : 1];
-    const uint32_t down = 8 * g + (s16 >> 2), along = s16 * 64 + ((g ^ (s16 >> 2)) * 16);
+    uint32_t ra[PA == 2 ? MT : 2], rb[PB == 2 ? NT : 2]; // ALONG: of either half
+    const uint32_t down = 8 * g + (s16 >> 2), along = s16 * 128 + ((g ^ exchange_of(s16 >> 1)) * 16);
     if constexpr (PA == 2) {
 #pragma unroll
         for (int m = 0; m < MT; ++m) ra[m] = down * K::RA + (((wn * MT + m) ^ K::turn_of(down, K::RA)) * 32) + 8 * (s16 & 3);
     } else {
-        ra[0] = wn * MT * 1024 + along;
+        ra[0] = wn * MT * 2048 + along, ra[1] = wn * MT * 2048 + (along ^ 64);
     }
     if constexpr (PB == 2) {
 #pragma unroll
         for (int n = 0; n < NT; ++n) rb[n] = K::A + down * K::RB + (((wd * NT + n) ^ K::turn_of(down, K::RB)) * 32) + 8 * (s16 & 3);
     } else {
-        rb[0] = K::A + wd * NT * 1024 + along;
+        rb[0] = K::A + wd * NT * 2048 + along, rb[1] = K::A + wd * NT * 2048 + (along ^ 64);
     }
 #pragma unroll
     for (int m = 0; m < MT; ++m)
@@ -218,35 +236,36 @@ __device__ __forceinline__ void multiply(const product_t &q, int64_t n0, int64_t
         for (int n = 0; n < NT; ++n) acc[m][n] = {};
     u32x2 fa[MT][2], fb[2][NT][2];
     uint32_t lies = 0;
-    const auto read_a = [&](int m, int part) {
+    const auto read_a = [&](int half, int m, int part) {
         if constexpr (PA == 2) {
             if (!part) lies = at + ra[m];
-            fa[m][part] = transposed(lies + 4 * part * K::RA);
+            fa[m][part] = transposed(lies + (32 * half + 4 * part) * K::RA);
         } else if (!part) {
-            const u32x4 v = lds_read16(at + ra[0] + m * 1024);
+            const u32x4 v = lds_read16(at + ra[half] + m * 2048);
             fa[m][0] = v.xy, fa[m][1] = v.zw;
         }
     };
-    const auto read_b = [&](int set, int n, int part) {
+    const auto read_b = [&](int half, int n, int part) { // into the set of registers of that half
         if constexpr (PB == 2) {
             if (!part) lies = at + rb[n];
-            fb[set][n][part] = transposed(lies + 4 * part * K::RB);
+            fb[half][n][part] = transposed(lies + (32 * half + 4 * part) * K::RB);
         } else if (!part) {
-            const u32x4 v = lds_read16(at + rb[0] + n * 1024);
-            fb[set][n][0] = v.xy, fb[set][n][1] = v.zw;
+            const u32x4 v = lds_read16(at + rb[half] + n * 2048);
+            fb[half][n][0] = v.xy, fb[half][n][1] = v.zw;
         }
     };
-    constexpr int PLACES = MT * NT, BARRIER = NT - 1; // a stage's matrix instructions are places, with what is issued beside each
+    constexpr int PLACES = MT * NT, BARRIER = NT - 1; // a half slab's matrix instructions are places, with what is issued beside each
     constexpr int READS_B = PB * NT, EACH = (READS_B + (MT - 1) * (NT - 2) - 1) / ((MT - 1) * (NT - 2)); // reads of B beside one of the places for them
-    static_assert(NT > 2 && K::COPIES <= PLACES - NT, "what goes beside the matrix instructions fits");
+    constexpr int APART = !FINE && (PLACES - NT) / COPIES > 2 ? 2 : 1, FIRST = FINE ? PLACES - COPIES : BARRIER + 1; // places from one copy to the next, the first one's
+    static_assert(NT > 2 && COPIES * APART <= PLACES - NT, "what goes beside the matrix instructions fits");
 
     trim();
 #pragma unroll 1
-    for (int i = 0; i < RING - 1; ++i) {
-        static_for<0, K::COPIES>(copy);
+    for (int i = 0; i < (FINE ? 3 : 2); ++i) {
+        static_for<0, COPIES>(copy);
         copied();
     }
-    wait_for_copies<(RING - 2) * K::COPIES>();
+    wait_for_copies<(FINE ? 2 : 1) * COPIES>();
     // Everything that the compiler counts with the reads of LDS is done before these, and these are issued in the order of the loop's: its waits in
     // the loop go by what may be outstanding on either way into it.
     __builtin_amdgcn_s_waitcnt(0xc07f); // lgkmcnt(0)
@@ -257,37 +276,41 @@ __device__ __forceinline__ void multiply(const product_t &q, int64_t n0, int64_t
 #pragma unroll
     for (int m = 0; m < MT - 1; ++m) {
         ADAHOP_PIN();
-        read_a(m, 0), read_a(m, 1);
+        read_a(0, m, 0), read_a(0, m, 1);
     }
     ADAHOP_PIN();
-    const auto stage = [&](auto which) {
-        constexpr int set = decltype(which)::value;
+    // A's operands are read again, for the next half, behind the last of the NT matrix instructions that use them, B's into the other set of registers.  The last of a unit is
+    // read behind its last half's first instructions; after the barrier that follows, what comes two slabs later goes in its place, and the next unit, copied
+    // for at least the time of one and a half halves, is there for all waves.
+    const auto half = [&](auto which) {
+        constexpr int now = decltype(which)::value, next = now ^ 1;
         static_for<0, PLACES>([&](auto number) {
             constexpr int place = decltype(number)::value, m = place / NT, n = place % NT;
             const uint4 va = make_uint4(fa[m][0].x, fa[m][0].y, fa[m][1].x, fa[m][1].y);
-            const uint4 vb = make_uint4(fb[set][n][0].x, fb[set][n][0].y, fb[set][n][1].x, fb[set][n][1].y);
+            const uint4 vb = make_uint4(fb[now][n][0].x, fb[now][n][0].y, fb[now][n][1].x, fb[now][n][1].y);
             acc[m][n] = mfma16<F16>(va, vb, acc[m][n]);
-            if constexpr (m == 0 && n < 2) read_a(MT - 1, n); // of this stage
-            if constexpr (place == BARRIER) {
-                asm volatile("s_waitcnt vmcnt(%0)\n\ts_barrier" ::"n"((RING - 3) * K::COPIES) : "memory"); // the next stage is there
-                at = after(at);
+            if constexpr (m == 0 && n < 2) read_a(now, MT - 1, n);
+            if constexpr ((FINE || now == 1) && place == BARRIER) {
+                asm volatile("s_waitcnt vmcnt(%0) lgkmcnt(0)\n\ts_barrier" ::"n"(FINE ? COPIES : 0) : "memory");
+                if constexpr (now == 1) at = other(at);
             }
             if constexpr (m > 0) {
                 constexpr int first = ((m - 1) * (NT - 2) + n - 2) * EACH;
                 if constexpr (n < 2)
-                    read_a(m - 1, n);
+                    read_a(next, m - 1, n);
                 else
-                    static_for<first, first + EACH < READS_B ? first + EACH : READS_B>([&](auto i) { read_b(set ^ 1, decltype(i)::value / PB, decltype(i)::value % PB); });
+                    static_for<first, first + EACH < READS_B ? first + EACH : READS_B>([&](auto i) { read_b(next, decltype(i)::value / PB, decltype(i)::value % PB); });
             }
-            if constexpr (place >= PLACES - K::COPIES) copy(std::integral_constant<int, place - (PLACES - K::COPIES)>{});
+            if constexpr ((FINE || now == 1) && place >= FIRST && (place - FIRST) % APART == 0 && (place - FIRST) / APART < COPIES)
+                copy(std::integral_constant<int, (place - FIRST) / APART>{});
             ADAHOP_PIN();
         });
-        copied();
-        left -= STAGE;
+        if constexpr (FINE || now == 1) copied();
     };
-    while (left > 0) { // two stages, one of each set of B's registers; the second may be one of zeros
-        stage(std::integral_constant<int, 0>{});
-        stage(std::integral_constant<int, 1>{});
+    while (left > 0) {
+        half(std::integral_constant<int, 0>{});
+        half(std::integral_constant<int, 1>{});
+        left -= SLAB;
     }
 }
 
@@ -425,7 +448,7 @@ __device__ __forceinline__ void finish_tile(const product_t &q, int64_t n0, int6
     }
 }
 
-// SYMMETRIC: A = B up to segments, so is C; both outer extents are one multiple of 32.
+// SYMMETRIC: A = B up to segments, so is C; both outer extents are one multiple of 64.
 template <class K, bool F16, lies_t LA, lies_t LB, bool SEG, bool SYMMETRIC, class E> __global__ __launch_bounds__(K::THREADS, 2) void k_product16(product_t q, E e)
 {
     extern __shared__ __attribute__((aligned(1024))) uint8_t smem[];
@@ -526,14 +549,14 @@ struct plan16_t {
     size_t part_bytes;
 };
 
-// In microseconds, on 256 compute units: a stage of a round of workgroups takes 0.74 with tiles of 256, 0.43 of 192, one workgroup per compute unit; of 128 0.6 where there are two
+// In microseconds, on 256 compute units: half a slab of a round of workgroups takes 0.74 with tiles of 256, 0.43 of 192, one workgroup per compute unit; of 128 0.6 where there are two
 // per compute unit, 0.3 where there is one; a round's beginning and end 12, 10 and 6.  Whole rounds of tiles are computed whole.  What is left is cut into slices if they,
 // their sums' way to memory and back and one launch more take less time than another round.  `slices_at_most` = 1: never.
 inline plan16_t plan16(int64_t rows, int64_t cols, int64_t K, bool symmetric, int64_t slices_at_most = 64)
 {
     plan16_t best = {};
     double best_time = 0.0;
-    const int64_t stages = ceil_div(ceil_div(K, STAGE), 2) * 2; // the kernel takes them in pairs
+    const int64_t stages = ceil_div(K, SLAB) * 2; // of 32 elements of the contraction
     for (const int edge : {256, 192, 128}) {
         const int64_t room = edge > 128 ? 256 : 512, down = ceil_div(rows, edge), across = ceil_div(cols, edge);
         const int64_t tiles = symmetric ? down * (down + 1) / 2 : down * across, rest = tiles % room;
@@ -547,7 +570,7 @@ inline plan16_t plan16(int64_t rows, int64_t cols, int64_t K, bool symmetric, in
                              (double)(rest * number * edge * edge) * 8 / 5e6;
             if (t < time) {
                 time = t;
-                p.whole = (uint32_t)(tiles - rest), p.slices = (uint32_t)number, p.slice = of * STAGE;
+                p.whole = (uint32_t)(tiles - rest), p.slices = (uint32_t)number, p.slice = of * 32;
                 p.part_bytes = (size_t)rest * number * edge * edge * sizeof(float);
             }
         }
