@@ -10,7 +10,7 @@
 //   * X is carried in fp32; only what enters the products is rounded, to fp16 (times a power of two), so that a X is exact.
 //   * The diagonals of A and of b A + c A^2 are apart, in fp32: they are by far the largest elements, their rounding would be the largest error.  With A = D + O:
 //     the polynomial is b (D + O) + c (D^2 + D O + O D + O^2), of which the matrix cores form O^2, and its diagonal joins a in what multiplies the carried X.
-//   * Where the smaller side is at most 256, X enters as the sum of two fp16 numbers: errors there average over fewer elements, and the products cost little.
+//   * Where the smaller side is at most 128, X enters as the sum of two fp16 numbers: errors there average over fewer elements, and the products cost little.
 // The result is then 2e-4 to 1e-3 of its norm off the same iteration in 64 bits (bf16's own rounding: 1.7e-3).
 //
 // A and A^2 are symmetric: only tiles on and below the diagonal are computed, the mirror image is stored with them.
@@ -24,7 +24,7 @@ namespace {
 
 constexpr int SX = 12, SO = 12, SB = 10; // X, O and the polynomial's off-diagonal part are held times 2^S in fp16: below 16, 16 and 64
 constexpr int PARTS = 1024;              // workgroups of the sum of squares, at most
-constexpr int SPLIT_SIDE = 256;
+constexpr int SPLIT_SIDE = 128;
 
 constexpr float pow2(int e) { return e >= 0 ? (float)((uint64_t)1 << e) : 1.0f / (float)((uint64_t)1 << -e); }
 
@@ -95,6 +95,8 @@ struct iterate_t {
     float *x;
     uint16_t *h; // fp16 of x 2^SX; split: what that leaves, in the same scale, `low` elements further on
     int64_t ld, low; // low = 0: not split
+    uint16_t *turned; // h transposed, for small products (or nullptr), rows of ld_turned
+    int64_t ld_turned;
 };
 
 __device__ __forceinline__ void put_half(uint16_t *high, uint16_t *low, bool split, const float (&v)[4])
@@ -139,6 +141,59 @@ __global__ __launch_bounds__(256) void k_first(source_t s, const double *part, i
         *reinterpret_cast<float4 *>(to.x + at + 4) = make_float4(hi[0], hi[1], hi[2], hi[3]);
         put_half(to.h + at, to.h + to.low + at, to.low != 0, lo);
         put_half(to.h + at + 4, to.h + to.low + at + 4, to.low != 0, hi);
+    }
+}
+
+// Eight elements of a column of the iterate as part of a row of its transpose.
+__device__ __forceinline__ void put_half_turned(const iterate_t &t, int64_t c, int64_t r, const float (&v)[8])
+{
+    uint16_t *const to = t.turned + c * t.ld_turned + r;
+    float lo[4], hi[4];
+#pragma unroll
+    for (int i = 0; i < 4; ++i) lo[i] = v[i], hi[i] = v[i + 4];
+    put_half(to, to + t.low, t.low != 0, lo);
+    put_half(to + 4, to + 4 + t.low, t.low != 0, hi);
+}
+
+// k_first for small products: the transpose as well, 64 x 64 elements a workgroup.
+__global__ __launch_bounds__(256) void k_first_turned(source_t s, const double *part, int parts, float eps, iterate_t to)
+{
+    __shared__ double of_wave[4];
+    __shared__ float tile[64][65];
+    double sum = 0.0;
+    for (int i = threadIdx.x; i < parts; i += 256) sum += part[i];
+#pragma unroll
+    for (int k = 1; k < 64; k *= 2) sum += __shfl_xor(sum, k);
+    if ((threadIdx.x & 63) == 0) of_wave[threadIdx.x >> 6] = sum;
+    __syncthreads();
+    const double inverse = 1.0 / (sqrt(of_wave[0] + of_wave[1] + of_wave[2] + of_wave[3]) + eps);
+    const int64_t r0 = (int64_t)blockIdx.x * 64, c0 = (int64_t)blockIdx.y * 64;
+#pragma unroll
+    for (int p = 0; p < 2; ++p) {
+        const int i = (threadIdx.x >> 3) + 32 * p, j = (threadIdx.x & 7) * 8;
+        const int64_t r = r0 + i, c = c0 + j, at = r * to.ld + c;
+        const int n = r < s.rows ? (int)(s.cols - c < 8 ? s.cols - c : 8) : 0;
+        float u[8] = {};
+        if (n > 0) u_at(s, s.m_out, r, c, n, false, u);
+        float lo[4], hi[4];
+#pragma unroll
+        for (int k = 0; k < 4; ++k) {
+            tile[i][j + k] = lo[k] = k < n ? (float)(u[k] * inverse) : 0.0f;
+            tile[i][j + k + 4] = hi[k] = k + 4 < n ? (float)(u[k + 4] * inverse) : 0.0f;
+        }
+        *reinterpret_cast<float4 *>(to.x + at) = make_float4(lo[0], lo[1], lo[2], lo[3]);
+        *reinterpret_cast<float4 *>(to.x + at + 4) = make_float4(hi[0], hi[1], hi[2], hi[3]);
+        put_half(to.h + at, to.h + to.low + at, to.low != 0, lo);
+        put_half(to.h + at + 4, to.h + to.low + at + 4, to.low != 0, hi);
+    }
+    __syncthreads();
+#pragma unroll
+    for (int p = 0; p < 2; ++p) {
+        const int j = (threadIdx.x >> 3) + 32 * p, i = (threadIdx.x & 7) * 8;
+        float v[8];
+#pragma unroll
+        for (int k = 0; k < 8; ++k) v[k] = tile[i + k][j];
+        put_half_turned(to, c0 + j, r0 + i, v);
     }
 }
 
@@ -259,8 +314,9 @@ template <bool BY_ROW> struct step_t { // the next iterate; x in place
         *reinterpret_cast<float4 *>(s.in(to.x, to.ld)) = make_float4(n[0], n[1], n[2], n[3]);
         uint16_t *const h = s.in(to.h, to.ld);
         put_half(h, h + to.low, to.low != 0, n);
-        return v;
+        return make_float4(n[0], n[1], n[2], n[3]);
     }
+    __device__ __forceinline__ void put_turned(int64_t c, int64_t r, const float (&v)[8]) const { put_half_turned(to, c, r, v); }
 };
 
 template <bool BY_ROW> struct result_t { // the last one, as the result
@@ -325,11 +381,13 @@ template <bool BY_ROW> struct update_t { // the last one, as a step of the weigh
 
 // ---- host ----------------------------------------------------------------------------------------------------------------------------
 struct ns_plan_t {
-    bool wide, split;
+    bool wide, split, gram_direct, poly_direct, step_direct; // direct: by k_direct16
+    bool keeps_turned;                                       // the iterate's transpose is kept for them
     int64_t rows, cols, side, length; // padded: the matrix's, the smaller one and the larger
-    int64_t ld, ld_side;              // of the iterate's rows, of the square matrices'
+    int64_t ld, ld_side, ld_turned;   // of the iterate's rows, of the square matrices', of the iterate's transpose's
     plan16_t gram, poly, step;
-    size_t sums, D, diagonal, O, P, x, h[2], part, total;
+    int64_t half; // elements from an iterate's high half to its low one
+    size_t sums, D, diagonal, O, P, x, h[2], turned[2], part, total;
 };
 
 // Rows of a multiple of 8 KB of 16-bit elements are held a line further apart: a slab's pieces of all rows would lie in few of the caches' channels.
@@ -342,10 +400,25 @@ ns_plan_t ns_plan(int64_t rows, int64_t cols)
     p.rows = align_up(rows, SLAB), p.cols = align_up(cols, SLAB);
     p.side = p.wide ? p.rows : p.cols, p.length = p.wide ? p.cols : p.rows;
     p.split = (p.wide ? rows : cols) <= SPLIT_SIDE;
-    p.ld = row_pitch(p.cols), p.ld_side = row_pitch(p.side);
-    p.gram = plan16(p.side, p.side, p.length * (p.split ? 3 : 1), true);
+    p.ld = row_pitch(p.cols), p.ld_side = row_pitch(p.side), p.ld_turned = row_pitch(p.rows);
+    const int64_t long_k = p.length * (p.split ? 3 : 1), side_k = p.side * (p.split ? 2 : 1);
+    p.gram = plan16(p.side, p.side, long_k, true);
     p.poly = plan16(p.side, p.side, p.side, true);
-    p.step = plan16(p.rows, p.cols, p.side * (p.split ? 2 : 1), false);
+    p.step = plan16(p.rows, p.cols, side_k, false);
+    const plan16_t gram = plan_direct16(p.side, p.side, long_k, true), poly = plan_direct16(p.side, p.side, p.side, true), step = plan_direct16(p.rows, p.cols, side_k, false);
+    // k_direct16 wants both operands by rows: the iterate's transpose for the step of a wide matrix, for A of a tall one.  It is the step that writes it, if it runs there.
+    p.poly_direct = poly.time < p.poly.time;
+    if (p.wide) {
+        p.gram_direct = gram.time < p.gram.time;
+        p.step_direct = step.time < p.step.time;
+    } else {
+        p.gram_direct = gram.time + step.time < p.gram.time + (step.time < p.step.time ? step.time : p.step.time);
+        p.step_direct = p.gram_direct || step.time < p.step.time;
+    }
+    p.keeps_turned = p.wide ? p.step_direct : p.gram_direct;
+    if (p.gram_direct) p.gram = gram;
+    if (p.poly_direct) p.poly = poly;
+    if (p.step_direct) p.step = step;
     size_t part = p.gram.part_bytes;
     for (const plan16_t *q : {&p.poly, &p.step})
         if (q->part_bytes > part) part = q->part_bytes;
@@ -355,7 +428,8 @@ ns_plan_t ns_plan(int64_t rows, int64_t cols)
         at = align_up(at + bytes, 256);
         return here;
     };
-    const size_t all = (size_t)p.rows * p.ld, square = (size_t)p.side * p.ld_side;
+    const size_t by_rows = (size_t)p.rows * p.ld, by_cols = (size_t)p.cols * p.ld_turned, all = by_rows > by_cols ? by_rows : by_cols, square = (size_t)p.side * p.ld_side;
+    p.half = (int64_t)all;
     p.sums = take(PARTS * sizeof(double));
     p.D = take(p.side * sizeof(float));
     p.diagonal = take(p.side * sizeof(float));
@@ -363,6 +437,7 @@ ns_plan_t ns_plan(int64_t rows, int64_t cols)
     p.P = take(square * 2);
     p.x = take(all * sizeof(float));
     for (size_t &h : p.h) h = take(all * 2 * (p.split ? 2 : 1));
+    for (size_t &h : p.turned) h = take(p.keeps_turned ? all * 2 * (p.split ? 2 : 1) : 0);
     p.part = take(part);
     p.total = at;
     return p;
@@ -380,6 +455,15 @@ template <bool SEG> int configure_some()
     if (rc == ADAHOP_OK) rc = configure_all16<true, ALONG, ALONG, SEG, false, result_t<false>>();
     if (rc == ADAHOP_OK) rc = configure_all16<true, ALONG, DOWN, SEG, false, update_t<true>>();
     if (rc == ADAHOP_OK) rc = configure_all16<true, ALONG, ALONG, SEG, false, update_t<false>>();
+    if (rc == ADAHOP_OK) rc = configure_direct16<true, SEG, true, true, gram_t>();
+    if (rc == ADAHOP_OK) rc = configure_direct16<true, SEG, false, true, step_t<true>>();
+    if (rc == ADAHOP_OK) rc = configure_direct16<true, SEG, false, false, step_t<true>>();
+    if (rc == ADAHOP_OK) rc = configure_direct16<true, SEG, false, true, step_t<false>>();
+    if (rc == ADAHOP_OK) rc = configure_direct16<true, SEG, false, false, step_t<false>>();
+    if (rc == ADAHOP_OK) rc = configure_direct16<true, SEG, false, false, result_t<true>>();
+    if (rc == ADAHOP_OK) rc = configure_direct16<true, SEG, false, false, result_t<false>>();
+    if (rc == ADAHOP_OK) rc = configure_direct16<true, SEG, false, false, update_t<true>>();
+    if (rc == ADAHOP_OK) rc = configure_direct16<true, SEG, false, false, update_t<false>>();
     return rc;
 }
 
@@ -390,7 +474,8 @@ struct ns_call_t {
     hipStream_t st;
     iterate_t at(int which) const
     {
-        return {reinterpret_cast<float *>(ws + p.x), reinterpret_cast<uint16_t *>(ws + p.h[which]), p.ld, p.split ? p.rows * p.ld : 0};
+        return {reinterpret_cast<float *>(ws + p.x), reinterpret_cast<uint16_t *>(ws + p.h[which]), p.ld, p.split ? p.half : 0,
+                p.keeps_turned ? reinterpret_cast<uint16_t *>(ws + p.turned[which]) : nullptr, p.ld_turned};
     }
     float *D() const { return reinterpret_cast<float *>(ws + p.D); }
     float *diagonal() const { return reinterpret_cast<float *>(ws + p.diagonal); }
@@ -405,6 +490,10 @@ struct ns_call_t {
         q.K = p.length;
         q.seg = {3, {0, 0, x.low}, {0, x.low, 0}}; // high high + high low + low high
         const gram_t e = {O(), D(), p.ld_side};
+        if (p.gram_direct) {
+            if (!p.wide) q.A = q.B = {x.turned, x.ld_turned, p.side};
+            return launch_direct16<true, SEG, true, true>(p.gram, q, e, ws + p.part, st);
+        }
         return p.wide ? launch_product16<true, ALONG, ALONG, SEG, true>(p.gram, q, e, ws + p.part, st) : launch_product16<true, DOWN, DOWN, SEG, true>(p.gram, q, e, ws + p.part, st);
     }
     int poly(const float (&k)[3]) const
@@ -413,14 +502,23 @@ struct ns_call_t {
         q.A = q.B = {O(), p.ld_side, p.side};
         q.K = p.side;
         const poly_t e = {O(), D(), P(), diagonal(), p.ld_side, k[0], k[1], k[2]};
-        return launch_product16<true, ALONG, ALONG, false, true>(p.poly, q, e, ws + p.part, st);
+        return p.poly_direct ? launch_direct16<true, false, true, true>(p.poly, q, e, ws + p.part, st) : launch_product16<true, ALONG, ALONG, false, true>(p.poly, q, e, ws + p.part, st);
     }
     // P X (wide), X P: with P symmetric, its rows serve as its columns
-    template <bool SEG, bool WIDE, class E> int step(int which, const E &e) const
+    template <bool SEG, bool WIDE, bool TURNED, class E> int step(int which, const E &e) const
     {
         const iterate_t x = at(which);
         product_t q = {};
         q.K = p.side;
+        if (p.step_direct) {
+            const side_t square = {P(), p.ld_side, p.side};
+            if (WIDE)
+                q.A = square, q.B = {x.turned, x.ld_turned, p.cols}, q.seg = {2, {0, 0, 0}, {0, x.low, 0}};
+            else
+                q.A = {x.h, x.ld, p.rows}, q.B = square, q.seg = {2, {0, x.low, 0}, {0, 0, 0}};
+            if (p.keeps_turned) return launch_direct16<true, SEG, false, TURNED>(p.step, q, e, ws + p.part, st);
+            return launch_direct16<true, SEG, false, false>(p.step, q, e, ws + p.part, st);
+        }
         if constexpr (WIDE) {
             q.A = {P(), p.ld_side, p.rows}, q.B = {x.h, x.ld, p.cols};
             q.seg = {2, {0, 0, 0}, {0, x.low, 0}};
@@ -442,11 +540,11 @@ template <bool SEG, bool WIDE> int iterate(const ns_call_t &c, const adahop_newt
         if (rc != ADAHOP_OK) return rc;
         const carried_t<WIDE> from = {c.at(0).x, c.diagonal(), c.p.ld};
         if (i + 1 < m.steps)
-            rc = c.step<SEG, WIDE>(i & 1, step_t<WIDE>{from, c.at((i & 1) ^ 1)});
+            rc = c.step<SEG, WIDE, true>(i & 1, step_t<WIDE>{from, c.at((i & 1) ^ 1)});
         else if (u)
-            rc = c.step<SEG, WIDE>(i & 1, update_t<WIDE>{from, u->w, u->w_out, u->w_bf16, u->rows, u->cols, 1.0f - u->rate * u->weight_decay, u->rate * m.scale});
+            rc = c.step<SEG, WIDE, false>(i & 1, update_t<WIDE>{from, u->w, u->w_out, u->w_bf16, u->rows, u->cols, 1.0f - u->rate * u->weight_decay, u->rate * m.scale});
         else
-            rc = c.step<SEG, WIDE>(i & 1, result_t<WIDE>{from, out, m.rows, m.cols, m.scale});
+            rc = c.step<SEG, WIDE, false>(i & 1, result_t<WIDE>{from, out, m.rows, m.cols, m.scale});
         if (rc != ADAHOP_OK) return rc;
     }
     return ADAHOP_OK;
@@ -462,6 +560,7 @@ int configure_newton_schulz()
     rc = configure_some<false>();
     if (rc == ADAHOP_OK) rc = configure_some<true>();
     if (rc == ADAHOP_OK) rc = configure_all16<true, ALONG, ALONG, false, true, poly_t>();
+    if (rc == ADAHOP_OK) rc = configure_direct16<true, false, true, true, poly_t>();
     if (rc == ADAHOP_OK) g_once.mark(dev);
     return rc;
 }
@@ -481,7 +580,10 @@ int launch_newton_schulz(const adahop_newton_schulz_t &m, const adahop_tensor_t 
     k_squares<<<parts, 256, 0, st>>>(s, sums);
     if ((rc = check_launch()) != ADAHOP_OK) return rc;
     const int64_t blocks = ceil_div(c.p.rows * (c.p.cols / 8), 256);
-    k_first<<<(unsigned)(blocks < 4096 ? blocks : 4096), 256, 0, st>>>(s, sums, parts, m.eps, c.at(0), c.p.rows, c.p.cols);
+    if (c.p.keeps_turned)
+        k_first_turned<<<dim3((unsigned)(c.p.rows / 64), (unsigned)(c.p.cols / 64)), 256, 0, st>>>(s, sums, parts, m.eps, c.at(0));
+    else
+        k_first<<<(unsigned)(blocks < 4096 ? blocks : 4096), 256, 0, st>>>(s, sums, parts, m.eps, c.at(0), c.p.rows, c.p.cols);
     if ((rc = check_launch()) != ADAHOP_OK) return rc;
     if (c.p.split) return c.p.wide ? iterate<true, true>(c, m, out, u) : iterate<true, false>(c, m, out, u);
     return c.p.wide ? iterate<false, true>(c, m, out, u) : iterate<false, false>(c, m, out, u);

@@ -476,10 +476,11 @@ template <class K, bool F16, lies_t LA, lies_t LB, bool SEG, bool SYMMETRIC, cla
 }
 
 // The sums of the slices of the tiles that have some, in their order, finished: a wave has 32 rows of 32 columns of a tile.
-template <class K, bool SYMMETRIC, class E> __global__ __launch_bounds__(64) void k_join16(product_t q, E e)
+// TURNED: the values go to put_turned, too, where the tile is not on a SYMMETRIC product's diagonal.
+template <class K, bool SYMMETRIC, bool TURNED, class E> __global__ __launch_bounds__(64) void k_join16(product_t q, E e)
 {
     constexpr int PITCH = 36, ACROSS = K::TN / 32, PATCHES = K::TM / 32 * ACROSS, STEPS = 4;
-    __shared__ float patch[SYMMETRIC ? 32 * PITCH : 1];
+    __shared__ float patch[TURNED ? 32 * PITCH : 1];
     const uint32_t tail = blockIdx.x / PATCHES, in = blockIdx.x % PATCHES;
     const int lane = threadIdx.x, c4 = (lane & 7) * 4, r0 = lane >> 3;
     int64_t n0, d0;
@@ -511,10 +512,10 @@ template <class K, bool SYMMETRIC, class E> __global__ __launch_bounds__(64) voi
     for (int i = 0; i < STEPS; ++i)
         if (have > 0 && r + 8 * i < q.A.outer) {
             const float4 done = e.apply(spot(i), have, sum[i], column, more[i]);
-            if constexpr (SYMMETRIC) *reinterpret_cast<float4 *>(patch + (r0 + 8 * i) * PITCH + c4) = done;
+            if constexpr (TURNED) *reinterpret_cast<float4 *>(patch + (r0 + 8 * i) * PITCH + c4) = done;
         }
-    if constexpr (SYMMETRIC) {
-        if (n0 == d0) return;
+    if constexpr (TURNED) {
+        if (SYMMETRIC && n0 == d0) return;
         lds_between_lanes();
         put_mirror<2>(q, first, c0, patch, e);
     }
@@ -540,6 +541,138 @@ struct grad_t {
     }
 };
 
+// ---- small products -----------------------------------------------------------------------------------------------------------------
+// Both operands ALONG, all extents multiples of 64: tiles of 64 x 64, whose four waves share the contraction.  A wave copies what it needs itself, two slabs ahead, to LDS of
+// its own: nothing waits for a barrier before the waves' sums meet.  What the finish reads is read before the first slab.  Where tiles are few, latency is all that
+// counts.  136 tiles of a symmetric product with a contraction of 1024: 18.5 us with tiles of 128, and 11.6 us with operands loaded straight to registers (a quarter of a wave reads 16 rows
+// then, each lane's 16 bytes an access of their own).
+struct direct_t {
+    static constexpr int TM = 64, TN = 64, WAVES = 4, THREADS = 256, PITCH = 68;
+    static constexpr uint32_t SIDE = 64 * 2 * SLAB, STEP = 2 * SIDE, OWN = 2 * STEP, LDS = WAVES * OWN;
+    static_assert(WAVES * 64 * PITCH * sizeof(float) <= LDS, "the waves' sums fit");
+};
+
+// TURNED: the finish's values go to put_turned, too, where the tile is not on a SYMMETRIC product's diagonal.
+template <bool F16, bool SEG, bool SYMMETRIC, bool TURNED, class E> __global__ __launch_bounds__(direct_t::THREADS) void k_direct16(product_t q, E e)
+{
+    typedef direct_t K;
+    extern __shared__ __attribute__((aligned(1024))) uint8_t smem[];
+    float *const sums = reinterpret_cast<float *>(smem); // [wave][64][PITCH]
+    int64_t n0, d0;
+    const uint32_t past = blockIdx.x - q.whole;
+    const bool sliced = blockIdx.x >= q.whole && q.slices > 1;
+    place_of<K, SYMMETRIC>(q.nt, q.dt, blockIdx.x < q.whole ? run_of_xcd(blockIdx.x, q.whole) : q.whole + past / q.slices, n0, d0);
+    const int lane = threadIdx.x & 63, w = __builtin_amdgcn_readfirstlane(threadIdx.x >> 6), s16 = lane & 15, g = lane >> 4;
+    // the contraction's slabs: this slice's, and this wave's of them
+    const int all = (int)((SEG ? q.K * q.seg.count : q.K) / SLAB), of_slice = sliced ? (int)(q.slice / SLAB) : all;
+    const int from = sliced ? (int)(past % q.slices) * of_slice : 0, till = from + of_slice < all ? from + of_slice : all;
+    const int first = __builtin_amdgcn_readfirstlane(from + (till - from) * w / K::WAVES), steps = __builtin_amdgcn_readfirstlane(from + (till - from) * (w + 1) / K::WAVES) - first;
+    const auto spot = [&](int p) { return spot_t{n0 + 16 * p + 4 * w, d0, (uint32_t)g, (uint32_t)s16 * 4}; };
+    typename E::column_t column;
+    typename E::more_t more[4];
+    if (!sliced) {
+        column = e.column(spot(0).col(), 4);
+#pragma unroll
+        for (int p = 0; p < 4; ++p) more[p] = e.get(spot(p), 4);
+    }
+    // eight lanes have a row of a copy of eight; the row's bits 1 and 2 are the lane's 4 and 5, bit 3 is the copy's parity
+    const uint32_t mine = lds_address(smem) + w * K::OWN;
+    uint32_t off_a[2], off_b[2];
+#pragma unroll
+    for (int i = 0; i < 2; ++i) {
+        const uint32_t piece = (lane & 7) ^ exchange_of(4 * i + (lane >> 4));
+        off_a[i] = ((uint32_t)(lane >> 3) * (uint32_t)q.A.ld + 8 * piece) * 2, off_b[i] = ((uint32_t)(lane >> 3) * (uint32_t)q.B.ld + 8 * piece) * 2;
+    }
+    const uint16_t *const pa = q.A.data + n0 * q.A.ld, *const pb = q.B.data + d0 * q.B.ld;
+    const int run = (int)(q.K / SLAB);
+    const auto copy = [&](int step, int half) {
+        int64_t a = 0, b = 0;
+        step += first;
+        if constexpr (SEG) {
+            const int segment = step >= run ? step >= 2 * run ? 2 : 1 : 0;
+            a = segment == 2 ? q.seg.a[2] : segment ? q.seg.a[1] : q.seg.a[0];
+            b = segment == 2 ? q.seg.b[2] : segment ? q.seg.b[1] : q.seg.b[0];
+            step -= segment * run;
+        }
+        const uint8_t *const ca = reinterpret_cast<const uint8_t *>(pa + a + step * SLAB), *const cb = reinterpret_cast<const uint8_t *>(pb + b + step * SLAB);
+#pragma unroll
+        for (int i = 0; i < 8; ++i) {
+            dma16(ca + i * 16 * q.A.ld, off_a[i & 1], mine + half * K::STEP + i * 1024);
+            dma16(cb + i * 16 * q.B.ld, off_b[i & 1], mine + half * K::STEP + K::SIDE + i * 1024);
+        }
+    };
+    v4f acc[4][4];
+#pragma unroll
+    for (int m = 0; m < 4; ++m)
+#pragma unroll
+        for (int n = 0; n < 4; ++n) acc[m][n] = {};
+    const uint32_t along = mine + s16 * 128 + (g ^ exchange_of(s16 >> 1)) * 16;
+    if (steps > 0) copy(0, 0);
+    if (steps > 1) copy(1, 1);
+    for (int i = 0; i < steps; ++i) {
+        if (i + 1 < steps)
+            wait_for_copies<16>();
+        else
+            wait_for_copies<0>();
+        u32x4 fa[2][4], fb[2][4];
+        const uint32_t at = along + (i & 1) * K::STEP;
+#pragma unroll
+        for (int h = 0; h < 2; ++h)
+#pragma unroll
+            for (int m = 0; m < 4; ++m) fa[h][m] = lds_read16((at ^ 64 * h) + m * 2048), fb[h][m] = lds_read16((at ^ 64 * h) + K::SIDE + m * 2048);
+        asm volatile("s_waitcnt lgkmcnt(0)" ::: "memory"); // read: what follows may go in its place
+        if (i + 2 < steps) copy(i + 2, i & 1);
+#pragma unroll
+        for (int h = 0; h < 2; ++h)
+#pragma unroll
+            for (int m = 0; m < 4; ++m)
+#pragma unroll
+                for (int n = 0; n < 4; ++n) acc[m][n] = mfma16<F16>(__builtin_bit_cast(uint4, fa[h][m]), __builtin_bit_cast(uint4, fb[h][n]), acc[m][n]);
+    }
+    __syncthreads();
+    float *const own = sums + w * 64 * K::PITCH;
+#pragma unroll
+    for (int m = 0; m < 4; ++m)
+#pragma unroll
+        for (int n = 0; n < 4; ++n)
+#pragma unroll
+            for (int i = 0; i < 4; ++i) own[(16 * m + 4 * g + i) * K::PITCH + 16 * n + s16] = acc[m][n][i];
+    __syncthreads();
+    float4 v[4];
+#pragma unroll
+    for (int p = 0; p < 4; ++p) {
+        v[p] = make_float4(0.0f, 0.0f, 0.0f, 0.0f);
+#pragma unroll
+        for (int k = 0; k < K::WAVES; ++k) {
+            const float4 o = *reinterpret_cast<const float4 *>(sums + (k * 64 + 16 * p + 4 * w + g) * K::PITCH + s16 * 4);
+            v[p] = make_float4(v[p].x + o.x, v[p].y + o.y, v[p].z + o.z, v[p].w + o.w);
+        }
+    }
+    if (sliced) {
+        const store_part_t part = {q.part + (int64_t)past * K::TM * K::TN, n0, d0, K::TN};
+#pragma unroll
+        for (int p = 0; p < 4; ++p) part.apply(spot(p), 4, v[p], {}, {});
+        return;
+    }
+#pragma unroll
+    for (int p = 0; p < 4; ++p) v[p] = e.apply(spot(p), 4, v[p], column, more[p]);
+    if constexpr (TURNED) {
+        if (SYMMETRIC && n0 == d0) return;
+        __syncthreads();
+#pragma unroll
+        for (int p = 0; p < 4; ++p) *reinterpret_cast<float4 *>(sums + (16 * p + 4 * w + g) * K::PITCH + s16 * 4) = v[p];
+        __syncthreads();
+#pragma unroll
+        for (int p = 0; p < 2; ++p) {
+            const int col = (threadIdx.x >> 3) + 32 * p, down = 8 * (threadIdx.x & 7);
+            float t[8];
+#pragma unroll
+            for (int j = 0; j < 8; ++j) t[j] = sums[(down + j) * K::PITCH + col];
+            e.put_turned(d0 + col, n0 + down, t);
+        }
+    }
+}
+
 // ---- host ----------------------------------------------------------------------------------------------------------------------
 // Tiles and slices of a product by its expected time.
 struct plan16_t {
@@ -547,6 +680,7 @@ struct plan16_t {
     uint32_t tiles, whole, slices; // of the tiles behind the whole ones
     int64_t slice;
     size_t part_bytes;
+    double time; // microseconds, as expected
 };
 
 // In microseconds, on 256 compute units: half a slab of a round of workgroups takes 0.74 with tiles of 256, 0.43 of 192, one workgroup per compute unit; of 128 0.6 where there are two
@@ -555,14 +689,13 @@ struct plan16_t {
 inline plan16_t plan16(int64_t rows, int64_t cols, int64_t K, bool symmetric, int64_t slices_at_most = 64)
 {
     plan16_t best = {};
-    double best_time = 0.0;
     const int64_t stages = ceil_div(K, SLAB) * 2; // of 32 elements of the contraction
     for (const int edge : {256, 192, 128}) {
         const int64_t room = edge > 128 ? 256 : 512, down = ceil_div(rows, edge), across = ceil_div(cols, edge);
         const int64_t tiles = symmetric ? down * (down + 1) / 2 : down * across, rest = tiles % room;
         const double each = edge == 256 ? 0.74 : edge == 192 ? 0.43 : 0.6, ends = edge == 256 ? 12.0 : edge == 192 ? 10.0 : 6.0, whole = (double)(tiles / room) * (ends + each * (double)stages);
         const auto a_round = [&](int64_t workgroups, int64_t of) { return ends + (workgroups <= 256 && edge == 128 ? 0.3 : each) * (double)of; };
-        plan16_t p = {edge, (uint32_t)tiles, (uint32_t)tiles, 1, 0, 0};
+        plan16_t p = {edge, (uint32_t)tiles, (uint32_t)tiles, 1, 0, 0, 0.0};
         double time = whole + (rest ? a_round(rest, stages) : 0.0);
         for (int64_t s = 2; rest && s <= slices_at_most && stages / s >= 4; ++s) {
             const int64_t of = ceil_div(ceil_div(stages, s), 2) * 2, number = ceil_div(stages, of);
@@ -574,7 +707,22 @@ inline plan16_t plan16(int64_t rows, int64_t cols, int64_t K, bool symmetric, in
                 p.part_bytes = (size_t)rest * number * edge * edge * sizeof(float);
             }
         }
-        if (edge == 256 || time < best_time) best = p, best_time = time;
+        if (edge == 256 || time < best.time) best = p, best.time = time;
+    }
+    return best;
+}
+
+// The same for k_direct16: a round of 256 tiles takes DIRECT_ENDS, and DIRECT_STEP for each 32 of the contraction; slices as above.
+constexpr double DIRECT_ENDS = 4.0, DIRECT_STEP = 0.14;
+
+inline plan16_t plan_direct16(int64_t rows, int64_t cols, int64_t K, bool symmetric)
+{
+    const int64_t down = ceil_div(rows, 64), tiles = symmetric ? down * (down + 1) / 2 : down * ceil_div(cols, 64), steps = ceil_div(K, SLAB) * 2;
+    plan16_t best = {64, (uint32_t)tiles, (uint32_t)tiles, 1, 0, 0, (double)ceil_div(tiles, 256) * (DIRECT_ENDS + DIRECT_STEP * (double)steps)};
+    for (int64_t s = 2; s <= 32 && steps / s >= 16 && tiles * s <= 512; ++s) {
+        const int64_t of = ceil_div(ceil_div(steps, s), 2) * 2, number = ceil_div(steps, of);
+        const double time = (double)ceil_div(tiles * number, 256) * (DIRECT_ENDS + DIRECT_STEP * (double)of) + 5.0;
+        if (time < best.time) best = {64, (uint32_t)tiles, 0, (uint32_t)number, of * 32, (size_t)tiles * number * 64 * 64 * sizeof(float), time};
     }
     return best;
 }
@@ -591,7 +739,7 @@ template <class K, bool F16, lies_t LA, lies_t LB, bool SEG, bool SYMMETRIC, cla
     k_product16<K, F16, LA, LB, SEG, SYMMETRIC, E><<<plan.whole + rest * plan.slices, K::THREADS, K::LDS, st>>>(q, e);
     const int rc = check_launch();
     if (rc != ADAHOP_OK || !rest) return rc;
-    k_join16<K, SYMMETRIC, E><<<rest * (K::TM / 32) * (K::TN / 32), 64, 0, st>>>(q, e);
+    k_join16<K, SYMMETRIC, SYMMETRIC, E><<<rest * (K::TM / 32) * (K::TN / 32), 64, 0, st>>>(q, e);
     return check_launch();
 }
 
@@ -603,6 +751,25 @@ inline int launch_product16(const plan16_t &plan, product_t q, const E &e, void 
     q.part = static_cast<float *>(part);
     return plan.edge == 256 ? launch_tiles16<tile256_t, F16, LA, LB, SEG, SYMMETRIC>(q, plan, e, st)
            : plan.edge == 192 ? launch_tiles16<tile192_t, F16, LA, LB, SEG, SYMMETRIC>(q, plan, e, st) : launch_tiles16<tile128_t, F16, LA, LB, SEG, SYMMETRIC>(q, plan, e, st);
+}
+
+template <bool F16, bool SEG, bool SYMMETRIC, bool TURNED, class E> inline int configure_direct16()
+{
+    return check_hip(hipFuncSetAttribute(reinterpret_cast<const void *>(&k_direct16<F16, SEG, SYMMETRIC, TURNED, E>), hipFuncAttributeMaxDynamicSharedMemorySize, direct_t::LDS));
+}
+
+template <bool F16, bool SEG, bool SYMMETRIC, bool TURNED, class E> inline int launch_direct16(const plan16_t &plan, product_t q, const E &e, void *part, hipStream_t st)
+{
+    typedef direct_t K;
+    const uint32_t rest = plan.tiles - plan.whole;
+    q.whole = plan.whole, q.slices = plan.slices, q.slice = plan.slice;
+    q.part = static_cast<float *>(part);
+    q.nt = (uint32_t)(q.A.outer / 64), q.dt = (uint32_t)(q.B.outer / 64);
+    k_direct16<F16, SEG, SYMMETRIC, TURNED, E><<<plan.whole + rest * plan.slices, K::THREADS, K::LDS, st>>>(q, e);
+    const int rc = check_launch();
+    if (rc != ADAHOP_OK || !rest) return rc;
+    k_join16<K, SYMMETRIC, TURNED, E><<<rest * 4, 64, 0, st>>>(q, e);
+    return check_launch();
 }
 
 template <bool F16, lies_t LA, lies_t LB, bool SEG, bool SYMMETRIC, class E> inline int configure_all16()

@@ -62,7 +62,7 @@ def distance(got, want):
 
 def bound(u, want, **how):
     """Of the distance of an fp32 result."""
-    own = distance(orc.newton_schulz_held(u, split=min(u.shape) <= 256, **how), want)
+    own = distance(orc.newton_schulz_held(u, split=min(u.shape) <= 128, **how), want)
     return 2.0 * own + 64 * U32 * own * 2.0 ** 12 + 64 * U32
 
 
