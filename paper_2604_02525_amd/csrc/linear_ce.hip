@@ -31,9 +31,17 @@ struct loss_t {
 // ---- forward --------------------------------------------------------------------------------------------------------------------
 struct stats_t {
     loss_t p;
-    float2 *part; // [T][tiles of the vocabulary]: largest logit, sum of exponentials relative to it
-    float *at;    // [T]: the target's logit
+    int64_t v0, tile, tiles; // the launch's first word, and its first of the parts of the vocabulary that a token has numbers of
+    float2 *part;            // [T][tiles]: largest logit, sum of exponentials relative to it
+    float *at;               // [T]: the target's logit
 };
+
+// A largest logit and the sum of exponentials relative to it, of two sets of words.
+__device__ __forceinline__ float2 joined(float2 a, float2 b)
+{
+    const float top = fmaxf(a.x, b.x), from = top == -INFINITY ? 0.0f : top;
+    return make_float2(top, a.y * __expf(a.x - from) + b.y * __expf(b.x - from));
+}
 
 template <int MASK> __device__ __forceinline__ float across(float v) { return __shfl_xor(v, MASK); }
 
@@ -50,12 +58,12 @@ template <class K> __global__ __launch_bounds__(K::THREADS, 2) void k_ce_stats(p
     __syncthreads();
     float2 *const of_wave = reinterpret_cast<float2 *>(smem); // [WN][TN]
     const int lane = threadIdx.x & 63, w = threadIdx.x >> 6, wn = w / K::WD, wd = w % K::WD;
-    const int first = (int)(e.p.V - n0 < K::TM ? e.p.V - n0 : K::TM) - wn * K::MT * 16 - 4 * (lane >> 4); // words of this lane's from its first on, below its rows' count
+    const int first = (int)(q.A.outer - n0 < K::TM ? q.A.outer - n0 : K::TM) - wn * K::MT * 16 - 4 * (lane >> 4); // words of this lane's from its first on, below its rows' count
 #pragma unroll
     for (int n = 0; n < K::NT; ++n) {
         const int64_t t = d0 + (wd * K::NT + n) * 16 + (lane & 15);
-        const int64_t y = t < q.B.outer ? e.p.targets[t] - n0 - wn * K::MT * 16 - 4 * (lane >> 4) : -1;
-        const int mine = y >= 0 && y < K::MT * 16 ? (int)y : -1; // the target as a row of this lane's, if it is one
+        const int64_t y = t < q.B.outer ? e.p.targets[t] - e.v0 - n0 - wn * K::MT * 16 - 4 * (lane >> 4) : -1;
+        const int mine = y >= 0 && y < K::MT * 16 && y < first ? (int)y : -1; // the target as a row of this lane's, if it is one
         float top = -INFINITY, sum = 0.0f, at = 0.0f;
         bool is = false;
 #pragma unroll
@@ -85,13 +93,90 @@ template <class K> __global__ __launch_bounds__(K::THREADS, 2) void k_ce_stats(p
         if (d0 + i >= q.B.outer) break;
         float2 s = of_wave[i];
 #pragma unroll
-        for (int k = 1; k < K::WN; ++k) {
-            const float2 o = of_wave[k * K::TN + i];
-            const float top = fmaxf(s.x, o.x), from = top == -INFINITY ? 0.0f : top;
-            s = make_float2(top, s.y * __expf(s.x - from) + o.y * __expf(o.x - from));
-        }
-        e.part[(d0 + i) * q.nt + n0 / K::TM] = s;
+        for (int k = 1; k < K::WN; ++k) s = joined(s, of_wave[k * K::TN + i]);
+        e.part[(d0 + i) * e.tiles + e.tile + n0 / K::TM] = s;
     }
+}
+
+// Up to FEW tokens (the likelihood of what has just been generated): bound by reading w once, a tile of tokens would be almost empty.  A wave forms the logits of four words
+// at a time, 512 elements of their rows a step, h from LDS; it keeps a token's largest logit and sum of exponentials over its words.
+constexpr int FEW = 8;
+
+template <int T> __global__ __launch_bounds__(256, 2) void k_ce_few(side_t w, side_t h, int64_t K, stats_t e)
+{
+    extern __shared__ __attribute__((aligned(1024))) uint8_t smem[];
+    uint16_t *const own = reinterpret_cast<uint16_t *>(smem); // [T][pitch]
+    const int lane = threadIdx.x & 63;
+    const int64_t pitch = (K + 511) / 512 * 512;
+    for (int64_t i = threadIdx.x * 8; i < T * pitch; i += 256 * 8) {
+        const int64_t t = i / pitch, k = i - t * pitch;
+        *reinterpret_cast<u32x4 *>(own + i) = t < h.outer && k < K ? *reinterpret_cast<const u32x4 *>(h.data + t * h.ld + k) : u32x4{0, 0, 0, 0};
+    }
+    __syncthreads();
+    const int64_t waves = (int64_t)gridDim.x * 4, wave = __builtin_amdgcn_readfirstlane(blockIdx.x * 4 + (threadIdx.x >> 6));
+    float top[T], sum[T];
+#pragma unroll
+    for (int t = 0; t < T; ++t) top[t] = -INFINITY, sum[t] = 0.0f;
+    for (int64_t v0 = wave * 4; v0 < w.outer; v0 += waves * 4) {
+        const uint16_t *row[4]; // (those behind the vocabulary: its last word's)
+#pragma unroll
+        for (int r = 0; r < 4; ++r) row[r] = w.data + (v0 + r < w.outer ? v0 + r : w.outer - 1) * w.ld;
+        float acc[4][T] = {};
+        u32x4 next[4];
+        const auto load = [&](int64_t k) {
+#pragma unroll
+            for (int r = 0; r < 4; ++r) next[r] = k + lane * 8 < K ? __builtin_nontemporal_load(reinterpret_cast<const u32x4 *>(row[r] + k + lane * 8)) : u32x4{0, 0, 0, 0};
+        };
+        load(0);
+        for (int64_t k = 0; k < pitch; k += 512) {
+            float x[4][8];
+#pragma unroll
+            for (int r = 0; r < 4; ++r)
+#pragma unroll
+                for (int i = 0; i < 8; ++i) x[r][i] = i & 1 ? bf16_hi(next[r][i >> 1]) : bf16_lo(next[r][i >> 1]);
+            if (k + 512 < pitch) load(k + 512);
+#pragma unroll
+            for (int t = 0; t < T; ++t) {
+                const u32x4 y = *reinterpret_cast<const u32x4 *>(own + t * pitch + k + lane * 8);
+#pragma unroll
+                for (int i = 0; i < 8; ++i) {
+                    const float b = i & 1 ? bf16_hi(y[i >> 1]) : bf16_lo(y[i >> 1]);
+#pragma unroll
+                    for (int r = 0; r < 4; ++r) acc[r][t] = fmaf(x[r][i], b, acc[r][t]);
+                }
+            }
+        }
+#pragma unroll
+        for (int t = 0; t < T; ++t) {
+            if (t >= h.outer) break;
+            const int64_t y = e.p.targets[t] - v0;
+            float z[4], most = top[t];
+#pragma unroll
+            for (int r = 0; r < 4; ++r) {
+                z[r] = sum64(acc[r][t]) * e.p.logit_scale;
+                if (y == r && lane == 0 && v0 + r < w.outer) e.at[t] = z[r];
+                if (v0 + r >= w.outer) z[r] = -INFINITY;
+                most = fmaxf(most, z[r]);
+            }
+            const float from = most == -INFINITY ? 0.0f : most;
+            sum[t] *= __expf(top[t] - from);
+#pragma unroll
+            for (int r = 0; r < 4; ++r) sum[t] += __expf(z[r] - from);
+            top[t] = most;
+        }
+    }
+    __syncthreads();
+    float2 *const of_wave = reinterpret_cast<float2 *>(smem); // [4][T]
+    if (lane == 0)
+#pragma unroll
+        for (int t = 0; t < T; ++t) of_wave[(threadIdx.x >> 6) * T + t] = make_float2(top[t], sum[t]);
+    __syncthreads();
+    const int t = threadIdx.x;
+    if (t >= h.outer) return;
+    float2 s = of_wave[t];
+#pragma unroll
+    for (int k = 1; k < 4; ++k) s = joined(s, of_wave[k * T + t]);
+    e.part[t * gridDim.x + blockIdx.x] = s;
 }
 
 // One wave per token: its tiles' numbers joined, the loss.
@@ -100,13 +185,11 @@ __global__ __launch_bounds__(256) void k_ce_join(loss_t p, const float2 *part, c
     const int64_t t = (int64_t)blockIdx.x * 4 + (threadIdx.x >> 6);
     const int lane = threadIdx.x & 63;
     if (t >= p.T) return;
-    float top = -INFINITY, sum = 0.0f;
-    for (int i = lane; i < tiles; i += 64) {
-        const float2 s = part[t * tiles + i];
-        const float to = fmaxf(top, s.x), from = to == -INFINITY ? 0.0f : to;
-        sum = sum * __expf(top - from) + s.y * __expf(s.x - from);
-        top = to;
-    }
+    float2 all = make_float2(-INFINITY, 0.0f);
+#pragma unroll 4
+    for (int i = lane; i < tiles; i += 64) all = joined(all, part[t * tiles + i]);
+    const float top = all.x;
+    float sum = all.y;
     float most = top;
 #pragma unroll
     for (int k = 1; k < 64; k *= 2) most = fmaxf(most, __shfl_xor(most, k));
@@ -120,37 +203,33 @@ __global__ __launch_bounds__(256) void k_ce_join(loss_t p, const float2 *part, c
 }
 
 // ---- backward -------------------------------------------------------------------------------------------------------------------
+// What dz of a token that has a target needs of it.
+struct token_t {
+    float lse, gain; // gain: what exp(z - lse) - [v = target] is multiplied by
+    int32_t target, token;
+};
+
 // dz of a piece of the vocabulary from its logits (rows: tokens, columns: words from v0 on), rounded to bf16; zeros from the piece's end to the row's.
 struct dlogits_t {
     static constexpr bool COUNTED = true;
     static constexpr int AHEAD = 2;
-    loss_t p;
-    const int32_t *token; // of each row
-    const float *lse, *d_loss;
-    int64_t d_loss_stride, v0, words, ld;
-    float factor; // in dz: logit_scale, or 1 where it comes later
-    uint16_t *dz;
     typedef nothing_t column_t;
+    typedef token_t more_t;
+    const token_t *rows;
+    float logit_scale, z_loss;
+    int64_t v0, words, ld;
+    uint16_t *dz;
     __device__ __forceinline__ column_t column(int64_t, int) const { return {}; }
-    struct more_t {
-        float lse, gain; // gain: what exp(z - lse) - [v = y] is multiplied by
-        int64_t y;
-    };
-    __device__ __forceinline__ more_t get(const spot_t &at, int) const
-    {
-        const int64_t t = token[at.row()], y = p.targets[t];
-        const float g = (d_loss ? d_loss[t * d_loss_stride] : 1.0f) * factor;
-        return {lse[t], y < p.V ? g : NAN, y};
-    }
+    __device__ __forceinline__ more_t get(const spot_t &at, int) const { return rows[at.row()]; }
     __device__ __forceinline__ float4 apply(const spot_t &at, int have, float4 v, column_t, const more_t &m) const
     {
         const int64_t c = at.col();
-        const float z[4] = {v.x, v.y, v.z, v.w}, s = 1.0f + 2.0f * p.z_loss * m.lse;
-        const int64_t hit = m.y - v0 - c;
+        const float z[4] = {v.x, v.y, v.z, v.w}, s = 1.0f + 2.0f * z_loss * m.lse;
+        const int64_t hit = m.target - v0 - c;
         float d[4];
 #pragma unroll
         for (int i = 0; i < 4; ++i) {
-            d[i] = (s * __expf(z[i] * p.logit_scale - m.lse) - (hit == i ? 1.0f : 0.0f)) * m.gain;
+            d[i] = (s * __expf(z[i] * logit_scale - m.lse) - (hit == i ? 1.0f : 0.0f)) * m.gain;
             if (i >= have) d[i] = 0.0f;
         }
         uint16_t *const to = at.in(dz, ld); // 8-byte aligned
@@ -207,12 +286,20 @@ __global__ __launch_bounds__(1024) void k_ce_tokens(const int64_t *targets, int6
     if (threadIdx.x == 0) *count = before;
 }
 
-// h's rows of these tokens, one after the other.  A workgroup has a row; those past the last token's have nothing to do.
-__global__ __launch_bounds__(256) void k_gather(adahop_tensor_t x, int64_t cols, const int32_t *token, const int32_t *count, uint16_t *out, int64_t ld)
+// h's rows of these tokens, one after the other, and what dz needs of them.  A workgroup has a row; those past the last token's have nothing to do.
+// factor: logit_scale, or 1 where it and a d_loss for all tokens come later (then d_loss = nullptr).
+__global__ __launch_bounds__(256) void k_gather(adahop_tensor_t x, int64_t cols, loss_t p, const float *lse, const float *d_loss, int64_t d_loss_stride, float factor, const int32_t *token,
+                                                const int32_t *count, uint16_t *out, int64_t ld, token_t *rows)
 {
     const int64_t r = blockIdx.x;
     if (r >= *count) return;
-    const int64_t from = (int64_t)token[r] * x.ld;
+    const int32_t t = token[r];
+    if (threadIdx.x == 0) {
+        const int64_t y = p.targets[t];
+        const float g = (d_loss ? d_loss[t * d_loss_stride] : 1.0f) * factor;
+        rows[r] = {lse[t], y < p.V ? g : NAN, (int32_t)(y < p.V ? y : 0), t};
+    }
+    const int64_t from = t * x.ld;
     for (int64_t c = threadIdx.x * 8; c < ld; c += 256 * 8) {
         const raw8<false> v = load8<false>(x.data, from + c, (int)(cols - c < 8 ? cols - c : 8));
         *reinterpret_cast<u32x4 *>(out + r * ld + c) = v.w[0];
@@ -234,24 +321,48 @@ constexpr int64_t PIECE_BYTES = (int64_t)1 << 30; // of dz in the workspace, at 
 bool copies_as_it_is(const adahop_tensor_t &x, int64_t cols) { return aligned(x.data, 16) && x.ld % 8 == 0 && cols % 8 == 0; }
 
 struct forward_plan_t {
-    int64_t tiles;
-    bool large;
+    int64_t tiles; // of whose words a token has numbers
+    int few;       // k_ce_few's workgroups, or 0
+    int64_t large; // words that large tiles are computed of, the first ones
     size_t part, at, h, w, total;
 };
 
 struct backward_plan_t {
     int64_t words, pieces, ld; // of a piece of the vocabulary
-    size_t dz, sum_h, part, count, token, h, w, total;
+    size_t dz, sum_h, part, count, token, rows, h, w, total;
 };
 
-bool large_tiles(int64_t T, int64_t V) { return ceil_div(T, 256) * ceil_div(V, 256) >= 256; }
+constexpr int64_t FEW_LDS = 64 * 1024; // of h: two workgroups on a compute unit, without an attribute
+
+// Time of the logits of V words by tiles of either size, as plan16 sees it.
+double time_of_logits(int64_t T, int64_t V, int64_t D, bool large)
+{
+    const int64_t edge = large ? 256 : 128, room = large ? 256 : 512, tiles = ceil_div(T, edge) * ceil_div(V, edge), half_slabs = ceil_div(D, SLAB) * 2, rest = tiles % room;
+    const double ends = large ? 12.0 : 6.0, each = (large ? 0.74 : 0.6) * (double)half_slabs;
+    return (double)(tiles / room) * (ends + each) + (rest == 0 ? 0.0 : ends + (!large && rest <= 256 ? 0.3 * (double)half_slabs : each));
+}
+
+// Large tiles for all words, for none, or for as many as make whole rounds of them (50021 words for 1003 tokens of 2048: 213 us with large ones alone, four rounds of which the last has 16
+// tiles).
+int64_t words_of_large_tiles(int64_t T, int64_t V, int64_t D)
+{
+    const int64_t across = ceil_div(T, 256), rounds = across * ceil_div(V, 256) / 256, whole = rounds * 256 / across * 256;
+    const double all = time_of_logits(T, V, D, true), none = time_of_logits(T, V, D, false);
+    const double some = rounds > 0 && whole < V ? time_of_logits(T, whole, D, true) + time_of_logits(T, V - whole, D, false) + 3.0 : all;
+    return some < all && some < none ? whole : all <= none ? V : 0;
+}
 
 // lay_h, lay_w: the operand is laid out anew
 forward_plan_t forward_plan(int64_t T, int64_t V, int64_t D, bool lay_h, bool lay_w)
 {
     forward_plan_t p;
-    p.large = large_tiles(T, V);
-    p.tiles = ceil_div(V, p.large ? tile256_t::TM : tile128_t::TM);
+    p.large = words_of_large_tiles(T, V, D);
+    p.tiles = ceil_div(p.large, tile256_t::TM) + ceil_div(V - p.large, tile128_t::TM);
+    p.few = 0;
+    if (T <= FEW && (T <= 1 ? 1 : T <= 2 ? 2 : T <= 4 ? 4 : 8) * align_up(D, 512) * 2 <= FEW_LDS) {
+        p.few = (int)(ceil_div(V, 16) < 512 ? ceil_div(V, 16) : 512); // two workgroups of four waves per compute unit
+        p.tiles = p.few;
+    }
     const size_t ld = align_up(D, 8) * 2;
     p.part = 0;
     p.at = align_up((size_t)T * p.tiles * sizeof(float2), 256);
@@ -280,7 +391,8 @@ backward_plan_t backward_plan(int64_t T, int64_t V, int64_t D, bool lay_w)
     p.part = align_up(p.sum_h + (p.pieces > 1 ? (size_t)T * D * sizeof(float) : 0), 256);
     p.count = align_up(p.part + part, 256);
     p.token = p.count + 256;
-    p.h = align_up(p.token + T * sizeof(int32_t), 256);
+    p.rows = align_up(p.token + T * sizeof(int32_t), 256);
+    p.h = align_up(p.rows + T * sizeof(token_t), 256);
     p.w = align_up(p.h + T * ld, 256);
     p.total = align_up(p.w + (lay_w ? V * ld : 0), 256);
     return p;
@@ -341,8 +453,24 @@ int launch_linear_ce(const adahop_linear_ce_t &c, void *workspace, hipStream_t s
     if ((rc = lay_out(c.w, c.vocab, c.dim, lay_w, ws + p.w, &q.A, st)) != ADAHOP_OK) return rc;
     if ((rc = lay_out(c.h, c.tokens, c.dim, lay_h, ws + p.h, &q.B, st)) != ADAHOP_OK) return rc;
     q.K = align_up(c.dim, 8);
-    const stats_t e = {{c.targets, c.tokens, c.vocab, c.logit_scale, c.z_loss}, reinterpret_cast<float2 *>(ws + p.part), reinterpret_cast<float *>(ws + p.at)};
-    rc = p.large ? launch_stats<tile256_t>(q, e, st) : launch_stats<tile128_t>(q, e, st);
+    stats_t e = {{c.targets, c.tokens, c.vocab, c.logit_scale, c.z_loss}, 0, 0, p.tiles, reinterpret_cast<float2 *>(ws + p.part), reinterpret_cast<float *>(ws + p.at)};
+    if (p.few) {
+        const int room = c.tokens <= 1 ? 1 : c.tokens <= 2 ? 2 : c.tokens <= 4 ? 4 : 8;
+        const size_t lds = (size_t)room * align_up(c.dim, 512) * 2;
+        switch (room) {
+        case 1: k_ce_few<1><<<p.few, 256, lds, st>>>(q.A, q.B, q.K, e); break;
+        case 2: k_ce_few<2><<<p.few, 256, lds, st>>>(q.A, q.B, q.K, e); break;
+        case 4: k_ce_few<4><<<p.few, 256, lds, st>>>(q.A, q.B, q.K, e); break;
+        default: k_ce_few<8><<<p.few, 256, lds, st>>>(q.A, q.B, q.K, e);
+        }
+        rc = check_launch();
+    } else {
+        q.A.outer = p.large;
+        if (p.large > 0 && (rc = launch_stats<tile256_t>(q, e, st)) != ADAHOP_OK) return rc;
+        q.A.data += p.large * q.A.ld, q.A.outer = c.vocab - p.large;
+        e.v0 = p.large, e.tile = ceil_div(p.large, tile256_t::TM);
+        if (q.A.outer > 0) rc = launch_stats<tile128_t>(q, e, st);
+    }
     if (rc != ADAHOP_OK) return rc;
     k_ce_join<<<(unsigned)ceil_div(c.tokens, 4), 256, 0, st>>>(e.p, e.part, e.at, (int)p.tiles, c.loss, c.lse);
     return check_launch();
@@ -358,27 +486,29 @@ int launch_linear_ce_backward(const adahop_linear_ce_t &c, void *workspace, hipS
     char *const ws = static_cast<char *>(workspace);
     int32_t *const count = reinterpret_cast<int32_t *>(ws + p.count), *const token = reinterpret_cast<int32_t *>(ws + p.token);
     uint16_t *const dz = reinterpret_cast<uint16_t *>(ws + p.dz), *const h = reinterpret_cast<uint16_t *>(ws + p.h);
+    token_t *const rows = reinterpret_cast<token_t *>(ws + p.rows);
     side_t w;
     if ((rc = lay_out(c.w, V, D, lay_w, ws + p.w, &w, st)) != ADAHOP_OK) return rc;
     k_ce_tokens<<<1, 1024, 0, st>>>(c.targets, T, token, count);
     if ((rc = check_launch()) != ADAHOP_OK) return rc;
-    k_gather<<<(unsigned)T, 256, 0, st>>>(c.h, D, token, count, h, ldh);
+    const bool one = !c.d_loss || c.d_loss_stride == 0; // d_loss for all tokens
+    const float factor = one ? c.logit_scale : 1.0f;
+    const float *const by = one ? c.d_loss : nullptr;
+    k_gather<<<(unsigned)T, 256, 0, st>>>(c.h, D, {c.targets, T, V, c.logit_scale, c.z_loss}, c.lse, one ? nullptr : c.d_loss, c.d_loss_stride, one ? 1.0f : c.logit_scale, token, count, h,
+                                          ldh, rows);
     if ((rc = check_launch()) != ADAHOP_OK) return rc;
     if (c.d_h.data) {
         k_ce_zeros<<<(unsigned)T, 256, 0, st>>>(c.targets, D, c.d_h);
         if ((rc = check_launch()) != ADAHOP_OK) return rc;
     }
     const adahop_tensor_t none = {}, sum_h = {ws + p.sum_h, D, 1};
-    const bool one = !c.d_loss || c.d_loss_stride == 0; // for all tokens
-    const float factor = one ? c.logit_scale : 1.0f;
-    const float *const by = one ? c.d_loss : nullptr;
     for (int64_t i = 0; i < p.pieces; ++i) {
         const int64_t v0 = i * p.words, words = V - v0 < p.words ? V - v0 : p.words, ld = align_up(words, 8);
         const side_t piece = {w.data + v0 * w.ld, w.ld, words};
         product_t q = {};
         q.A = {h, ldh, T}, q.B = piece, q.K = ldh;
         q.rows_of = count;
-        const dlogits_t e = {{c.targets, T, V, c.logit_scale, c.z_loss}, token, c.lse, one ? nullptr : c.d_loss, c.d_loss_stride, v0, words, ld, one ? 1.0f : c.logit_scale, dz};
+        const dlogits_t e = {rows, c.logit_scale, c.z_loss, v0, words, ld, dz};
         if ((rc = launch_product16<false, ALONG, ALONG, false, false>(plan16(T, words, q.K, false, 1), q, e, nullptr, st)) != ADAHOP_OK) return rc;
         if (c.d_w.data) {
             const int64_t size = c.d_w.f32 ? 4 : 2, size_add = c.add.f32 ? 4 : 2;

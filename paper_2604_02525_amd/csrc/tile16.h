@@ -525,18 +525,21 @@ template <class K, bool SYMMETRIC, bool TURNED, class E> __global__ __launch_bou
 struct grad_t {
     static constexpr bool COUNTED = true;
     static constexpr int AHEAD = 2;
-    typedef nothing_t column_t;
-    typedef float4 more_t;
+    typedef float column_t; // the factor
+    struct more_t {
+        float4 add;
+        int32_t place;
+    };
     adahop_tensor_t to, add;
     const int32_t *place;
     float factor;
     const float *by;
-    __device__ __forceinline__ column_t column(int64_t, int) const { return {}; }
-    __device__ __forceinline__ more_t get(const spot_t &s, int have) const { return get4(add, s.row(), s.col(), have); }
-    __device__ __forceinline__ float4 apply(const spot_t &s, int have, float4 v, column_t, more_t more) const
+    __device__ __forceinline__ column_t column(int64_t, int) const { return by ? factor * *by : factor; }
+    __device__ __forceinline__ more_t get(const spot_t &s, int have) const { return {get4(add, s.row(), s.col(), have), place ? place[s.row()] : 0}; }
+    __device__ __forceinline__ float4 apply(const spot_t &s, int have, float4 v, column_t f, const more_t &m) const
     {
-        const float f = by ? factor * *by : factor, scale[4] = {f, f, f, f};
-        put4(to, place ? place[s.row()] : s.row(), s.col(), have, scale, v, more);
+        const float scale[4] = {f, f, f, f};
+        put4(to, place ? m.place : s.row(), s.col(), have, scale, v, m.add);
         return v;
     }
 };

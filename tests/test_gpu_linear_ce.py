@@ -86,7 +86,7 @@ class Case:
             assert np.all(off <= bound), (what, n, (off / bound).max())
 
 
-SIZES = [(1, 8, 1), (1, 64, 300), (3, 40, 257), (16, 128, 1000), (17, 72, 129), (127, 96, 255), (130, 264, 513), (257, 33, 1001), (300, 1024, 700), (520, 64, 2050)]
+SIZES = [(1, 8, 1), (1, 64, 300), (2, 1032, 9000), (3, 40, 257), (5, 504, 1003), (8, 512, 34), (8, 4104, 2051), (9, 512, 64), (16, 128, 1000), (17, 72, 129), (127, 96, 255), (130, 264, 513), (257, 33, 1001), (300, 1024, 700), (520, 64, 2050)]
 
 
 @pytest.mark.parametrize("T,D,V", SIZES)
