@@ -455,7 +455,7 @@ int adahop_linear_ce_backward(const adahop_linear_ce_t *p, void *workspace, size
  * have to stay below 4, as those of all usual coefficients do: X is held in fp32 and enters the products in fp16 (as two numbers where a side is at
  * most 128), the diagonals of A and of b A + c A^2 stay in fp32.  The result is then within about 1e-3 of its norm of the
  * same iteration in exact arithmetic.  A zero matrix gives zero (with eps = 0: NaN); infinities or NaN anywhere make the result NaN.
- * Sizes: 1 <= rows, cols <= 2^16, rows * cols < 2^31.  workspace: adahop_newton_schulz_workspace_bytes(rows, cols) bytes, 256-byte aligned,
+ * Sizes: 1 <= rows, cols <= 2^16, rows * cols < 2^31, ld < 2^26.  workspace: adahop_newton_schulz_workspace_bytes(rows, cols) bytes, 256-byte aligned,
  * contents undefined on return. */
 typedef struct {
     int64_t rows, cols;

@@ -8,15 +8,15 @@ namespace adahop {
 namespace {
 
 constexpr int64_t MAX_EXTENT = (int64_t)1 << 21, MAX_ELEMENTS = (int64_t)1 << 35, MAX_LD = (int64_t)1 << 40;
-constexpr int64_t MAX_SIDE = (int64_t)1 << 16, MAX_MATRIX = (int64_t)1 << 31, MAX_OPERAND_LD = (int64_t)1 << 22;
+constexpr int64_t MAX_SIDE = (int64_t)1 << 16, MAX_MATRIX = (int64_t)1 << 31, MAX_OPERAND_LD = (int64_t)1 << 22, MAX_MATRIX_LD = (int64_t)1 << 26;
 constexpr int MAX_STEPS = 64;
 
 bool present(const adahop_tensor_t &t) { return t.data != nullptr; }
 
-bool valid(const adahop_tensor_t &t, int64_t cols)
+bool valid(const adahop_tensor_t &t, int64_t cols, int64_t max_ld = MAX_LD)
 {
     if (!present(t)) return true;
-    return (t.f32 == 0 || t.f32 == 1) && t.ld >= cols && t.ld < MAX_LD && aligned(t.data, t.f32 ? 4 : 2);
+    return (t.f32 == 0 || t.f32 == 1) && t.ld >= cols && t.ld < max_ld && aligned(t.data, t.f32 ? 4 : 2);
 }
 
 bool valid_loss(const adahop_linear_ce_t *p)
@@ -83,7 +83,7 @@ size_t adahop_newton_schulz_workspace_bytes(int64_t rows, int64_t cols)
 int adahop_orthogonalize(const adahop_newton_schulz_t *method, const adahop_tensor_t *g, const adahop_tensor_t *out, void *workspace,
                          size_t workspace_bytes, void *stream)
 {
-    if (!valid_method(method) || !g || !out || !present(*g) || !present(*out) || !valid(*g, method->cols) || !valid(*out, method->cols)) return ADAHOP_E_INVALID_ARG;
+    if (!valid_method(method) || !g || !out || !present(*g) || !present(*out) || !valid(*g, method->cols, MAX_MATRIX_LD) || !valid(*out, method->cols, MAX_MATRIX_LD)) return ADAHOP_E_INVALID_ARG;
     if (!holds(workspace, workspace_bytes, newton_schulz_workspace_bytes(method->rows, method->cols))) return ADAHOP_E_WORKSPACE;
     return launch_newton_schulz(*method, *g, *out, nullptr, workspace, static_cast<hipStream_t>(stream));
 }
@@ -92,8 +92,8 @@ int adahop_muon_update(const adahop_newton_schulz_t *method, const adahop_muon_t
 {
     if (!valid_method(method) || !p || p->rows != method->rows || p->cols != method->cols) return ADAHOP_E_INVALID_ARG;
     for (const adahop_tensor_t *t : {&p->g, &p->momentum, &p->momentum_out, &p->w, &p->w_out})
-        if (!present(*t) || !valid(*t, p->cols)) return ADAHOP_E_INVALID_ARG;
-    if (!valid(p->w_bf16, p->cols) || (present(p->w_bf16) && p->w_bf16.f32)) return ADAHOP_E_INVALID_ARG;
+        if (!present(*t) || !valid(*t, p->cols, MAX_MATRIX_LD)) return ADAHOP_E_INVALID_ARG;
+    if (!valid(p->w_bf16, p->cols, MAX_MATRIX_LD) || (present(p->w_bf16) && p->w_bf16.f32)) return ADAHOP_E_INVALID_ARG;
     if (!p->momentum.f32 || !p->momentum_out.f32 || p->w.f32 != p->w_out.f32) return ADAHOP_E_INVALID_ARG;
     if (!isfinite(p->rate) || !isfinite(p->mu) || !isfinite(p->weight_decay) || (p->nesterov != 0 && p->nesterov != 1)) return ADAHOP_E_INVALID_ARG;
     if (!holds(workspace, workspace_bytes, newton_schulz_workspace_bytes(p->rows, p->cols))) return ADAHOP_E_WORKSPACE;

@@ -332,12 +332,12 @@ template <bool BY_ROW> struct result_t { // the last one, as the result
     __device__ __forceinline__ more_t get(const spot_t &s, int) const { return from.get(s); }
     __device__ __forceinline__ float4 apply(const spot_t &at, int, float4 v, const column_t &d, const more_t &m) const
     {
-        const int64_t r = at.row(), c = at.col();
-        if (r >= rows || c >= cols) return v;
+        if (at.row() >= rows || at.col() >= cols) return v;
         float n[4];
         from.next(v, d, m, n);
-        const float s[4] = {scale, scale, scale, scale};
-        put4(out, r, c, (int)(cols - c < 4 ? cols - c : 4), s, make_float4(n[0], n[1], n[2], n[3]), make_float4(0.0f, 0.0f, 0.0f, 0.0f));
+#pragma unroll
+        for (int i = 0; i < 4; ++i) n[i] *= scale;
+        put4_at(out, at, (int)(cols - at.col() < 4 ? cols - at.col() : 4), n);
         return v;
     }
 };
@@ -357,24 +357,20 @@ template <bool BY_ROW> struct update_t { // the last one, as a step of the weigh
     __device__ __forceinline__ column_t column(int64_t c, int have) const { return from.column(c, have); }
     __device__ __forceinline__ more_t get(const spot_t &s, int) const
     {
-        const int64_t r = s.row(), c = s.col();
         more_t m;
         m.x = from.get(s);
-        m.w = r < rows && c < cols ? get4(w, r, c, (int)(cols - c < 4 ? cols - c : 4)) : make_float4(0.0f, 0.0f, 0.0f, 0.0f);
+        m.w = s.row() < rows && s.col() < cols ? get4_at(w, s, (int)(cols - s.col() < 4 ? cols - s.col() : 4)) : make_float4(0.0f, 0.0f, 0.0f, 0.0f);
         return m;
     }
     __device__ __forceinline__ float4 apply(const spot_t &at, int, float4 v, const column_t &d, const more_t &m) const
     {
-        const int64_t r = at.row(), c = at.col();
-        if (r >= rows || c >= cols) return v;
-        const int have = (int)(cols - c < 4 ? cols - c : 4);
+        if (at.row() >= rows || at.col() >= cols) return v;
+        const int have = (int)(cols - at.col() < 4 ? cols - at.col() : 4);
         float n[4];
         from.next(v, d, m.x, n);
-        const float one[4] = {1.0f, 1.0f, 1.0f, 1.0f};
-        const float4 to = make_float4(keep * m.w.x - rate * n[0], keep * m.w.y - rate * n[1], keep * m.w.z - rate * n[2], keep * m.w.w - rate * n[3]),
-                     zero = make_float4(0.0f, 0.0f, 0.0f, 0.0f);
-        put4(out, r, c, have, one, to, zero);
-        if (copy.data) put4(copy, r, c, have, one, to, zero);
+        n[0] = keep * m.w.x - rate * n[0], n[1] = keep * m.w.y - rate * n[1], n[2] = keep * m.w.z - rate * n[2], n[3] = keep * m.w.w - rate * n[3];
+        put4_at(out, at, have, n);
+        if (copy.data) put4_at(copy, at, have, n);
         return v;
     }
 };

@@ -343,14 +343,6 @@ __device__ __forceinline__ uint32_t run_of_xcd(uint32_t id, uint32_t tiles)
     return xcd * per + (xcd < rest ? xcd : rest) + id / 8;
 }
 
-// What becomes of the sums is a finish E:
-//   COUNTED                        whether rows_of and K_of are looked at
-//   E::column_t, column(c, have)   what it reads for four columns, once for all their rows
-//   E::more_t, get(spot, have)     what it reads for four elements, ahead of its use (AHEAD - 1 blocks of 32 rows)
-//   float4 apply(spot, have, v, column, more) finishes and stores the first `have` of them; returns the values for put_turned
-//   put_turned(c, r, v)            SYMMETRIC: stores eight of them, C[r .. r + 8, c], as row c
-struct nothing_t {};
-
 // Where a lane's four elements are: a row and a column for the whole wave, and the lane's from there on.
 struct spot_t {
     int64_t r0, c0;
@@ -364,6 +356,64 @@ struct spot_t {
         return reinterpret_cast<T *>(reinterpret_cast<byte_t *>(base + r0 * ld + c0) + (uint32_t)((r * (uint32_t)ld + c) * sizeof(T)));
     }
 };
+
+// Four elements of a tensor of rows of ld < 2^26, and storing them: get4 and put4 with a wave's address in scalar registers.
+__device__ __forceinline__ float4 get4_at(const adahop_tensor_t &t, const spot_t &s, int have)
+{
+    float o[4] = {};
+    if (t.f32) {
+        const uint32_t *const p = s.in(static_cast<const uint32_t *>(t.data), t.ld);
+        if (have == 4) {
+            const u32x4 a = *reinterpret_cast<const u32x4_e4 *>(p);
+#pragma unroll
+            for (int i = 0; i < 4; ++i) o[i] = __uint_as_float(a[i]);
+        } else {
+#pragma unroll
+            for (int i = 0; i < 3; ++i)
+                if (i < have) o[i] = __uint_as_float(p[i]);
+        }
+    } else {
+        const uint16_t *const p = s.in(static_cast<const uint16_t *>(t.data), t.ld);
+#pragma unroll
+        for (int i = 0; i < 4; ++i)
+            if (i < have) o[i] = bf16_one(p[i]);
+    }
+    return make_float4(o[0], o[1], o[2], o[3]);
+}
+
+__device__ __forceinline__ void put4_at(const adahop_tensor_t &t, const spot_t &s, int have, const float (&v)[4])
+{
+    if (t.f32) {
+        uint32_t *const p = s.in(static_cast<uint32_t *>(t.data), t.ld);
+        if (have == 4) {
+            *reinterpret_cast<u32x4_e4 *>(p) = u32x4{__float_as_uint(v[0]), __float_as_uint(v[1]), __float_as_uint(v[2]), __float_as_uint(v[3])};
+        } else {
+#pragma unroll
+            for (int i = 0; i < 3; ++i)
+                if (i < have) p[i] = __float_as_uint(v[i]);
+        }
+    } else {
+        typedef uint32_t u32x2_e2 __attribute__((ext_vector_type(2), aligned(2), may_alias));
+        uint16_t *const p = s.in(static_cast<uint16_t *>(t.data), t.ld);
+        const u32x2 w = {bf16_pair(v[0], v[1]), bf16_pair(v[2], v[3])};
+        if (have == 4) {
+            *reinterpret_cast<u32x2_e2 *>(p) = w;
+        } else {
+#pragma unroll
+            for (int i = 0; i < 3; ++i)
+                if (i < have) p[i] = (uint16_t)(w[i >> 1] >> 16 * (i & 1));
+        }
+    }
+}
+
+// What becomes of the sums is a finish E:
+//   COUNTED                        whether rows_of and K_of are looked at
+//   E::column_t, column(c, have)   what it reads for four columns, once for all their rows
+//   E::more_t, get(spot, have)     what it reads for four elements, ahead of its use (AHEAD - 1 blocks of 32 rows)
+//   float4 apply(spot, have, v, column, more) finishes and stores the first `have` of them; returns the values for put_turned
+//   put_turned(c, r, v)            SYMMETRIC: stores eight of them, C[r .. r + 8, c], as row c
+struct nothing_t {};
+
 
 struct store_part_t { // a slice's sums as they are
     static constexpr int AHEAD = 2;
@@ -475,49 +525,57 @@ template <class K, bool F16, lies_t LA, lies_t LB, bool SEG, bool SYMMETRIC, cla
         finish_tile<K, SYMMETRIC>(q, n0, d0, smem, acc, e);
 }
 
-// The sums of the slices of the tiles that have some, in their order, finished: a wave has 32 rows of 32 columns of a tile.
+// The sums of the slices of the tiles that have some, finished: a workgroup has 32 rows of 32 columns of a tile, each of its waves every fourth slice, and the waves' sums are added in
+// their order.  (One wave for all slices: 31 of them of three tiles took 23 us.)
 // TURNED: the values go to put_turned, too, where the tile is not on a SYMMETRIC product's diagonal.
-template <class K, bool SYMMETRIC, bool TURNED, class E> __global__ __launch_bounds__(64) void k_join16(product_t q, E e)
+template <class K, bool SYMMETRIC, bool TURNED, class E> __global__ __launch_bounds__(256) void k_join16(product_t q, E e)
 {
-    constexpr int PITCH = 36, ACROSS = K::TN / 32, PATCHES = K::TM / 32 * ACROSS, STEPS = 4;
-    __shared__ float patch[TURNED ? 32 * PITCH : 1];
+    constexpr int PITCH = 36, ACROSS = K::TN / 32, PATCHES = K::TM / 32 * ACROSS;
+    __shared__ __attribute__((aligned(16))) float sums[4][32 * PITCH];
     const uint32_t tail = blockIdx.x / PATCHES, in = blockIdx.x % PATCHES;
-    const int lane = threadIdx.x, c4 = (lane & 7) * 4, r0 = lane >> 3;
+    const int lane = threadIdx.x & 63, w = __builtin_amdgcn_readfirstlane(threadIdx.x >> 6), c4 = (lane & 7) * 4, r0 = lane >> 3;
     int64_t n0, d0;
     place_of<K, SYMMETRIC>(q.nt, q.dt, q.whole + tail, n0, d0);
     if constexpr (E::COUNTED) {
         if (q.rows_of) q.A.outer = *q.rows_of;
     }
-    const int64_t first = n0 + in / ACROSS * 32, c0 = d0 + in % ACROSS * 32, r = first + r0, c = c0 + c4;
-    const auto spot = [&](int i) { return spot_t{first + 8 * i, c0, (uint32_t)r0, (uint32_t)c4}; };
+    const int64_t first = n0 + in / ACROSS * 32, c0 = d0 + in % ACROSS * 32, c = c0 + c4;
+    const spot_t spot = {first + 8 * w, c0, (uint32_t)r0, (uint32_t)c4};
     const int have = (int)(q.B.outer - c < 4 ? q.B.outer - c : 4);
-    const float *p = q.part + (int64_t)tail * q.slices * K::TM * K::TN + (r - n0) * K::TN + (c - d0); // of every element of a tile, whether C has it or not
+    const bool is = have > 0 && spot.row() < q.A.outer;
     typename E::column_t column;
-    typename E::more_t more[STEPS];
-    if (have > 0) column = e.column(c, have);
-    float4 sum[STEPS];
+    typename E::more_t more;
+    if (is) column = e.column(c, have), more = e.get(spot, have);
+    // of every element of a tile, whether C has it or not
+    const float *p = q.part + ((int64_t)tail * q.slices + w) * K::TM * K::TN + (first - n0 + r0) * K::TN + (c - d0);
+    float4 sum[4];
 #pragma unroll
-    for (int i = 0; i < STEPS; ++i) {
-        sum[i] = make_float4(0.0f, 0.0f, 0.0f, 0.0f);
-        if (have > 0 && r + 8 * i < q.A.outer) more[i] = e.get(spot(i), have);
-    }
-#pragma unroll 8
-    for (uint32_t s = 0; s < q.slices; ++s, p += K::TM * K::TN)
+    for (int i = 0; i < 4; ++i) sum[i] = make_float4(0.0f, 0.0f, 0.0f, 0.0f);
+#pragma unroll 4
+    for (uint32_t s = w; s < q.slices; s += 4, p += 4 * K::TM * K::TN)
 #pragma unroll
-        for (int i = 0; i < STEPS; ++i) {
+        for (int i = 0; i < 4; ++i) {
             const float4 v = *reinterpret_cast<const float4 *>(p + i * 8 * K::TN);
             sum[i] = make_float4(sum[i].x + v.x, sum[i].y + v.y, sum[i].z + v.z, sum[i].w + v.w);
         }
 #pragma unroll
-    for (int i = 0; i < STEPS; ++i)
-        if (have > 0 && r + 8 * i < q.A.outer) {
-            const float4 done = e.apply(spot(i), have, sum[i], column, more[i]);
-            if constexpr (TURNED) *reinterpret_cast<float4 *>(patch + (r0 + 8 * i) * PITCH + c4) = done;
+    for (int i = 0; i < 4; ++i) *reinterpret_cast<float4 *>(sums[w] + (r0 + 8 * i) * PITCH + c4) = sum[i];
+    __syncthreads();
+    float *const at = sums[0] + (r0 + 8 * w) * PITCH + c4;
+    if (is) {
+        float4 v = *reinterpret_cast<const float4 *>(at);
+#pragma unroll
+        for (int k = 1; k < 4; ++k) {
+            const float4 o = *reinterpret_cast<const float4 *>(at + k * 32 * PITCH);
+            v = make_float4(v.x + o.x, v.y + o.y, v.z + o.z, v.w + o.w);
         }
+        v = e.apply(spot, have, v, column, more);
+        if constexpr (TURNED) *reinterpret_cast<float4 *>(at) = v;
+    }
     if constexpr (TURNED) {
-        if (SYMMETRIC && n0 == d0) return;
-        lds_between_lanes();
-        put_mirror<2>(q, first, c0, patch, e);
+        __syncthreads();
+        if (w || (SYMMETRIC && n0 == d0)) return;
+        put_mirror<2>(q, first, c0, sums[0], e);
     }
 }
 
@@ -742,7 +800,7 @@ template <class K, bool F16, lies_t LA, lies_t LB, bool SEG, bool SYMMETRIC, cla
     k_product16<K, F16, LA, LB, SEG, SYMMETRIC, E><<<plan.whole + rest * plan.slices, K::THREADS, K::LDS, st>>>(q, e);
     const int rc = check_launch();
     if (rc != ADAHOP_OK || !rest) return rc;
-    k_join16<K, SYMMETRIC, SYMMETRIC, E><<<rest * (K::TM / 32) * (K::TN / 32), 64, 0, st>>>(q, e);
+    k_join16<K, SYMMETRIC, SYMMETRIC, E><<<rest * (K::TM / 32) * (K::TN / 32), 256, 0, st>>>(q, e);
     return check_launch();
 }
 
@@ -771,7 +829,7 @@ template <bool F16, bool SEG, bool SYMMETRIC, bool TURNED, class E> inline int l
     k_direct16<F16, SEG, SYMMETRIC, TURNED, E><<<plan.whole + rest * plan.slices, K::THREADS, K::LDS, st>>>(q, e);
     const int rc = check_launch();
     if (rc != ADAHOP_OK || !rest) return rc;
-    k_join16<K, SYMMETRIC, TURNED, E><<<rest * 4, 64, 0, st>>>(q, e);
+    k_join16<K, SYMMETRIC, TURNED, E><<<rest * 4, 256, 0, st>>>(q, e);
     return check_launch();
 }
 

@@ -89,7 +89,7 @@ def muon(rows=64, cols=96, method_rows=64, ws=FAKE, size=1 << 40, **more):
 def test_newton_schulz_refuses():
     assert ns(rows=0) == ns(cols=0) == ns(rows=(1 << 16) + 1) == ns(rows=1 << 16, cols=1 << 15, g=t(ld=1 << 15), out=t(ld=1 << 15)) == BAD
     assert ns(steps=0) == ns(steps=65) == ns(a=float("nan")) == ns(b=float("inf")) == ns(eps=-1.0) == ns(eps=float("nan")) == ns(scale=float("inf")) == BAD
-    assert ns(g=None) == ns(out=None) == ns(g=t(data=None)) == ns(out=t(data=None)) == ns(g=t(ld=95)) == ns(out=t(ld=96, f32=3)) == ns(g=t(ld=96, data=FAKE + 1)) == BAD
+    assert ns(g=None) == ns(out=None) == ns(g=t(data=None)) == ns(out=t(data=None)) == ns(g=t(ld=95)) == ns(out=t(ld=96, f32=3)) == ns(g=t(ld=96, data=FAKE + 1)) == ns(g=t(ld=1 << 26)) == ns(out=t(ld=1 << 26)) == BAD
     assert ns(ws=None) == ns(ws=FAKE + 128) == ns(size=1000) == SPACE
     assert ah.lib().adahop_newton_schulz_workspace_bytes(0, 5) == 0
     assert muon(rows=63) == muon(cols=95) == muon(method_rows=0) == BAD
