@@ -409,7 +409,7 @@ __device__ __forceinline__ void put4_at(const adahop_tensor_t &t, const spot_t &
 // What becomes of the sums is a finish E:
 //   COUNTED                        whether rows_of and K_of are looked at
 //   E::column_t, column(c, have)   what it reads for four columns, once for all their rows
-//   E::more_t, get(spot, have)     what it reads for four elements, ahead of its use (AHEAD - 1 blocks of 32 rows)
+//   E::more_t, get(spot, have)     what it reads for four elements, ahead of its use (by AHEAD - 1 blocks of 32 rows)
 //   float4 apply(spot, have, v, column, more) finishes and stores the first `have` of them; returns the values for put_turned
 //   put_turned(c, r, v)            SYMMETRIC: stores eight of them, C[r .. r + 8, c], as row c
 struct nothing_t {};
@@ -445,8 +445,8 @@ template <int NT, class E> __device__ __forceinline__ void put_mirror(const prod
 }
 
 // C's rows go by way of a wave's own patch of LDS, 32 at a time, so that a lane has four consecutive columns of a row: 16-byte stores of whole rows.  In
-// the accumulators a lane has column lane % 16 of a tile, rows 4 (lane / 16) + i.  What the finish reads is read 64 rows ahead: no load passes a store that it might
-// depend on, and one block of rows ahead does not cover the memory's latency.
+// the accumulators a lane has column lane % 16 of a tile, rows 4 (lane / 16) + i.  What the finish reads is read a block of rows ahead (AHEAD = 2), or with the block itself (1): no load
+// passes a store that it might depend on.  Two blocks ahead measured the same.
 template <class K, bool SYMMETRIC, class E>
 __device__ __forceinline__ void finish_tile(const product_t &q, int64_t n0, int64_t d0, uint8_t *smem, const v4f (&acc)[K::MT][K::NT], const E &e)
 {
