@@ -7,7 +7,7 @@
 //
 // The scheme is that of the weight gradient from a checkpoint (wgrad8.hip): both operands go to LDS by copies that pass no register, a wave's 16 x 16 x 32 instructions are fed
 // from LDS 32 elements of the contraction ahead.  A DOWN operand is turned by the transposing reads of LDS; an ALONG one is read as it lies, 16 bytes (eight elements
-// of a row) per lane.  What lies outside an operand reads as zero, in both.  Here LDS holds two slabs of 64 elements of the contraction rather than four of 32: an ALONG
+// of a row) per lane.  What lies outside an operand reads as zero, in both.  Here LDS holds slabs of 64 elements of the contraction rather than stages of 32: an ALONG
 // operand's rows are then fetched in whole lines of 128 bytes (where both are DOWN, whose rows are long, in halves all the same, further ahead).  In halves of them the L2s' requests, not the matrix cores, set the pace: 32 compute units' took as long as their matrix instructions
 // (matrix cores busy 53 % against 79 % with both operands DOWN).
 //
@@ -53,11 +53,11 @@ struct product_t {
     const int32_t *rows_of, *K_of; // (or nullptr) how many of A's outer indices and of the contraction's elements there are, where only the device knows
 };
 
-// Tiles of C by WN x WD waves of 16 MT x 16 NT.
-template <int MT_, int NT_, int WN_, int WD_> struct shape_t {
-    static constexpr int MT = MT_, NT = NT_, WN = WN_, WD = WD_;
+// Tiles of C by WN x WD waves of 16 MT x 16 NT, a ring of RING slabs.
+template <int MT_, int NT_, int WN_, int WD_, int RING_> struct shape_t {
+    static constexpr int MT = MT_, NT = NT_, WN = WN_, WD = WD_, RING = RING_;
     static constexpr int WAVES = WN * WD, THREADS = 64 * WAVES, TM = 16 * WN * MT, TN = 16 * WD * NT, RA = 2 * TM, RB = 2 * TN; // bytes of a row of a DOWN slab
-    static constexpr uint32_t A = SLAB * RA, B = SLAB * RB, SLOT = A + B, LDS = 2 * SLOT;
+    static constexpr uint32_t A = SLAB * RA, B = SLAB * RB, SLOT = A + B, LDS = RING * SLOT;
     static constexpr int COPIES = A / 1024 / (WAVES / 2); // per wave and slab: half of the waves copy A, the others B
     static_assert(TM == TN && COPIES * (WAVES / 2) * 1024 == A && COPIES % 2 == 0, "whole copies");
     // DOWN: by what the pieces of 32 bytes of a row are exchanged, so that the eight rows of a transposing read of half a wave (four consecutive ones and those 8 further on)
@@ -72,9 +72,10 @@ template <int MT_, int NT_, int WN_, int WD_> struct shape_t {
     }
 };
 
-typedef shape_t<8, 4, 2, 4> tile256_t;
-typedef shape_t<6, 3, 2, 4> tile192_t;
-typedef shape_t<4, 4, 2, 2> tile128_t;
+typedef shape_t<8, 4, 2, 4, 2> tile256_t;
+typedef shape_t<6, 3, 2, 4, 3> tile192_t;
+typedef shape_t<4, 4, 2, 2, 2> tile128_t;       // two workgroups on a compute unit
+typedef shape_t<4, 4, 2, 2, 4> tile128_alone_t; // one: a slab takes less time than its copies, so they go further ahead
 
 // A wave's copies, all of one operand: the resource that a slab is read from, where it goes on, and what this lane reads of it.
 // UNIT: elements of the contraction that are copied at a time, a slab or half of one.
@@ -123,10 +124,11 @@ template <class K, bool SEG, int UNIT> struct copies_t {
         }
     }
     // Into scalar registers, which the copies take the resource from: it is the same in all lanes, but the compiler may have come to it another way.
+    static __device__ __forceinline__ uint32_t one(uint32_t v) { return (uint32_t)__builtin_amdgcn_readfirstlane(v); }
+    __device__ __forceinline__ void settle_from() { from.x = one(from.x), from.y = one(from.y), from.z = one(from.z), from.w = one(from.w); }
     __device__ __forceinline__ void settle()
     {
-        const auto one = [](uint32_t v) { return (uint32_t)__builtin_amdgcn_readfirstlane(v); };
-        from.x = one(from.x), from.y = one(from.y), from.z = one(from.z), from.w = one(from.w);
+        settle_from();
         full = one(full), last = one(last), step = one(step);
         if constexpr (SEG) {
 #pragma unroll
@@ -156,8 +158,8 @@ __device__ __forceinline__ u32x4 lds_read16(uint32_t lds_addr) { return *(const 
 template <class K, bool F16, lies_t LA, lies_t LB, bool SEG>
 __device__ __forceinline__ void multiply(const product_t &q, int64_t n0, int64_t d0, int64_t begin, int64_t end, uint8_t *smem, v4f (&acc)[K::MT][K::NT])
 {
-    constexpr int MT = K::MT, NT = K::NT;
-    constexpr bool FINE = LA == DOWN && LB == DOWN; // halves of slabs are copied, three ahead
+    constexpr int MT = K::MT, NT = K::NT, RING = K::RING;
+    constexpr bool FINE = LA == DOWN && LB == DOWN; // halves of slabs are copied, 2 RING - 1 ahead
     constexpr int UNIT = FINE ? SLAB / 2 : SLAB;
     typedef copies_t<K, SEG, UNIT> mine_t;
     constexpr int COPIES = mine_t::COPIES;
@@ -181,20 +183,17 @@ __device__ __forceinline__ void multiply(const product_t &q, int64_t n0, int64_t
         mine.set(LA, q.A, q.K, n0, begin, odd, w, lane, q.seg.a, segment);
     mine.settle();
     const uint32_t own = of_b ? K::A + (w - K::WAVES / 2) * COPIES * 1024 : w * COPIES * 1024;
-    uint32_t to = base, at = base; // where is copied to next, the slab that is read next
-    const auto other = [&](uint32_t slot) { return slot == base ? base + K::SLOT : base; };
-    const auto after = [&](uint32_t place) { // FINE: slab, second half, the other slab, its second half
-        constexpr uint32_t HALF = SLAB / 2 * K::RA;
-        return place == base ? base + HALF : place == base + HALF ? base + K::SLOT : place == base + K::SLOT ? base + K::SLOT + HALF : base;
-    };
+    uint32_t to = base, at = base; // the slabs that are copied to next and read next
+    const auto after = [&](uint32_t slot) { return slot == base + (RING - 1) * K::SLOT ? base : slot + K::SLOT; };
     uint32_t cut[2] = {};
     // The resource of what is copied next: a whole unit, the contraction's end, or nothing.  Without a branch: it would end the block that the
     // instructions around are scheduled in.
     const auto trim = [&] {
         mine.from.z = ahead >= UNIT ? mine.full : ahead > 0 ? mine.last : 0;
+        mine.settle_from();
         if constexpr (LA == ALONG || LB == ALONG) cut[0] = ahead >= UNIT ? 0 : mine.beyond[0], cut[1] = ahead >= UNIT ? 0 : mine.beyond[1];
     };
-    const auto copied = [&] {
+    const auto copied = [&](bool whole_slab) { // whole_slab: with this unit it is
         if constexpr (SEG) {
             const bool cross = ++in == run;
             mine.forward(cross ? (segment ? mine.hop[1] : mine.hop[0]) : (int64_t)mine.step);
@@ -204,12 +203,13 @@ __device__ __forceinline__ void multiply(const product_t &q, int64_t n0, int64_t
             mine.forward(mine.step);
         }
         ahead -= UNIT;
-        to = FINE ? after(to) : other(to);
+        to = whole_slab ? after(to) : to;
         trim();
     };
-    const auto copy = [&](auto number) {
+    const auto copy = [&](auto number, auto half) {
         constexpr int i = decltype(number)::value;
-        dma16_bounded<i * 1024>(mine.from, LA == ALONG || LB == ALONG ? mine.off[i] | cut[i & 1] : mine.off[i], __builtin_amdgcn_readfirstlane(to + own));
+        constexpr uint32_t lies_at = decltype(half)::value * (SLAB / 2) * K::RA + i * 1024; // half: which of a slab's a FINE unit is
+        dma16_bounded<lies_at>(mine.from, LA == ALONG || LB == ALONG ? mine.off[i] | cut[i & 1] : mine.off[i], __builtin_amdgcn_readfirstlane(to + own));
     };
 
     // What this lane reads of a half slab: the matrix instruction wants the eight elements from 8 (lane / 16) on of row or column lane % 16.  DOWN: four lanes of a group of
@@ -260,12 +260,12 @@ __device__ __forceinline__ void multiply(const product_t &q, int64_t n0, int64_t
     static_assert(NT > 2 && COPIES * APART <= PLACES - NT, "what goes beside the matrix instructions fits");
 
     trim();
-#pragma unroll 1
-    for (int i = 0; i < (FINE ? 3 : 2); ++i) {
-        static_for<0, COPIES>(copy);
-        copied();
-    }
-    wait_for_copies<(FINE ? 2 : 1) * COPIES>();
+    static_for<0, FINE ? 2 * RING - 1 : RING>([&](auto unit) {
+        constexpr int half = FINE ? decltype(unit)::value & 1 : 0;
+        static_for<0, COPIES>([&](auto i) { copy(i, std::integral_constant<int, half>{}); });
+        copied(!FINE || half);
+    });
+    wait_for_copies<(FINE ? 2 * RING - 2 : RING - 1) * COPIES>();
     // Everything that the compiler counts with the reads of LDS is done before these, and these are issued in the order of the loop's: its waits in
     // the loop go by what may be outstanding on either way into it.
     __builtin_amdgcn_s_waitcnt(0xc07f); // lgkmcnt(0)
@@ -280,8 +280,8 @@ __device__ __forceinline__ void multiply(const product_t &q, int64_t n0, int64_t
     }
     ADAHOP_PIN();
     // A's operands are read again, for the next half, behind the last of the NT matrix instructions that use them, B's into the other set of registers.  The last of a unit is
-    // read behind its last half's first instructions; after the barrier that follows, what comes two slabs later goes in its place, and the next unit, copied
-    // for at least the time of one and a half halves, is there for all waves.
+    // read behind its last half's first instructions; after the barrier that follows, what comes RING slabs later goes in its place, and the next unit, copied
+    // for at least the time of one and a half halves with two slabs, is there for all waves.
     const auto half = [&](auto which) {
         constexpr int now = decltype(which)::value, next = now ^ 1;
         static_for<0, PLACES>([&](auto number) {
@@ -291,8 +291,8 @@ __device__ __forceinline__ void multiply(const product_t &q, int64_t n0, int64_t
             acc[m][n] = mfma16<F16>(va, vb, acc[m][n]);
             if constexpr (m == 0 && n < 2) read_a(now, MT - 1, n);
             if constexpr ((FINE || now == 1) && place == BARRIER) {
-                asm volatile("s_waitcnt vmcnt(%0) lgkmcnt(0)\n\ts_barrier" ::"n"(FINE ? COPIES : 0) : "memory");
-                if constexpr (now == 1) at = other(at);
+                asm volatile("s_waitcnt vmcnt(%0) lgkmcnt(0)\n\ts_barrier" ::"n"((FINE ? 2 * RING - 3 : RING - 2) * COPIES) : "memory");
+                if constexpr (now == 1) at = after(at);
             }
             if constexpr (m > 0) {
                 constexpr int first = ((m - 1) * (NT - 2) + n - 2) * EACH;
@@ -302,10 +302,10 @@ __device__ __forceinline__ void multiply(const product_t &q, int64_t n0, int64_t
                     static_for<first, first + EACH < READS_B ? first + EACH : READS_B>([&](auto i) { read_b(next, decltype(i)::value / PB, decltype(i)::value % PB); });
             }
             if constexpr ((FINE || now == 1) && place >= FIRST && (place - FIRST) % APART == 0 && (place - FIRST) / APART < COPIES)
-                copy(std::integral_constant<int, (place - FIRST) / APART>{});
+                copy(std::integral_constant<int, (place - FIRST) / APART>{}, std::integral_constant<int, FINE ? next : 0>{});
             ADAHOP_PIN();
         });
-        if constexpr (FINE || now == 1) copied();
+        if constexpr (FINE || now == 1) copied(!FINE || now == 0); // (FINE: in a first half the second one of a slab, in a second half the next one's first)
     };
     while (left > 0) {
         half(std::integral_constant<int, 0>{});
@@ -747,6 +747,8 @@ struct plan16_t {
 // In microseconds, on 256 compute units: half a slab of a round of workgroups takes 0.74 with tiles of 256, 0.43 of 192, one workgroup per compute unit; of 128 0.6 where there are two
 // per compute unit, 0.3 where there is one; a round's beginning and end 12, 10 and 6.  Whole rounds of tiles are computed whole.  What is left is cut into slices if they,
 // their sums' way to memory and back and one launch more take less time than another round.  `slices_at_most` = 1: never.
+constexpr double ROUND192 = 0.43, ALONE128 = 0.3;
+
 inline plan16_t plan16(int64_t rows, int64_t cols, int64_t K, bool symmetric, int64_t slices_at_most = 64)
 {
     plan16_t best = {};
@@ -754,8 +756,8 @@ inline plan16_t plan16(int64_t rows, int64_t cols, int64_t K, bool symmetric, in
     for (const int edge : {256, 192, 128}) {
         const int64_t room = edge > 128 ? 256 : 512, down = ceil_div(rows, edge), across = ceil_div(cols, edge);
         const int64_t tiles = symmetric ? down * (down + 1) / 2 : down * across, rest = tiles % room;
-        const double each = edge == 256 ? 0.74 : edge == 192 ? 0.43 : 0.6, ends = edge == 256 ? 12.0 : edge == 192 ? 10.0 : 6.0, whole = (double)(tiles / room) * (ends + each * (double)stages);
-        const auto a_round = [&](int64_t workgroups, int64_t of) { return ends + (workgroups <= 256 && edge == 128 ? 0.3 : each) * (double)of; };
+        const double each = edge == 256 ? 0.74 : edge == 192 ? ROUND192 : 0.6, ends = edge == 256 ? 12.0 : edge == 192 ? 10.0 : 6.0, whole = (double)(tiles / room) * (ends + each * (double)stages);
+        const auto a_round = [&](int64_t workgroups, int64_t of) { return ends + (workgroups <= 256 && edge == 128 ? ALONE128 : each) * (double)of; };
         plan16_t p = {edge, (uint32_t)tiles, (uint32_t)tiles, 1, 0, 0, 0.0};
         double time = whole + (rest ? a_round(rest, stages) : 0.0);
         for (int64_t s = 2; rest && s <= slices_at_most && stages / s >= 4; ++s) {
@@ -811,7 +813,9 @@ inline int launch_product16(const plan16_t &plan, product_t q, const E &e, void 
     q.whole = plan.whole, q.slices = plan.slices, q.slice = plan.slice;
     q.part = static_cast<float *>(part);
     return plan.edge == 256 ? launch_tiles16<tile256_t, F16, LA, LB, SEG, SYMMETRIC>(q, plan, e, st)
-           : plan.edge == 192 ? launch_tiles16<tile192_t, F16, LA, LB, SEG, SYMMETRIC>(q, plan, e, st) : launch_tiles16<tile128_t, F16, LA, LB, SEG, SYMMETRIC>(q, plan, e, st);
+           : plan.edge == 192 ? launch_tiles16<tile192_t, F16, LA, LB, SEG, SYMMETRIC>(q, plan, e, st)
+           : plan.whole + (plan.tiles - plan.whole) * plan.slices <= 256 ? launch_tiles16<tile128_alone_t, F16, LA, LB, SEG, SYMMETRIC>(q, plan, e, st)
+                                                                         : launch_tiles16<tile128_t, F16, LA, LB, SEG, SYMMETRIC>(q, plan, e, st);
 }
 
 template <bool F16, bool SEG, bool SYMMETRIC, bool TURNED, class E> inline int configure_direct16()
@@ -837,6 +841,7 @@ template <bool F16, lies_t LA, lies_t LB, bool SEG, bool SYMMETRIC, class E> inl
 {
     int rc = configure_product16<tile256_t, F16, LA, LB, SEG, SYMMETRIC, E>();
     if (rc == ADAHOP_OK) rc = configure_product16<tile192_t, F16, LA, LB, SEG, SYMMETRIC, E>();
+    if (rc == ADAHOP_OK) rc = configure_product16<tile128_alone_t, F16, LA, LB, SEG, SYMMETRIC, E>();
     return rc == ADAHOP_OK ? configure_product16<tile128_t, F16, LA, LB, SEG, SYMMETRIC, E>() : rc;
 }
 
