@@ -75,7 +75,7 @@ template <int MT_, int NT_, int WN_, int WD_, int RING_> struct shape_t {
 typedef shape_t<8, 4, 2, 4, 2> tile256_t;
 typedef shape_t<6, 3, 2, 4, 3> tile192_t;
 typedef shape_t<4, 4, 2, 2, 2> tile128_t;       // two workgroups on a compute unit
-typedef shape_t<4, 4, 2, 2, 4> tile128_alone_t; // one: a slab takes less time than its copies, so they go further ahead
+typedef shape_t<2, 4, 4, 2, 4> tile128_alone_t; // one: a slab takes less time than its copies, so they go further ahead
 
 // A wave's copies, all of one operand: the resource that a slab is read from, where it goes on, and what this lane reads of it.
 // UNIT: elements of the contraction that are copied at a time, a slab or half of one.
@@ -747,7 +747,7 @@ struct plan16_t {
 // In microseconds, on 256 compute units: half a slab of a round of workgroups takes 0.74 with tiles of 256, 0.43 of 192, one workgroup per compute unit; of 128 0.6 where there are two
 // per compute unit, 0.3 where there is one; a round's beginning and end 12, 10 and 6.  Whole rounds of tiles are computed whole.  What is left is cut into slices if they,
 // their sums' way to memory and back and one launch more take less time than another round.  `slices_at_most` = 1: never.
-constexpr double ROUND192 = 0.43, ALONE128 = 0.3;
+constexpr double ROUND192 = 0.43, ALONE128 = 0.23;
 
 inline plan16_t plan16(int64_t rows, int64_t cols, int64_t K, bool symmetric, int64_t slices_at_most = 64)
 {
