@@ -1,6 +1,7 @@
 """A stack of gated MLP blocks trained with MXFP4 products (forward and input gradients), its activations kept in 8 bits.
 
     python examples/gated_mlp_stack.py --tokens 4096 --hidden 2048 --ffn 5632 --blocks 4 --steps 10
+    python examples/gated_mlp_stack.py --tokens 4096 --hidden 2048 --ffn 5632 --blocks 4 --steps 10 --vocab 32000
 
 Each block is  h -> [g | u] = h W_gu^T -> a = silu(g) u -> y = a W_down^T,  and between two blocks
 
@@ -11,6 +12,9 @@ backward pass takes: norm(s') and norm(y) in 8 bits, g and u in 8 bits, two numb
 element; a is formed again from g and u by the backward pass, and the weight gradients are computed from the 8-bit
 rows, in bf16: nothing is rounded to 4 bits on the way into the float32 gradient. Where speed counts for more, adahop_ckpt8_unpack and an
 MXFP4 product take less than half of the time for large layers.  The one checkpoint of norm(s') serves the gradient of W_gu (times w_pre, feature by feature) and the norm's own backward pass.
+
+With --vocab the stack ends in the loss of one word per token (adahop_linear_ce: h times bf16 output weights, the logits never in memory), and the matrices of the blocks are updated by
+their orthogonalised momentum (adahop_muon_update), which leaves the next step's bf16 weights behind; the vectors and the output weights take the plain step.
 """
 import argparse
 import os
@@ -29,7 +33,7 @@ class GatedMlpStack:
     """hidden and ffn are multiples of 32 (of iht_block if that is larger).  Weights are bfloat16 with float32 masters; `grads` holds
     their float32 gradients, which backward() adds to once accumulate is set."""
 
-    def __init__(self, hidden, ffn, blocks, iht_block=32, residual_scale=1.0, seed=0, device="cuda"):
+    def __init__(self, hidden, ffn, blocks, iht_block=32, residual_scale=1.0, seed=0, device="cuda", vocab=0):
         self.hidden, self.ffn, self.blocks, self.iht_block, self.residual_scale = hidden, ffn, blocks, iht_block, residual_scale
         draw = torch.Generator(device=device).manual_seed(seed)
         self.masters = {}
@@ -40,6 +44,9 @@ class GatedMlpStack:
             self.masters[f"post{b}"] = torch.ones(hidden, device=device)
             self.masters[f"gate{b}"] = torch.full((hidden,), 0.5, device=device)
         self.masters[f"pre{blocks}"] = torch.ones(hidden, device=device)
+        if vocab:
+            self.masters["out"] = torch.randn(vocab, hidden, generator=draw, device=device) * hidden ** -0.5
+        self.momentum = {}
         self.grads = {k: torch.empty_like(w) for k, w in self.masters.items()}
         self.round_weights()
 
@@ -113,6 +120,30 @@ class GatedMlpStack:
         self.update(rate)
         return off.square().mean() / 2
 
+    def words_loss_and_gradients(self, x, words):
+        """Mean loss of predicting `words` (int64 per token, negative: none) from h, a tensor; fills grads."""
+        h, kept = self.forward(x)
+        f = ah.adahop_linear_ce(h, self.w["out"], words)
+        each = 1.0 / (words >= 0).sum().clamp(min=1).float()
+        d_h = ah.adahop_linear_ce_backward(h, self.w["out"], words, f["lse"], each.expand(len(words)), d_w=self.grads["out"])["d_h"]
+        self.backward(d_h, kept)
+        return f["loss"].sum() * each
+
+    def orthogonal_update(self, rate, scale=0.2):
+        """The blocks' matrices a step of `scale * rate` per element along their orthogonalised momentum, all else as in update()."""
+        for k, m in self.masters.items():
+            if m.dim() == 2 and k != "out":
+                momentum = self.momentum.setdefault(k, torch.zeros_like(m))
+                ah.adahop_muon_update(m, self.grads[k], momentum, rate, scale=scale * max(m.shape) ** 0.5, w_bf16=self.w[k])
+            else:
+                m -= self.grads[k] * (rate * m.norm() / self.grads[k].norm().clamp(min=1e-30))
+                self.w[k] = m.to(torch.bfloat16) if m.dim() == 2 else m
+
+    def words_step(self, x, words, rate):
+        loss = self.words_loss_and_gradients(x, words)
+        self.orthogonal_update(rate)
+        return loss
+
 
 def kept_bytes(kept):
     """Bytes of all that forward() leaves for the backward pass."""
@@ -128,12 +159,13 @@ def main():
     for name, default in (("tokens", 4096), ("hidden", 2048), ("ffn", 5632), ("blocks", 4), ("steps", 10), ("iht-block", 32)):
         p.add_argument("--" + name, type=int, default=default)
     p.add_argument("--rate", type=float, default=0.02)
+    p.add_argument("--vocab", type=int, default=0)
     a = p.parse_args()
     ah.adahop_prepare_device()
-    net = GatedMlpStack(a.hidden, a.ffn, a.blocks, a.iht_block)
+    net = GatedMlpStack(a.hidden, a.ffn, a.blocks, a.iht_block, vocab=a.vocab)
     draw = torch.Generator(device="cuda").manual_seed(1)
     x = torch.randn(a.tokens, a.hidden, generator=draw, device="cuda").to(torch.bfloat16)
-    target = x.float().roll(1, 1)
+    target = torch.randint(0, a.vocab, (a.tokens,), generator=draw, device="cuda") if a.vocab else x.float().roll(1, 1)
     kept = net.forward(x)[1]
     elements = a.tokens * a.blocks * (2 * a.hidden + 2 * a.ffn) + a.tokens * a.hidden
     print(f"kept for the backward pass: {kept_bytes(kept) / 2**20:.1f} MiB ({kept_bytes(kept) / elements:.3f} bytes an element)", flush=True)
@@ -141,7 +173,7 @@ def main():
     for i in range(a.steps):
         torch.cuda.synchronize()
         t = time.perf_counter()
-        loss = net.step(x, target, a.rate)
+        loss = (net.words_step if a.vocab else net.step)(x, target, a.rate)
         torch.cuda.synchronize()
         print(f"step {i}: loss {loss.item():.5f}, {(time.perf_counter() - t) * 1e3:.2f} ms", flush=True)
 

@@ -13,6 +13,9 @@
 // errors of the elements are independent, adds less than that to a sum over them.  Where all tokens have one d_loss (that of a mean), it and logit_scale are left out of
 // dz and multiply the products' fp32 sums: the target's element, mostly the largest of its row, is then -1 and little more, which loses next to nothing (8192 x 4096 x 32000: d_h 2.6e-3
 // of its norm off with them inside).  All sums, lse and the loss are fp32.
+//
+// What bounds it: the matrix cores' power (8192 x 4096 x 32000: forward 1.6 ms, 1.35 PFLOP/s; backward, three such products, 4.9 ms, 1.31; 16384 x 8192 x 65536 backward 38.4 ms, 1.37);
+// a few tokens: reading w (one of 4096 against 32000 words: 45 us, 5.8 TB/s).  Forward that writes no logits spares 2 T V bytes twice, 0.2 ms of the 1.6 at the copy's rate.
 #include <math.h>
 
 #include "row_sums.h"

@@ -11,9 +11,13 @@
 //   * The diagonals of A and of b A + c A^2 are apart, in fp32: they are by far the largest elements, their rounding would be the largest error.  With A = D + O:
 //     the polynomial is b (D + O) + c (D^2 + D O + O D + O^2), of which the matrix cores form O^2, and its diagonal joins a in what multiplies the carried X.
 //   * Where the smaller side is at most 128, X enters as the sum of two fp16 numbers: errors there average over fewer elements, and the products cost little.
-// The result is then 2e-4 to 1e-3 of its norm off the same iteration in 64 bits (bf16's own rounding: 1.7e-3).
+// The result is then 2e-4 to 1.6e-3 of its norm off the same iteration in 64 bits (bf16's own rounding: 1.7e-3).
 //
 // A and A^2 are symmetric: only tiles on and below the diagonal are computed, the mirror image is stored with them.
+//
+// What bounds it (five steps): large matrices the matrix cores' power, and the step product's end, which reads and writes 10 bytes an element of fp32 and fp16 iterates (28672 x 8192 updated: 28.1 ms,
+// 1.12 PFLOP/s of what is counted once); middle ones rounds of tiles that do not fill the card (4096 x 4096: 1.41 ms, 0.97; 2048 x 2048 updated: 0.35 ms, 0.5), where the split of the last round into slices and the choice of tiles is
+// worth most; small ones 17 launches of some 5 us that wait for each other (256 x 256: 86 us, 185 with tiles of 128 or more).
 #include <math.h>
 
 #include "tile16.h"
@@ -398,20 +402,19 @@ ns_plan_t ns_plan(int64_t rows, int64_t cols)
     p.split = (p.wide ? rows : cols) <= SPLIT_SIDE;
     p.ld = row_pitch(p.cols), p.ld_side = row_pitch(p.side), p.ld_turned = row_pitch(p.rows);
     const int64_t long_k = p.length * (p.split ? 3 : 1), side_k = p.side * (p.split ? 2 : 1);
-    p.gram = plan16(p.side, p.side, long_k, true);
+    p.gram = plan16(p.side, p.side, long_k, true, 64, p.split);
     p.poly = plan16(p.side, p.side, p.side, true);
-    p.step = plan16(p.rows, p.cols, side_k, false);
+    p.step = plan16(p.rows, p.cols, side_k, false, 64, p.split);
     const plan16_t gram = plan_direct16(p.side, p.side, long_k, true), poly = plan_direct16(p.side, p.side, p.side, true), step = plan_direct16(p.rows, p.cols, side_k, false);
-    // k_direct16 wants both operands by rows: the iterate's transpose for the step of a wide matrix, for A of a tall one.  It is the step that writes it, if it runs there.
+    // k_direct16 wants both operands by rows: the iterate's transpose for the step of a wide matrix, for A of a tall one.  It is the step that writes it, running there itself: a tall
+    // matrix has both there or neither.  A of a split wide matrix (one tile of 128, both operands by rows) is always better off there.
     p.poly_direct = poly.time < p.poly.time;
     if (p.wide) {
-        p.gram_direct = gram.time < p.gram.time;
+        p.gram_direct = p.split || gram.time < p.gram.time;
         p.step_direct = step.time < p.step.time;
-    } else {
-        p.gram_direct = gram.time + step.time < p.gram.time + (step.time < p.step.time ? step.time : p.step.time);
-        p.step_direct = p.gram_direct || step.time < p.step.time;
-    }
-    p.keeps_turned = p.wide ? p.step_direct : p.gram_direct;
+    } else
+        p.gram_direct = p.step_direct = gram.time + step.time < p.gram.time + p.step.time;
+    p.keeps_turned = p.step_direct;
     if (p.gram_direct) p.gram = gram;
     if (p.poly_direct) p.poly = poly;
     if (p.step_direct) p.step = step;
@@ -443,7 +446,8 @@ device_once_t g_once;
 
 template <bool SEG> int configure_some()
 {
-    int rc = configure_all16<true, ALONG, ALONG, SEG, true, gram_t>();
+    int rc = ADAHOP_OK;
+    if constexpr (!SEG) rc = configure_all16<true, ALONG, ALONG, SEG, true, gram_t>();
     if (rc == ADAHOP_OK) rc = configure_all16<true, DOWN, DOWN, SEG, true, gram_t>();
     if (rc == ADAHOP_OK) rc = configure_all16<true, ALONG, DOWN, SEG, false, step_t<true>>();
     if (rc == ADAHOP_OK) rc = configure_all16<true, ALONG, ALONG, SEG, false, step_t<false>>();
@@ -453,9 +457,7 @@ template <bool SEG> int configure_some()
     if (rc == ADAHOP_OK) rc = configure_all16<true, ALONG, ALONG, SEG, false, update_t<false>>();
     if (rc == ADAHOP_OK) rc = configure_direct16<true, SEG, true, true, gram_t>();
     if (rc == ADAHOP_OK) rc = configure_direct16<true, SEG, false, true, step_t<true>>();
-    if (rc == ADAHOP_OK) rc = configure_direct16<true, SEG, false, false, step_t<true>>();
     if (rc == ADAHOP_OK) rc = configure_direct16<true, SEG, false, true, step_t<false>>();
-    if (rc == ADAHOP_OK) rc = configure_direct16<true, SEG, false, false, step_t<false>>();
     if (rc == ADAHOP_OK) rc = configure_direct16<true, SEG, false, false, result_t<true>>();
     if (rc == ADAHOP_OK) rc = configure_direct16<true, SEG, false, false, result_t<false>>();
     if (rc == ADAHOP_OK) rc = configure_direct16<true, SEG, false, false, update_t<true>>();
@@ -490,7 +492,9 @@ struct ns_call_t {
             if (!p.wide) q.A = q.B = {x.turned, x.ld_turned, p.side};
             return launch_direct16<true, SEG, true, true>(p.gram, q, e, ws + p.part, st);
         }
-        return p.wide ? launch_product16<true, ALONG, ALONG, SEG, true>(p.gram, q, e, ws + p.part, st) : launch_product16<true, DOWN, DOWN, SEG, true>(p.gram, q, e, ws + p.part, st);
+        if constexpr (!SEG)
+            if (p.wide) return launch_product16<true, ALONG, ALONG, SEG, true>(p.gram, q, e, ws + p.part, st);
+        return launch_product16<true, DOWN, DOWN, SEG, true>(p.gram, q, e, ws + p.part, st);
     }
     int poly(const float (&k)[3]) const
     {
@@ -512,8 +516,7 @@ struct ns_call_t {
                 q.A = square, q.B = {x.turned, x.ld_turned, p.cols}, q.seg = {2, {0, 0, 0}, {0, x.low, 0}};
             else
                 q.A = {x.h, x.ld, p.rows}, q.B = square, q.seg = {2, {0, x.low, 0}, {0, 0, 0}};
-            if (p.keeps_turned) return launch_direct16<true, SEG, false, TURNED>(p.step, q, e, ws + p.part, st);
-            return launch_direct16<true, SEG, false, false>(p.step, q, e, ws + p.part, st);
+            return launch_direct16<true, SEG, false, TURNED>(p.step, q, e, ws + p.part, st);
         }
         if constexpr (WIDE) {
             q.A = {P(), p.ld_side, p.rows}, q.B = {x.h, x.ld, p.cols};

@@ -5,6 +5,9 @@
 // Either operand may hold the contraction along its rows (ALONG, [outer][K]) or down its columns (DOWN, [K][outer]), so that no operand is ever transposed
 // in memory: a gradient of logits [tokens][vocabulary] enters one product by its rows and another by its columns.
 //
+// What bounds it: the matrix cores, on large problems their power (16384 x 8192 x 65536, three such products: 1.37 PFLOP/s, the library's bf16 product of 8192 x 8192 x 8192 1.33 with contiguous
+// contraction, 1.04 with both operands strided); where a compute unit has one workgroup, the pace of its copies and barriers (half a slab of a tile of 128: 0.23 us, its matrix instructions 0.11).
+//
 // The scheme is that of the weight gradient from a checkpoint (wgrad8.hip): both operands go to LDS by copies that pass no register, a wave's 16 x 16 x 32 instructions are fed
 // from LDS 32 elements of the contraction ahead.  A DOWN operand is turned by the transposing reads of LDS; an ALONG one is read as it lies, 16 bytes (eight elements
 // of a row) per lane.  What lies outside an operand reads as zero, in both.  Here LDS holds slabs of 64 elements of the contraction rather than stages of 32: an ALONG
@@ -75,7 +78,8 @@ template <int MT_, int NT_, int WN_, int WD_, int RING_> struct shape_t {
 typedef shape_t<8, 4, 2, 4, 2> tile256_t;
 typedef shape_t<6, 3, 2, 4, 3> tile192_t;
 typedef shape_t<4, 4, 2, 2, 2> tile128_t;       // two workgroups on a compute unit
-typedef shape_t<2, 4, 4, 2, 4> tile128_alone_t; // one: a slab takes less time than its copies, so they go further ahead
+typedef shape_t<2, 4, 4, 2, 4> tile128_alone_t; // one: a slab takes less time than its copies, so they go further ahead.  2048 x 2048 updated: 359 us, with tile128_t 459, with a
+                                                // ring of four and four waves 413; two of these tiles on a compute unit (rings of two) were slower or the same
 
 // A wave's copies, all of one operand: the resource that a slab is read from, where it goes on, and what this lane reads of it.
 // UNIT: elements of the contraction that are copied at a time, a slab or half of one.
@@ -745,15 +749,16 @@ struct plan16_t {
 };
 
 // In microseconds, on 256 compute units: half a slab of a round of workgroups takes 0.74 with tiles of 256, 0.43 of 192, one workgroup per compute unit; of 128 0.6 where there are two
-// per compute unit, 0.3 where there is one; a round's beginning and end 12, 10 and 6.  Whole rounds of tiles are computed whole.  What is left is cut into slices if they,
-// their sums' way to memory and back and one launch more take less time than another round.  `slices_at_most` = 1: never.
+// per compute unit, 0.23 where there is one; a round's beginning and end 12, 10 and 6.  Whole rounds of tiles are computed whole.  What is left is cut into slices if they,
+// their sums' way to memory and back and one launch more take less time than another round.  `slices_at_most` = 1: never.  `small`: tiles of 128 alone.
 constexpr double ROUND192 = 0.43, ALONE128 = 0.23;
 
-inline plan16_t plan16(int64_t rows, int64_t cols, int64_t K, bool symmetric, int64_t slices_at_most = 64)
+inline plan16_t plan16(int64_t rows, int64_t cols, int64_t K, bool symmetric, int64_t slices_at_most = 64, bool small = false)
 {
     plan16_t best = {};
     const int64_t stages = ceil_div(K, SLAB) * 2; // of 32 elements of the contraction
     for (const int edge : {256, 192, 128}) {
+        if (small && edge > 128) continue;
         const int64_t room = edge > 128 ? 256 : 512, down = ceil_div(rows, edge), across = ceil_div(cols, edge);
         const int64_t tiles = symmetric ? down * (down + 1) / 2 : down * across, rest = tiles % room;
         const double each = edge == 256 ? 0.74 : edge == 192 ? ROUND192 : 0.6, ends = edge == 256 ? 12.0 : edge == 192 ? 10.0 : 6.0, whole = (double)(tiles / room) * (ends + each * (double)stages);
@@ -770,7 +775,7 @@ inline plan16_t plan16(int64_t rows, int64_t cols, int64_t K, bool symmetric, in
                 p.part_bytes = (size_t)rest * number * edge * edge * sizeof(float);
             }
         }
-        if (edge == 256 || time < best.time) best = p, best.time = time;
+        if (!best.edge || time < best.time) best = p, best.time = time;
     }
     return best;
 }
@@ -806,16 +811,18 @@ template <class K, bool F16, lies_t LA, lies_t LB, bool SEG, bool SYMMETRIC, cla
     return check_launch();
 }
 
-// A product as planned.  part: room for plan.part_bytes.
+// A product as planned (SEG: with `small`).  part: room for plan.part_bytes.
 template <bool F16, lies_t LA, lies_t LB, bool SEG, bool SYMMETRIC, class E>
 inline int launch_product16(const plan16_t &plan, product_t q, const E &e, void *part, hipStream_t st)
 {
     q.whole = plan.whole, q.slices = plan.slices, q.slice = plan.slice;
     q.part = static_cast<float *>(part);
-    return plan.edge == 256 ? launch_tiles16<tile256_t, F16, LA, LB, SEG, SYMMETRIC>(q, plan, e, st)
-           : plan.edge == 192 ? launch_tiles16<tile192_t, F16, LA, LB, SEG, SYMMETRIC>(q, plan, e, st)
-           : plan.whole + (plan.tiles - plan.whole) * plan.slices <= 256 ? launch_tiles16<tile128_alone_t, F16, LA, LB, SEG, SYMMETRIC>(q, plan, e, st)
-                                                                         : launch_tiles16<tile128_t, F16, LA, LB, SEG, SYMMETRIC>(q, plan, e, st);
+    if constexpr (!SEG) {
+        if (plan.edge == 256) return launch_tiles16<tile256_t, F16, LA, LB, SEG, SYMMETRIC>(q, plan, e, st);
+        if (plan.edge == 192) return launch_tiles16<tile192_t, F16, LA, LB, SEG, SYMMETRIC>(q, plan, e, st);
+    }
+    return plan.whole + (plan.tiles - plan.whole) * plan.slices <= 256 ? launch_tiles16<tile128_alone_t, F16, LA, LB, SEG, SYMMETRIC>(q, plan, e, st)
+                                                                       : launch_tiles16<tile128_t, F16, LA, LB, SEG, SYMMETRIC>(q, plan, e, st);
 }
 
 template <bool F16, bool SEG, bool SYMMETRIC, bool TURNED, class E> inline int configure_direct16()
@@ -839,8 +846,11 @@ template <bool F16, bool SEG, bool SYMMETRIC, bool TURNED, class E> inline int l
 
 template <bool F16, lies_t LA, lies_t LB, bool SEG, bool SYMMETRIC, class E> inline int configure_all16()
 {
-    int rc = configure_product16<tile256_t, F16, LA, LB, SEG, SYMMETRIC, E>();
-    if (rc == ADAHOP_OK) rc = configure_product16<tile192_t, F16, LA, LB, SEG, SYMMETRIC, E>();
+    int rc = ADAHOP_OK;
+    if constexpr (!SEG) {
+        rc = configure_product16<tile256_t, F16, LA, LB, SEG, SYMMETRIC, E>();
+        if (rc == ADAHOP_OK) rc = configure_product16<tile192_t, F16, LA, LB, SEG, SYMMETRIC, E>();
+    }
     if (rc == ADAHOP_OK) rc = configure_product16<tile128_alone_t, F16, LA, LB, SEG, SYMMETRIC, E>();
     return rc == ADAHOP_OK ? configure_product16<tile128_t, F16, LA, LB, SEG, SYMMETRIC, E>() : rc;
 }
