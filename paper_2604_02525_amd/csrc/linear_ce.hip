@@ -318,6 +318,49 @@ __global__ __launch_bounds__(256) void k_ce_zeros(const int64_t *targets, int64_
     for (int64_t c = threadIdx.x * 8; c < cols; c += 256 * 8) store8_any(out, t * out.ld + c, (int)(cols - c < 8 ? cols - c : 8), zero);
 }
 
+// d_w of up to FEW_D_W tokens: bound by writing it.  A lane has four features of all tokens in registers and forms their sums for eight words at a time, in the tokens' order; what dz
+// it needs is the same for a whole workgroup and comes by scalar loads.  131072 words of 2048 features, bf16: 152 us, as a product's tiles, which would be nothing but their beginnings and ends,
+// 229 (and by matrix instructions of 32 tokens without tiles 178 to 192); twice the tokens take 328 for 65536 words of 4096, and the tiles 212.
+constexpr int FEW_D_W = 8, D_W_WORDS = 32; // words of a workgroup
+
+__global__ __launch_bounds__(256) void k_ce_d_w_few(const uint16_t *__restrict__ h, int64_t ldh, const uint16_t *__restrict__ dz, int64_t ld, const int32_t *__restrict__ count, int64_t words,
+                                                    int64_t cols, grad_t e)
+{
+    const int n = *count;
+    const int64_t c = ((int64_t)blockIdx.y * 256 + threadIdx.x) * 4, v0 = (int64_t)blockIdx.x * D_W_WORDS;
+    if (c >= cols) return;
+    const int have = (int)(cols - c < 4 ? cols - c : 4);
+    const float f = e.column(c, have), scale[4] = {f, f, f, f};
+    float x[FEW_D_W][4];
+#pragma unroll
+    for (int t = 0; t < FEW_D_W; ++t) {
+        u32x2 four = {0, 0};
+        if (t < n) four = *reinterpret_cast<const u32x2 *>(h + t * ldh + c); // rows of whole pieces of eight
+        x[t][0] = bf16_lo(four[0]), x[t][1] = bf16_hi(four[0]), x[t][2] = bf16_lo(four[1]), x[t][3] = bf16_hi(four[1]);
+    }
+    for (int64_t v = v0; v < words && v < v0 + D_W_WORDS; v += 8) {
+        float4 more[8];
+#pragma unroll
+        for (int j = 0; j < 8; ++j)
+            if (v + j < words) more[j] = get4(e.add, v + j, c, have);
+        float sum[8][4] = {};
+#pragma unroll
+        for (int t = 0; t < FEW_D_W; ++t) {
+            if (t >= n) break;
+            const u32x4 z = *reinterpret_cast<const u32x4 *>(dz + t * ld + v); // dz's rows too
+#pragma unroll
+            for (int j = 0; j < 8; ++j) {
+                const float of = j & 1 ? bf16_hi(z[j >> 1]) : bf16_lo(z[j >> 1]);
+#pragma unroll
+                for (int k = 0; k < 4; ++k) sum[j][k] = fmaf(of, x[t][k], sum[j][k]);
+            }
+        }
+#pragma unroll
+        for (int j = 0; j < 8; ++j)
+            if (v + j < words) put4(e.to, v + j, c, have, scale, make_float4(sum[j][0], sum[j][1], sum[j][2], sum[j][3]), more[j]);
+    }
+}
+
 // ---- host -----------------------------------------------------------------------------------------------------------------------
 constexpr int64_t PIECE_BYTES = (int64_t)1 << 30; // of dz in the workspace, at most (one word's column however long)
 
@@ -519,7 +562,12 @@ int launch_linear_ce_backward(const adahop_linear_ce_t &c, void *workspace, hipS
             q.rows_of = nullptr, q.K_of = count;
             const grad_t g = {{static_cast<char *>(c.d_w.data) + v0 * c.d_w.ld * size, c.d_w.ld, c.d_w.f32},
                               c.add.data ? adahop_tensor_t{static_cast<char *>(c.add.data) + v0 * c.add.ld * size_add, c.add.ld, c.add.f32} : none, nullptr, factor, by};
-            if ((rc = launch_product16<false, DOWN, DOWN, false, false>(plan16(words, D, T, false), q, g, ws + p.part, st)) != ADAHOP_OK) return rc;
+            if (T <= FEW_D_W) {
+                k_ce_d_w_few<<<dim3((unsigned)ceil_div(words, D_W_WORDS), (unsigned)ceil_div(D, 1024)), 256, 0, st>>>(h, ldh, dz, ld, count, words, D, g);
+                rc = check_launch();
+            } else
+                rc = launch_product16<false, DOWN, DOWN, false, false>(plan16(words, D, T, false), q, g, ws + p.part, st);
+            if (rc != ADAHOP_OK) return rc;
         }
         if (c.d_h.data) {
             const bool end = i + 1 == p.pieces;

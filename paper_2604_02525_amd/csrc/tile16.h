@@ -6,7 +6,9 @@
 // in memory: a gradient of logits [tokens][vocabulary] enters one product by its rows and another by its columns.
 //
 // What bounds it: the matrix cores, on large problems their power (16384 x 8192 x 65536, three such products: 1.37 PFLOP/s, the library's bf16 product of 8192 x 8192 x 8192 1.33 with contiguous
-// contraction, 1.04 with both operands strided); where a compute unit has one workgroup, the pace of its copies and barriers (half a slab of a tile of 128: 0.23 us, its matrix instructions 0.11).
+// contraction, 1.04 with both operands strided); where a compute unit has one workgroup of 128 x 128, LDS: half a slab
+// takes 0.23 us, its matrix instructions 0.11, 48 KB read from LDS and 16 KB copied there 0.21 at 128 bytes a cycle (four waves would read 32 KB, but there is nothing to hide a wave's waits behind then: 413 us
+// for an update that takes 359).
 //
 // The scheme is that of the weight gradient from a checkpoint (wgrad8.hip): both operands go to LDS by copies that pass no register, a wave's 16 x 16 x 32 instructions are fed
 // from LDS 32 elements of the contraction ahead.  A DOWN operand is turned by the transposing reads of LDS; an ALONG one is read as it lies, 16 bytes (eight elements
