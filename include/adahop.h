@@ -452,8 +452,8 @@ int adahop_linear_ce_backward(const adahop_linear_ce_t *p, void *workspace, size
 /* Orthogonalisation by Newton-Schulz products:
  *   X = U / (|U| + eps) (Frobenius norm),  `steps` times  X <- a X + (b A + c A^2) X  with A = X X^T,  result = scale X
  * For rows > cols the same from the other side (A = X^T X).  1 <= steps <= 64; a, b, c, scale finite, eps >= 0 and finite.  The singular values of X
- * have to stay below 4, as those of all usual coefficients do: X is held in fp32 and enters the products in fp16 (as two numbers where a side is at
- * most 128), the diagonals of A and of b A + c A^2 stay in fp32.  The result is then within about 2e-3 of its norm of the
+ * have to stay below 4 and the elements of b A + c A^2 off its diagonal below 60, as with all usual coefficients, or the result is NaN or infinite: X is held in fp32 and enters
+ * the products in fp16 (as two numbers where a side is at most 128), the diagonals of A and of b A + c A^2 stay in fp32.  The result is then within about 2e-3 of its norm of the
  * same iteration in exact arithmetic.  A zero matrix gives zero (with eps = 0: NaN); infinities or NaN anywhere make the result NaN.
  * Sizes: 1 <= rows, cols <= 2^16, rows * cols < 2^31, ld < 2^26.  workspace: adahop_newton_schulz_workspace_bytes(rows, cols) bytes, 256-byte aligned,
  * contents undefined on return. */
