@@ -129,7 +129,7 @@ class GatedMlpStack:
         self.backward(d_h, kept)
         return f["loss"].sum() * each
 
-    def orthogonal_update(self, rate, scale=0.2):
+    def orthogonal_update(self, rate, scale=0.02):
         """The blocks' matrices a step of `scale * rate` per element along their orthogonalised momentum, all else as in update()."""
         for k, m in self.masters.items():
             if m.dim() == 2 and k != "out":
