@@ -11,7 +11,9 @@
 //   * The diagonals of A and of b A + c A^2 are apart, in fp32: they are by far the largest elements, their rounding would be the largest error.  With A = D + O:
 //     the polynomial is b (D + O) + c (D^2 + D O + O D + O^2), of which the matrix cores form O^2, and its diagonal joins a in what multiplies the carried X.
 //   * Where the smaller side is at most 128, X enters as the sum of two fp16 numbers: errors there average over fewer elements, and the products cost little.
-// The result is then 2e-4 to 1.6e-3 of its norm off the same iteration in 64 bits (bf16's own rounding: 1.7e-3).
+//   * In the steps whose noise later ones multiply, the diagonal takes X as the products take it (as_rounded_t).
+// The result of five steps is then 2e-4 to 1.2e-3 of its norm off the same iteration in 64 bits for matrices of random elements and gradients with a few strong directions (bf16's own rounding: 1.7e-3), 4e-3 at most
+// whatever the singular values, 5e-3 where the elements are two or four different numbers; in ten steps 3e-3 and 1.2e-2 (one direction alone: the fp32 iterate's rounding times 3.4445^10).
 //
 // A and A^2 are symmetric: only tiles on and below the diagonal are computed, the mirror image is stored with them.
 //
@@ -269,6 +271,26 @@ struct poly_t {
     __device__ __forceinline__ void put_turned(int64_t col, int64_t r, const float (&v)[8]) const { store_eight(P + col * ld + r, v); }
 };
 
+// In a step whose noise many others multiply, the diagonal of b A + c A^2 takes X as the products take it, in fp16, and a alone the carried one.  X of few directions, X = u v^T say,
+// has P X = p u (u^T X) with P = b A + c A^2 for whatever X holds, also for its rounding N: along u.  With P's diagonal times the exact X, - p diag(u^2) N is left, in directions that
+// X does not have, and each later step multiplies those by a.  (160 x 200 of one direction: 2.7e-3 of the result's norm off after five steps
+// and 6.9e-2 after eight; this way 4e-4 and 1e-3.)
+// Where A is mostly diagonal the exact X is what is better, so the last steps have it: iterate() decides.
+struct as_rounded_t {
+    float a;
+    int on;
+    __device__ __forceinline__ void put_right(const float (&x)[4], const float (&d)[4], float (&n)[4]) const
+    {
+        if (!on) return;
+        float s[4], back[4];
+#pragma unroll
+        for (int i = 0; i < 4; ++i) s[i] = x[i] * pow2(SX);
+        f16_values(f16_four(s), back);
+#pragma unroll
+        for (int i = 0; i < 4; ++i) n[i] += (d[i] - a) * (back[i] * pow2(-SX) - x[i]);
+    }
+};
+
 // The next iterate's elements from the product's and the carried ones.  BY_ROW: the diagonal goes by rows (A = X X^T), else by columns.
 template <bool BY_ROW> struct carried_t;
 
@@ -280,12 +302,14 @@ template <> struct carried_t<true> {
     };
     const float *x, *diagonal;
     int64_t ld;
+    as_rounded_t as;
     __device__ __forceinline__ column_t column(int64_t, int) const { return {}; }
     __device__ __forceinline__ more_t get(const spot_t &s) const { return {*reinterpret_cast<const float4 *>(s.in(x, ld)), diagonal[s.row()]}; }
-    static __device__ __forceinline__ void next(float4 v, column_t, const more_t &m, float (&n)[4])
+    __device__ __forceinline__ void next(float4 v, column_t, const more_t &m, float (&n)[4]) const
     {
-        const float k = pow2(-SB - SX);
+        const float k = pow2(-SB - SX), x4[4] = {m.x.x, m.x.y, m.x.z, m.x.w}, d[4] = {m.d, m.d, m.d, m.d};
         n[0] = m.d * m.x.x + v.x * k, n[1] = m.d * m.x.y + v.y * k, n[2] = m.d * m.x.z + v.z * k, n[3] = m.d * m.x.w + v.w * k;
+        as.put_right(x4, d, n);
     }
 };
 
@@ -293,12 +317,14 @@ template <> struct carried_t<false> {
     typedef float4 column_t, more_t;
     const float *x, *diagonal;
     int64_t ld;
+    as_rounded_t as;
     __device__ __forceinline__ column_t column(int64_t c, int) const { return *reinterpret_cast<const float4 *>(diagonal + c); }
     __device__ __forceinline__ more_t get(const spot_t &s) const { return *reinterpret_cast<const float4 *>(s.in(x, ld)); }
-    static __device__ __forceinline__ void next(float4 v, const column_t &d, const more_t &x, float (&n)[4])
+    __device__ __forceinline__ void next(float4 v, const column_t &d, const more_t &x, float (&n)[4]) const
     {
-        const float k = pow2(-SB - SX);
+        const float k = pow2(-SB - SX), x4[4] = {x.x, x.y, x.z, x.w}, d4[4] = {d.x, d.y, d.z, d.w};
         n[0] = d.x * x.x + v.x * k, n[1] = d.y * x.y + v.y * k, n[2] = d.z * x.z + v.z * k, n[3] = d.w * x.w + v.w * k;
+        as.put_right(x4, d4, n);
     }
 };
 
@@ -534,10 +560,13 @@ template <bool SEG, bool WIDE> int iterate(const ns_call_t &c, const adahop_newt
 {
     const float k[3] = {m.a, m.b, m.c};
     for (int i = 0; i < m.steps; ++i) {
+        // As long as later steps multiply what X lacks by more than 4: with the usual coefficients all but the last two.  (All of them: matrices of no preferred directions are 1.4e-3 off after five steps
+        // instead of 0.8e-3; none or all but the last three: those of half of the directions 4e-3 instead of 1.5e-3.)
+        const bool rounded = !SEG && pow(fabs((double)m.a), m.steps - 1 - i) > 4.0;
         int rc = c.gram<SEG>(i & 1);
         if (rc == ADAHOP_OK) rc = c.poly(k);
         if (rc != ADAHOP_OK) return rc;
-        const carried_t<WIDE> from = {c.at(0).x, c.diagonal(), c.p.ld};
+        const carried_t<WIDE> from = {c.at(0).x, c.diagonal(), c.p.ld, {m.a, rounded}};
         if (i + 1 < m.steps)
             rc = c.step<SEG, WIDE, true>(i & 1, step_t<WIDE>{from, c.at((i & 1) ^ 1)});
         else if (u)
