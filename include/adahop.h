@@ -425,7 +425,7 @@ int adahop_ckpt8_wgrad(int64_t tokens, int64_t d_out, int64_t d_in, const adahop
  *   backward  reads these, lse and d_loss (float, element t at t * d_loss_stride, 0 for one that serves all; NULL: 1); writes
  *             d_h and d_w (either may be absent).  add: what earlier micro-batches left; it may be d_w.
  * h: bf16 [tokens, dim], w: bf16 [vocab, dim]; d_h [tokens, dim], d_w and add [vocab, dim] of either type.
- * A token whose target is negative (padding, a prompt) has the loss 0 and no part in the gradients; a target of vocab
+ * A token whose target is negative (padding, a prompt) has the loss 0 and no part in the gradients (a d_loss for all has none without a token that has a target: 1 / 0 of a mean over none); a target of vocab
  * or more makes the loss and the gradients NaN.  lse is that of all tokens.  A row of z with NaN or +infinity has the lse NaN.
  * The products are of bf16 values with fp32 sums; dz is rounded to bf16 (by at most 2^-8 of each element) before the gradients'
  * products, whose results are rounded once more if they are bf16.  No atomics: the same bits in every call.

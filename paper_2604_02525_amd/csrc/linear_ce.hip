@@ -560,7 +560,7 @@ int launch_linear_ce_backward(const adahop_linear_ce_t &c, void *workspace, hipS
             const bool end = i + 1 == p.pieces;
             q.A = {dz, ld, T}, q.B = {piece.data, piece.ld, D}, q.K = words;
             q.rows_of = count, q.K_of = nullptr;
-            const grad_t g = {end ? c.d_h : sum_h, i ? sum_h : none, end ? token : nullptr, factor, by};
+            const grad_t g = {end ? c.d_h : sum_h, i ? sum_h : none, end ? token : nullptr, factor, by, count};
             if ((rc = launch_product16<false, ALONG, DOWN, false, false>(plan16(T, D, words, false), q, g, ws + p.part, st)) != ADAHOP_OK) return rc;
         }
         if (c.d_w.data) {
@@ -568,7 +568,7 @@ int launch_linear_ce_backward(const adahop_linear_ce_t &c, void *workspace, hipS
             q.A = {dz, ld, words}, q.B = {h, ldh, D}, q.K = T;
             q.rows_of = nullptr, q.K_of = count;
             const grad_t g = {{static_cast<char *>(c.d_w.data) + v0 * c.d_w.ld * size, c.d_w.ld, c.d_w.f32},
-                              c.add.data ? adahop_tensor_t{static_cast<char *>(c.add.data) + v0 * c.add.ld * size_add, c.add.ld, c.add.f32} : none, nullptr, factor, by};
+                              c.add.data ? adahop_tensor_t{static_cast<char *>(c.add.data) + v0 * c.add.ld * size_add, c.add.ld, c.add.f32} : none, nullptr, factor, by, count};
             if (T <= FEW_D_W) {
                 k_ce_d_w_few<<<dim3((unsigned)ceil_div(words, D_W_WORDS), (unsigned)ceil_div(D, 1024)), 256, 0, st>>>(h, ldh, dz, ld, count, words, D, g);
                 rc = check_launch();

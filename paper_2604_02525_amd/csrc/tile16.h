@@ -585,7 +585,8 @@ template <class K, bool SYMMETRIC, bool TURNED, class E> __global__ __launch_bou
     }
 }
 
-// to = factor v + add, of bf16 or float.  place (or nullptr): which of `to`'s rows row r is.  by (or nullptr): a number on the device that the factor is multiplied by.
+// to = factor v + add, of bf16 or float.  place (or nullptr): which of `to`'s rows row r is.  by (or nullptr): a number on the device that the factor is multiplied by, of
+// tokens of which there are *tokens: without one it takes no part, whatever it is.
 struct grad_t {
     static constexpr bool COUNTED = true;
     static constexpr int AHEAD = 2;
@@ -598,7 +599,8 @@ struct grad_t {
     const int32_t *place;
     float factor;
     const float *by;
-    __device__ __forceinline__ column_t column(int64_t, int) const { return by ? factor * *by : factor; }
+    const int32_t *tokens;
+    __device__ __forceinline__ column_t column(int64_t, int) const { return by && *tokens ? factor * *by : factor; }
     __device__ __forceinline__ more_t get(const spot_t &s, int have) const { return {get4(add, s.row(), s.col(), have), place ? place[s.row()] : 0}; }
     __device__ __forceinline__ float4 apply(const spot_t &s, int have, float4 v, column_t f, const more_t &m) const
     {
