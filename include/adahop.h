@@ -528,6 +528,13 @@ int adahop_debug_force_gemm_kernel(int which);
  * tokens are summed up by a second kernel (1: none).  Returns ADAHOP_E_INVALID_ARG for sizes that it refuses or a null pointer. */
 int adahop_debug_ckpt8_wgrad_plan(int64_t tokens, int64_t d_out, int64_t d_in, int *tile, int *shares, int *slices);
 
+/* The same for a product of adahop_linear_ce_backward (0: the logits, 1: d_h, 2: d_w; of the first piece of the vocabulary) and for one of
+ * adahop_orthogonalize and adahop_muon_update (0: A, 1: its polynomial, 2: the step): *tile = 256, 192, 128 or 64 rows and columns of a workgroup (0: d_w of a few
+ * tokens, without tiles), *alone = 1 where a tile of 128 has a compute unit to itself, else 0, *slices = how many slices of the contraction the tiles of the last
+ * round are cut into (1: none). */
+int adahop_debug_linear_ce_plan(int64_t tokens, int64_t vocab, int64_t dim, int product, int *tile, int *alone, int *slices);
+int adahop_debug_newton_schulz_plan(int64_t rows, int64_t cols, int product, int *tile, int *alone, int *slices);
+
 #ifdef __cplusplus
 }
 #endif

@@ -27,7 +27,7 @@ EXPORTS = ["adahop_quantize_mx", "adahop_iht_quantize", "adahop_foid_topk", "ada
            "adahop_block_norm_backward", "adahop_block_norm_backward_workspace_bytes", "adahop_ckpt8_wgrad", "adahop_ckpt8_wgrad_workspace_bytes",
            "adahop_linear_ce", "adahop_linear_ce_backward", "adahop_linear_ce_workspace_bytes", "adahop_orthogonalize", "adahop_muon_update",
            "adahop_newton_schulz_workspace_bytes",
-           "adahop_select_strategy", "adahop_vote_pattern", "adahop_probe_mfma_rate", "adahop_debug_force_gemm_kernel", "adahop_debug_ckpt8_wgrad_plan", "adahop_prepare_device", "adahop_last_hip_error", "adahop_status_string",
+           "adahop_select_strategy", "adahop_vote_pattern", "adahop_probe_mfma_rate", "adahop_debug_force_gemm_kernel", "adahop_debug_ckpt8_wgrad_plan", "adahop_debug_linear_ce_plan", "adahop_debug_newton_schulz_plan", "adahop_prepare_device", "adahop_last_hip_error", "adahop_status_string",
            "adahop_abi_version"]
 
 
@@ -155,6 +155,8 @@ def lib():
         L.adahop_probe_mfma_rate.argtypes = [I, I, I, I, P, P]
         L.adahop_debug_force_gemm_kernel.argtypes = [I]
         L.adahop_debug_ckpt8_wgrad_plan.argtypes = [I64, I64, I64] + [C.POINTER(C.c_int)] * 3
+        L.adahop_debug_linear_ce_plan.argtypes = [I64, I64, I64, I] + [C.POINTER(C.c_int)] * 3
+        L.adahop_debug_newton_schulz_plan.argtypes = [I64, I64, I] + [C.POINTER(C.c_int)] * 3
         L.adahop_status_string.restype = C.c_char_p
         L.adahop_status_string.argtypes = [I]
         for name in EXPORTS:
@@ -652,3 +654,17 @@ def adahop_muon_update(w, g, momentum, rate, mu=0.95, weight_decay=0.0, nesterov
                                         workspace, stream)
     _check(status, "adahop_muon_update")
     return out
+
+
+def adahop_debug_linear_ce_plan(tokens, vocab, dim, product):
+    """(tile, alone, slices) that adahop_linear_ce_backward takes for the logits (0), d_h (1) or d_w (2)."""
+    out = [C.c_int() for _ in range(3)]
+    _check(lib().adahop_debug_linear_ce_plan(tokens, vocab, dim, product, *(C.byref(v) for v in out)), "adahop_debug_linear_ce_plan")
+    return tuple(v.value for v in out)
+
+
+def adahop_debug_newton_schulz_plan(rows, cols, product):
+    """(tile, alone, slices) that adahop_orthogonalize and adahop_muon_update take for A (0), its polynomial (1) or the step (2)."""
+    out = [C.c_int() for _ in range(3)]
+    _check(lib().adahop_debug_newton_schulz_plan(rows, cols, product, *(C.byref(v) for v in out)), "adahop_debug_newton_schulz_plan")
+    return tuple(v.value for v in out)

@@ -19,10 +19,15 @@ bool valid(const adahop_tensor_t &t, int64_t cols, int64_t max_ld = MAX_LD)
     return (t.f32 == 0 || t.f32 == 1) && t.ld >= cols && t.ld < max_ld && aligned(t.data, t.f32 ? 4 : 2);
 }
 
+bool valid_extents(int64_t tokens, int64_t vocab, int64_t dim)
+{
+    if (tokens < 0 || tokens > MAX_EXTENT || vocab < 1 || vocab > MAX_EXTENT || dim < 1 || dim > MAX_EXTENT) return false;
+    return tokens * dim < MAX_ELEMENTS && vocab * dim < MAX_ELEMENTS && tokens * vocab < MAX_ELEMENTS;
+}
+
 bool valid_loss(const adahop_linear_ce_t *p)
 {
-    if (!p || p->tokens < 0 || p->tokens > MAX_EXTENT || p->vocab < 1 || p->vocab > MAX_EXTENT || p->dim < 1 || p->dim > MAX_EXTENT) return false;
-    if (p->tokens * p->dim >= MAX_ELEMENTS || p->vocab * p->dim >= MAX_ELEMENTS || p->tokens * p->vocab >= MAX_ELEMENTS) return false;
+    if (!p || !valid_extents(p->tokens, p->vocab, p->dim)) return false;
     for (const adahop_tensor_t *t : {&p->h, &p->w})
         if (t->f32 || t->ld < p->dim || t->ld >= MAX_OPERAND_LD || !aligned(t->data, 2)) return false;
     return isfinite(p->logit_scale) && isfinite(p->z_loss);
@@ -31,9 +36,11 @@ bool valid_loss(const adahop_linear_ce_t *p)
 // What both directions read, where there are tokens.
 bool has_operands(const adahop_linear_ce_t &p) { return present(p.h) && present(p.w) && p.targets && aligned(p.targets, 8); }
 
+bool valid_sides(int64_t rows, int64_t cols) { return rows >= 1 && rows <= MAX_SIDE && cols >= 1 && cols <= MAX_SIDE && rows * cols < MAX_MATRIX; }
+
 bool valid_method(const adahop_newton_schulz_t *m)
 {
-    if (!m || m->rows < 1 || m->rows > MAX_SIDE || m->cols < 1 || m->cols > MAX_SIDE || m->rows * m->cols >= MAX_MATRIX) return false;
+    if (!m || !valid_sides(m->rows, m->cols)) return false;
     for (const float f : {m->a, m->b, m->c, m->eps, m->scale})
         if (!isfinite(f)) return false;
     return m->steps >= 1 && m->steps <= MAX_STEPS && m->eps >= 0.0f;
@@ -76,8 +83,7 @@ int adahop_linear_ce_backward(const adahop_linear_ce_t *p, void *workspace, size
 
 size_t adahop_newton_schulz_workspace_bytes(int64_t rows, int64_t cols)
 {
-    if (rows < 1 || rows > MAX_SIDE || cols < 1 || cols > MAX_SIDE || rows * cols >= MAX_MATRIX) return 0;
-    return newton_schulz_workspace_bytes(rows, cols);
+    return valid_sides(rows, cols) ? newton_schulz_workspace_bytes(rows, cols) : 0;
 }
 
 int adahop_orthogonalize(const adahop_newton_schulz_t *method, const adahop_tensor_t *g, const adahop_tensor_t *out, void *workspace,
@@ -98,6 +104,20 @@ int adahop_muon_update(const adahop_newton_schulz_t *method, const adahop_muon_t
     if (!isfinite(p->rate) || !isfinite(p->mu) || !isfinite(p->weight_decay) || (p->nesterov != 0 && p->nesterov != 1)) return ADAHOP_E_INVALID_ARG;
     if (!holds(workspace, workspace_bytes, newton_schulz_workspace_bytes(p->rows, p->cols))) return ADAHOP_E_WORKSPACE;
     return launch_newton_schulz(*method, p->g, {}, p, workspace, static_cast<hipStream_t>(stream));
+}
+
+int adahop_debug_linear_ce_plan(int64_t tokens, int64_t vocab, int64_t dim, int product, int *tile, int *alone, int *slices)
+{
+    if (!valid_extents(tokens, vocab, dim) || tokens < 1 || product < 0 || product > 2 || !tile || !alone || !slices) return ADAHOP_E_INVALID_ARG;
+    linear_ce_plan(tokens, vocab, dim, product, tile, alone, slices);
+    return ADAHOP_OK;
+}
+
+int adahop_debug_newton_schulz_plan(int64_t rows, int64_t cols, int product, int *tile, int *alone, int *slices)
+{
+    if (!valid_sides(rows, cols) || product < 0 || product > 2 || !tile || !alone || !slices) return ADAHOP_E_INVALID_ARG;
+    newton_schulz_plan(rows, cols, product, tile, alone, slices);
+    return ADAHOP_OK;
 }
 
 } // extern "C"

@@ -198,7 +198,9 @@ size_t linear_ce_workspace_bytes(const adahop_linear_ce_t &q, bool backward); //
 int launch_linear_ce(const adahop_linear_ce_t &q, void *workspace, hipStream_t st);
 int launch_linear_ce_backward(const adahop_linear_ce_t &q, void *workspace, hipStream_t st);
 int launch_linear_ce_no_tokens(const adahop_linear_ce_t &q, hipStream_t st); // d_w = add, or 0
+void linear_ce_plan(int64_t tokens, int64_t vocab, int64_t dim, int product, int *tile, int *alone, int *slices); // of the first piece of the vocabulary
 size_t newton_schulz_workspace_bytes(int64_t rows, int64_t cols);
+void newton_schulz_plan(int64_t rows, int64_t cols, int product, int *tile, int *alone, int *slices);
 // out: the result; u: the update of a weight instead (g is its gradient).
 int launch_newton_schulz(const adahop_newton_schulz_t &m, const adahop_tensor_t &g, const adahop_tensor_t &out, const adahop_muon_t *u, void *workspace, hipStream_t st);
 

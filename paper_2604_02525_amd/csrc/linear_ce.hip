@@ -362,6 +362,11 @@ __global__ __launch_bounds__(256) void k_ce_d_w_few(const uint16_t *__restrict__
 }
 
 // ---- host -----------------------------------------------------------------------------------------------------------------------
+// The three products of a piece of the vocabulary.
+plan16_t logits_plan(int64_t T, int64_t words, int64_t D) { return plan16(T, words, align_up(D, 8), false, 1); }
+plan16_t d_h_plan(int64_t T, int64_t words, int64_t D) { return plan16(T, D, words, false); }
+plan16_t d_w_plan(int64_t T, int64_t words, int64_t D) { return plan16(words, D, T, false); }
+
 constexpr int64_t PIECE_BYTES = (int64_t)1 << 30; // of dz in the workspace, at most (one word's column however long)
 
 bool copies_as_it_is(const adahop_tensor_t &x, int64_t cols) { return aligned(x.data, 16) && x.ld % 8 == 0 && cols % 8 == 0; }
@@ -431,7 +436,7 @@ backward_plan_t backward_plan(int64_t T, int64_t V, int64_t D, bool lay_w)
     const size_t ld = align_up(D, 8) * 2;
     const int64_t rest = V - (p.pieces - 1) * p.words;
     size_t part = 0;
-    for (const int64_t words : {p.words, rest}) part = most(part, most(plan16(T, D, words, false).part_bytes, plan16(words, D, T, false).part_bytes));
+    for (const int64_t words : {p.words, rest}) part = most(part, most(d_h_plan(T, words, D).part_bytes, d_w_plan(T, words, D).part_bytes));
     p.dz = 0;
     p.sum_h = align_up((size_t)T * p.ld * 2, 256);
     p.part = align_up(p.sum_h + (p.pieces > 1 ? (size_t)T * D * sizeof(float) : 0), 256);
@@ -486,6 +491,17 @@ size_t linear_ce_workspace_bytes(const adahop_linear_ce_t &q, bool backward)
 {
     const bool lay_h = !copies_as_it_is(q.h, q.dim), lay_w = !copies_as_it_is(q.w, q.dim);
     return backward ? backward_plan(q.tokens, q.vocab, q.dim, lay_w).total : forward_plan(q.tokens, q.vocab, q.dim, lay_h, lay_w).total;
+}
+
+void linear_ce_plan(int64_t T, int64_t V, int64_t D, int product, int *tile, int *alone, int *slices)
+{
+    const int64_t words = backward_plan(T, V, D, false).words;
+    if (product == 2 && T <= FEW_D_W) {
+        *tile = 0, *alone = 0, *slices = 1;
+        return;
+    }
+    const plan16_t p = product == 0 ? logits_plan(T, words, D) : product == 1 ? d_h_plan(T, words, D) : d_w_plan(T, words, D);
+    *tile = p.edge, *alone = alone16(p), *slices = (int)p.slices;
 }
 
 int launch_linear_ce(const adahop_linear_ce_t &c, void *workspace, hipStream_t st)
@@ -555,13 +571,13 @@ int launch_linear_ce_backward(const adahop_linear_ce_t &c, void *workspace, hipS
         q.A = {h, ldh, T}, q.B = piece, q.K = ldh;
         q.rows_of = count;
         const dlogits_t e = {rows, c.logit_scale, c.z_loss, v0, words, ld, dz};
-        if ((rc = launch_product16<false, ALONG, ALONG, false, false>(plan16(T, words, q.K, false, 1), q, e, nullptr, st)) != ADAHOP_OK) return rc;
+        if ((rc = launch_product16<false, ALONG, ALONG, false, false>(logits_plan(T, words, D), q, e, nullptr, st)) != ADAHOP_OK) return rc;
         if (c.d_h.data) { // first: what the caches still hold of w is of use (15 tokens of 4096, 65536 words: 476 us, 491 behind d_w)
             const bool end = i + 1 == p.pieces;
             q.A = {dz, ld, T}, q.B = {piece.data, piece.ld, D}, q.K = words;
             q.rows_of = count, q.K_of = nullptr;
             const grad_t g = {end ? c.d_h : sum_h, i ? sum_h : none, end ? token : nullptr, factor, by, count};
-            if ((rc = launch_product16<false, ALONG, DOWN, false, false>(plan16(T, D, words, false), q, g, ws + p.part, st)) != ADAHOP_OK) return rc;
+            if ((rc = launch_product16<false, ALONG, DOWN, false, false>(d_h_plan(T, words, D), q, g, ws + p.part, st)) != ADAHOP_OK) return rc;
         }
         if (c.d_w.data) {
             const int64_t size = c.d_w.f32 ? 4 : 2, size_add = c.add.f32 ? 4 : 2;
@@ -573,7 +589,7 @@ int launch_linear_ce_backward(const adahop_linear_ce_t &c, void *workspace, hipS
                 k_ce_d_w_few<<<dim3((unsigned)ceil_div(words, D_W_WORDS), (unsigned)ceil_div(D, 1024)), 256, 0, st>>>(h, ldh, dz, ld, count, words, D, g);
                 rc = check_launch();
             } else
-                rc = launch_product16<false, DOWN, DOWN, false, false>(plan16(words, D, T, false), q, g, ws + p.part, st);
+                rc = launch_product16<false, DOWN, DOWN, false, false>(d_w_plan(T, words, D), q, g, ws + p.part, st);
             if (rc != ADAHOP_OK) return rc;
         }
     }

@@ -595,6 +595,13 @@ int configure_newton_schulz()
 
 size_t newton_schulz_workspace_bytes(int64_t rows, int64_t cols) { return ns_plan(rows, cols).total; }
 
+void newton_schulz_plan(int64_t rows, int64_t cols, int product, int *tile, int *alone, int *slices)
+{
+    const ns_plan_t p = ns_plan(rows, cols);
+    const plan16_t &q = product == 0 ? p.gram : product == 1 ? p.poly : p.step;
+    *tile = q.edge, *alone = alone16(q), *slices = (int)q.slices;
+}
+
 int launch_newton_schulz(const adahop_newton_schulz_t &m, const adahop_tensor_t &g, const adahop_tensor_t &out, const adahop_muon_t *u, void *workspace, hipStream_t st)
 {
     int rc = configure_newton_schulz();

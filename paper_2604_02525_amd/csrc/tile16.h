@@ -799,6 +799,9 @@ inline plan16_t plan_direct16(int64_t rows, int64_t cols, int64_t K, bool symmet
     return best;
 }
 
+// Whether a plan's tiles of 128 have a compute unit each.
+inline bool alone16(const plan16_t &plan) { return plan.edge == 128 && plan.whole + (plan.tiles - plan.whole) * plan.slices <= 256; }
+
 template <class K, bool F16, lies_t LA, lies_t LB, bool SEG, bool SYMMETRIC, class E> inline int configure_product16()
 {
     return check_hip(hipFuncSetAttribute(reinterpret_cast<const void *>(&k_product16<K, F16, LA, LB, SEG, SYMMETRIC, E>), hipFuncAttributeMaxDynamicSharedMemorySize, K::LDS));
@@ -825,8 +828,7 @@ inline int launch_product16(const plan16_t &plan, product_t q, const E &e, void 
         if (plan.edge == 256) return launch_tiles16<tile256_t, F16, LA, LB, SEG, SYMMETRIC>(q, plan, e, st);
         if (plan.edge == 192) return launch_tiles16<tile192_t, F16, LA, LB, SEG, SYMMETRIC>(q, plan, e, st);
     }
-    return plan.whole + (plan.tiles - plan.whole) * plan.slices <= 256 ? launch_tiles16<tile128_alone_t, F16, LA, LB, SEG, SYMMETRIC>(q, plan, e, st)
-                                                                       : launch_tiles16<tile128_t, F16, LA, LB, SEG, SYMMETRIC>(q, plan, e, st);
+    return alone16(plan) ? launch_tiles16<tile128_alone_t, F16, LA, LB, SEG, SYMMETRIC>(q, plan, e, st) : launch_tiles16<tile128_t, F16, LA, LB, SEG, SYMMETRIC>(q, plan, e, st);
 }
 
 template <bool F16, bool SEG, bool SYMMETRIC, bool TURNED, class E> inline int configure_direct16()
