@@ -207,9 +207,9 @@ __global__ __launch_bounds__(256) void k_ce_join(loss_t p, const float2 *part, c
 
 // ---- backward -------------------------------------------------------------------------------------------------------------------
 // What dz of a token that has a target needs of it.
-struct token_t {
+struct alignas(16) token_t { // (read in one load)
     float lse, gain; // gain: what exp(z - lse) - [v = target] is multiplied by
-    int32_t target, token;
+    int32_t target;
 };
 
 // dz of a piece of the vocabulary from its logits (rows: tokens, columns: words from v0 on), rounded to bf16; zeros from the piece's end to the row's.
@@ -300,7 +300,7 @@ __global__ __launch_bounds__(256) void k_gather(adahop_tensor_t x, int64_t cols,
     if (threadIdx.x == 0) {
         const int64_t y = p.targets[t];
         const float g = (d_loss ? d_loss[t * d_loss_stride] : 1.0f) * factor;
-        rows[r] = {lse[t], y < p.V ? g : NAN, (int32_t)(y < p.V ? y : 0), t};
+        rows[r] = {lse[t], y < p.V ? g : NAN, (int32_t)(y < p.V ? y : 0)};
     }
     const int64_t from = t * x.ld;
     for (int64_t c = threadIdx.x * 8; c < ld; c += 256 * 8) {
