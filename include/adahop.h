@@ -474,7 +474,7 @@ int adahop_orthogonalize(const adahop_newton_schulz_t *method, const adahop_tens
  *   momentum_out = mu momentum + g,   U = g + mu momentum_out (nesterov) or momentum_out,   X as above
  *   w_out = (1 - rate weight_decay) w - rate scale X,   w_bf16 = w_out rounded (where present)
  * g: of either type.  momentum, momentum_out: float; momentum_out may be momentum.  w, w_out: of one type; w_out may be w.  w_bf16: bf16 or absent.
- * All [rows, cols] of `method`.  rate, mu and weight_decay are finite. */
+ * All [rows, cols] of `method`.  rate, mu and weight_decay are finite.  No other output may overlap an input or another output. */
 typedef struct {
     int64_t rows, cols;
     adahop_tensor_t g, momentum, momentum_out, w, w_out, w_bf16;

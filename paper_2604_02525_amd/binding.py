@@ -627,7 +627,7 @@ def adahop_linear_ce_backward(h, w, targets, lse, d_loss=None, logit_scale=1.0, 
     return out
 
 
-NEWTON_SCHULZ = (3.4445, -4.7750, 2.0315)
+NEWTON_SCHULZ = (3.4445, -4.7750, 2.0315)  # those published with the method (Jordan et al., 2024): five steps bring most singular values between 0.7 and 1.2
 
 
 def adahop_orthogonalize(g, out=None, dtype=torch.bfloat16, steps=5, coefficients=NEWTON_SCHULZ, eps=1e-7, scale=1.0, workspace=None, stream=None):

@@ -3,7 +3,9 @@
 //     z[t, v] = logit_scale sum_d h[t, d] w[v, d],   lse[t] = log sum_v exp z[t, v],   loss[t] = lse - z[t, y_t] + z_loss lse^2
 //     dz[t, v] = d_loss[t] logit_scale ((1 + 2 z_loss lse) exp(z - lse) - [v = y_t]),   d_h = dz w,   d_w = dz^T h
 //
-// Backward, the tokens that have a target are gathered first: the others take no part in either gradient, whatever they hold, and cost nothing.
+// Backward, the tokens that have a target are gathered first: the others take no part in either gradient, whatever they hold.  What they save: d_w's contraction is
+// of the tokens that are left; the logits and d_h have fewer tiles, but not less time until few are left, as those that remain are the first XCDs' (8192 x 4096 x 32000 with one d_loss, none, half, nine tenths of the tokens
+// without a target: 4.91, 4.02 and 2.99 ms).  The forward pass computes all of them: lse is that of every token.
 //
 // Forward: a tile of z (words of the vocabulary by tokens) stays in the matrix cores' accumulators and leaves two numbers per token, its largest logit and
 // the sum of exponentials relative to that; a second kernel joins the tiles of a token.  Backward: a piece of the vocabulary at a time, z is
@@ -14,7 +16,8 @@
 // dz and multiply the products' fp32 sums: the target's element, mostly the largest of its row, is then -1 and little more, which loses next to nothing (8192 x 4096 x 32000: d_h 2.6e-3
 // of its norm off with them inside).  All sums, lse and the loss are fp32.
 //
-// What bounds it: the matrix cores' power (8192 x 4096 x 32000: forward 1.6 ms, 1.35 PFLOP/s; backward, three such products, 4.9 ms, 1.31; 16384 x 8192 x 65536 backward 38.4 ms, 1.37);
+// What bounds it: the matrix cores' power (8192 x 4096 x 32000: forward 1.60 to 1.67 ms on different cards, 1.29 to 1.35 PFLOP/s; backward, three such products, 4.87 to 5.01 ms, 1.29 to 1.32; 16384 x 8192 x 65536 backward 38.7 to
+// 39.8 ms, 1.33 to 1.36);
 // a few tokens: reading w (one of 4096 against 32000 words: 45 us, 5.8 TB/s).  Forward that writes no logits spares 2 T V bytes twice, 0.2 ms of the 1.6 at the copy's rate.
 #include <math.h>
 
@@ -385,7 +388,7 @@ struct backward_plan_t {
 
 constexpr int64_t FEW_LDS = 64 * 1024; // of h: two workgroups on a compute unit, without an attribute
 
-// Time of the logits of V words by tiles of either size, as plan16 sees it.
+// Time of the logits of V words by tiles of either size, as plan16 sees it; a tile of 128 that has a compute unit to itself is of four waves here and takes 0.3 for half a slab.
 double time_of_logits(int64_t T, int64_t V, int64_t D, bool large)
 {
     const int64_t edge = large ? 256 : 128, room = large ? 256 : 512, tiles = ceil_div(T, edge) * ceil_div(V, edge), half_slabs = ceil_div(D, SLAB) * 2, rest = tiles % room;

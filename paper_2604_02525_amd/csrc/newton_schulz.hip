@@ -15,11 +15,12 @@
 // The result of five steps is then 2e-4 to 1.2e-3 of its norm off the same iteration in 64 bits for matrices of random elements and gradients with a few strong directions (bf16's own rounding: 1.7e-3), 4e-3 at most
 // whatever the singular values, 5e-3 where the elements are two or four different numbers; in ten steps 3e-3 and 1.2e-2 (one direction alone: the fp32 iterate's rounding times 3.4445^10).
 //
-// A and A^2 are symmetric: only tiles on and below the diagonal are computed, the mirror image is stored with them.
+// A and A^2 are symmetric: only tiles on and below the diagonal are computed, the mirror image is stored with them.  (Within a tile on the diagonal of an A of two numbers the two halves are sums
+// in another order, equal to rounding.)
 //
-// What bounds it (five steps): large matrices the matrix cores' power, and the step product's end, which reads and writes 10 bytes an element of fp32 and fp16 iterates (28672 x 8192 updated: 28.1 ms,
-// 1.12 PFLOP/s of what is counted once); middle ones rounds of tiles that do not fill the card (4096 x 4096: 1.41 ms, 0.97; 2048 x 2048 updated: 0.35 ms, 0.5), where the split of the last round into slices and the choice of tiles is
-// worth most; small ones 17 launches of some 5 us that wait for each other (256 x 256: 86 us, 185 with tiles of 128 or more).
+// What bounds it (five steps): large matrices the matrix cores' power, and the step product's end, which reads and writes 10 bytes an element of fp32 and fp16 iterates (28672 x 8192 updated: 28.1 to 28.8 ms on different cards,
+// 1.10 to 1.12 PFLOP/s of what is counted once); middle ones rounds of tiles that do not fill the card (4096 x 4096: 1.42 to 1.47 ms, 0.94 to 0.97; 2048 x 2048 updated: 0.35 to 0.37 ms, 0.47 to 0.49), where the split of the last round into slices and the choice of tiles is
+// worth most; small ones 17 launches of some 5 us that wait for each other (256 x 256: 87 us, 185 with tiles of 128 or more).
 #include <math.h>
 
 #include "tile16.h"
@@ -561,7 +562,8 @@ template <bool SEG, bool WIDE> int iterate(const ns_call_t &c, const adahop_newt
     const float k[3] = {m.a, m.b, m.c};
     for (int i = 0; i < m.steps; ++i) {
         // As long as later steps multiply what X lacks by more than 4: with the usual coefficients all but the last two.  (All of them: matrices of no preferred directions are 1.4e-3 off after five steps
-        // instead of 0.8e-3; none or all but the last three: those of half of the directions 4e-3 instead of 1.5e-3.)
+        // instead of 0.8e-3; none or all but the last three: those of half of the directions 4e-3 instead of 1.5e-3; by a
+        // model of the roundings.)
         const bool rounded = !SEG && pow(fabs((double)m.a), m.steps - 1 - i) > 4.0;
         int rc = c.gram<SEG>(i & 1);
         if (rc == ADAHOP_OK) rc = c.poly(k);

@@ -19,6 +19,8 @@
 // LDS layout of a slab of an ALONG operand: 128 bytes a row, its eight pieces of 16 bytes exchanged by a number for the row's bits 1 to 3 (exchange_of).  A read of 16 bytes per lane serves
 // sixteen lanes at a time, not lanes in a row: any two of the sixteen are in different banks for sixteen rows with one piece, for four rows at either end with one piece and
 // the eight between them with its neighbour, and for eight rows with two neighbouring pieces.  With a number that does so for the first alone half of the reads' cycles were conflicts (counted).
+// What conflicts are left are at the ends of symmetric products: put_mirror and k_direct16 read eight rows of a patch in neighbouring lanes eight rows apart, a multiple of 32 banks (33 to 40 % of the LDS cycles of
+// a product of few slabs, 4 % of a long one's).
 #pragma once
 #include "tile_copies.h"
 
