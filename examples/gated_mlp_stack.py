@@ -47,7 +47,7 @@ class GatedMlpStack:
         if vocab:
             self.masters["out"] = torch.randn(vocab, hidden, generator=draw, device=device) * hidden ** -0.5
         self.momentum = {}
-        self.grads = {k: torch.empty_like(w) for k, w in self.masters.items()}
+        self.grads = {k: torch.zeros_like(w) for k, w in self.masters.items()}  # (the output weights stay as they are in steps without words)
         self.round_weights()
 
     def round_weights(self):
