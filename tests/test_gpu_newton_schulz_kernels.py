@@ -69,6 +69,8 @@ def test_against_64_bits(ah, m, n, gram, poly, step):
         space = torch.full((ah.lib().adahop_newton_schulz_workspace_bytes(m, n),), 255, dtype=torch.uint8, device="cuda")  # NaN wherever nothing has been written
         out = ah.adahop_orthogonalize(g, out=room[:m, :n], steps=steps, workspace=space)
         check(out, want, 0.0 if dtype == torch.float32 else BF16)
+        for _ in range(3):
+            assert torch.equal(out, ah.adahop_orthogonalize(g, dtype=dtype, steps=steps)), "other bits in another call"
         assert bool((room[m:] == 7).all()) and bool((room[:, n:] == 7).all())
     common.say("update kernels", m, n)
     w, mom = torch.randn(m, n, device="cuda").mul_(0.02), matrix(n, m).t().contiguous()
